@@ -88,6 +88,7 @@ extern "C" {
 #define KVP_PHASE_PREFILL   0
 #define KVP_PHASE_DECODE    1
 #define KVP_PHASE_BACKWARD  2  /* workspace of kvp_backward (kvp_workspace_size only) */
+#define KVP_PHASE_STEP_FP8  3  /* workspace of kvp_step_fp8, kvp_attention_fp8 (likewise) */
 
 #define KVP_STOP_FIR_MET        0  /* FIR <= 1 + eps                                    */
 #define KVP_STOP_BUDGET         1  /* m conversions made                                */
@@ -288,7 +289,9 @@ int kvp_set_kv_slot(kvp_ctx* ctx, int l, void* K, void* V);
 
 /*
  * kvp_workspace_size -- bytes of device scratch that a call with this phase,
- * batch B and length S (prefill, backward; ignored for decode) needs.  The
+ * batch B and length S (prefill, backward; ignored for decode) needs.  For
+ * KVP_PHASE_STEP_FP8 S is the number of rows of the whole call (kvp_rows.rows, at most
+ * max_batch * max_seq).  The
  * workspace holds Q, the attention output, the fp32 residual stream and its
  * bf16 copy, the RoPE table (prefill) and split-K partial results (decode);
  * for KVP_PHASE_BACKWARD the gradients in flight, (bf16 models) their
@@ -297,7 +300,8 @@ int kvp_set_kv_slot(kvp_ctx* ctx, int l, void* K, void* V);
  * head) softmax statistics, and the producers' fp32 dK/dV sums.  The size never
  * shrinks as B or S grows: a workspace sized for max_batch and max_seq serves
  * every call of its phase.
- * Errors: KVP_E_INVALID_ARG, KVP_E_CAPACITY (B > max_batch, S > max_seq).
+ * Errors: KVP_E_INVALID_ARG, KVP_E_CAPACITY (B > max_batch, S > max_seq), KVP_E_SHAPE
+ * (KVP_PHASE_STEP_FP8 of an fp32 model).
  */
 int kvp_workspace_size(const kvp_ctx* ctx, int phase, int B, int S, size_t* bytes);
 
@@ -433,6 +437,143 @@ int kvp_pager_reserve(kvp_pager* p, int seq, int n_tokens);
 int kvp_pager_release(kvp_pager* p, int seq);
 int kvp_pager_free_pages(const kvp_pager* p, int* n);
 int kvp_pager_rows(const kvp_pager* p, const int32_t* seqs, int B, int32_t* out);
+
+/* ======================================================================== */
+/* 8-bit paged K/V storage                                                    */
+/* ======================================================================== */
+/*
+ * Decode over a long context takes the time of reading the cache (Sec. 4); sharing saves
+ * capacity, not those bytes, since every layer still reads its producer's K/V.  Held in 8 bits,
+ * a pool takes half the bytes of kvp_set_kv_pool's, in capacity and in every read.
+ *
+ * A value is code * scale.  Codes are e4m3 numbers (OCP: 1 sign, 4 exponent, 3 mantissa bits,
+ * largest 448), scales fp32 powers of two, one for each block of 16 positions (16 j ..
+ * 16 j + 15 of a sequence) and KV head, for K and for V.  Page layout, producer l's head-major
+ * pools (bytes), n_pages pages of 64 positions:
+ *     K      [g][n_pages][64][128]         post-RoPE keys
+ *     V      [g][n_pages][4][128][16]      16 positions of one dimension side by side
+ *     scales [g][n_pages][2][4] fp32       K's then V's, one for each 16 positions
+ * The page table and the host page allocator are those of kvp_set_kv_pool's pools.
+ *
+ * Scale of a block: with f(m) = the least power of two s with m <= 448 s, at least 2^-100, and m
+ * the largest magnitude among the values that a call appends to the block, the scale becomes f(m)
+ * where the call fills the block from its first position on, and else the larger of f(m) and the
+ * scale it had; the codes that the block held before the call are then rounded to the larger
+ * scale.  New codes are the nearest to value / scale, ties to even.  If a value is infinite or
+ * NaN, the block's scale becomes NaN and its codes 0 (all 16 positions read as NaN) until the
+ * block is filled again from its first position.
+ */
+
+/* kvp_set_kv_pool_fp8 -- producer l's pools and scales (device, caller-owned, 16-byte
+ * aligned), n_pages pages each.  Independent of the pools of kvp_set_kv_pool.
+ * Errors: KVP_E_INVALID_ARG (NULL, n_pages < 1, l not a producer), KVP_E_SHAPE (fp32 model). */
+int kvp_set_kv_pool_fp8(kvp_ctx* ctx, int l, void* K, void* V, void* scales, int n_pages);
+
+/* kvp_page_bytes_fp8 -- bytes of one page (K, V and scales) in one producer's pools:
+ * g (2 * 64 * d_h + 32).  Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE. */
+int kvp_page_bytes_fp8(const kvp_ctx* ctx, size_t* bytes);
+
+/*
+ * New rows of a call, for B sequences.  Sequence b owns rows cu[b] .. cu[b + 1] - 1 of the call's
+ * tensors (none if they are equal), at positions len[b], len[b] + 1, ...; cu NULL: row b alone,
+ * one new token a sequence.  len[b] < 0 marks an inactive sequence (a padded batch): nothing is
+ * appended for it, and its rows see nothing.
+ * The host values bound the device's, which are not read on the host: cu within [0, rows] and not
+ * decreasing, at most max_new rows a sequence, no row at a position above max_pos.  Rows past
+ * max_new of a sequence count as no sequence's, rows past max_pos see nothing and are not
+ * appended; no device value leads outside a buffer.  A page may appear in several rows of the table
+ * (a shared prefix) as long as no call appends to it.
+ */
+typedef struct kvp_rows {
+    const int32_t* cu;      /* device [B + 1], or NULL                                       */
+    const int32_t* len;     /* device [B]: positions cached before this call                 */
+    const int32_t* pages;   /* device [B][pages_stride] page table                           */
+    int32_t pages_stride;
+    int32_t B;              /* sequences, <= max_batch                                       */
+    int32_t rows;           /* rows of the call's tensors (cu NULL: B)                       */
+    int32_t max_new;        /* most rows of a sequence, <= max_seq (cu NULL: 1)              */
+    int32_t max_pos;        /* last position of any row, < 64 * pages_stride                 */
+} kvp_rows;
+
+/*
+ * kvp_append_fp8 -- appends rows of keys and values to producer l's 8-bit pools, rotated to
+ * their positions on the way, and rotates the call's queries beside them.  q, k, v are bf16
+ * before RoPE: rows of a * d_h, g * d_h, g * d_h values, ld values apart (the parts of one fused
+ * projection, say; ld % 8 == 0, 16-byte aligned).  q_out [rows][a * d_h] receives the rotated
+ * queries in bf16 (q_out == q with ld == a * d_h rotates in place).  Angles are evaluated in double, the rotation in
+ * fp32; keys and values go to 8 bits without a rounding between.  q with q_out, or k with v, may
+ * be NULL together; a consumer's k and v must be (it rotates queries only).  Rows of no
+ * sequence and of inactive ones are left as they are in q_out, positions that are not appended as they
+ * are in the pools (but see the block's scale above).
+ * Errors: KVP_E_INVALID_ARG, KVP_E_CAPACITY, KVP_E_SHAPE, KVP_E_STATE (pools never set), KVP_E_HIP.
+ */
+int kvp_append_fp8(kvp_ctx* ctx, int l, const void* q, const void* k, const void* v, int ld,
+                   const kvp_rows* r, void* q_out, void* stream);
+
+/*
+ * kvp_attention_fp8 -- attention of the rows of q [rows][a * d_h] (bf16, rotated) over the 8-bit
+ * pools of tau(l), into out (same shape, bf16): the row at position p sees positions [0, p], which
+ * must have been appended, its own among them.  One row a sequence is a decode step, more are
+ * proposed tokens or a (part of a) prompt.  Rows of inactive sequences become 0; rows of no
+ * sequence are left as they are.  Products on bf16 matrix cores, e4m3 widened exactly, softmax
+ * statistics and sums in fp32, its weights rounded to bf16.  Workspace: KVP_PHASE_STEP_FP8 with
+ * B and rows.  Errors: as kvp_append_fp8, KVP_E_WORKSPACE.
+ */
+int kvp_attention_fp8(kvp_ctx* ctx, int l, const void* q, const kvp_rows* r, void* out, void* ws,
+                      size_t ws_bytes, void* stream);
+
+/*
+ * kvp_step_fp8 -- rows of new tokens through all L layers on the 8-bit pools: x [rows][h] to
+ * y [rows][h], for each layer projection, kvp_append_fp8, kvp_attention_fp8 and output projection
+ * with the residual, as kvp_decode_step (cu NULL) or kvp_prefill (len 0) do on bf16 storage, and
+ * whatever lies between: chunks of prompts beside single tokens.  Layers with 4-bit weights
+ * (kvp_set_layer_w4) run on those.  Up to 64 rows the projections stay in fp32 up to the
+ * rotation; more are rounded to bf16 before it.  Rows of no sequence and of inactive ones pass
+ * through (y = x).  Workspace: KVP_PHASE_STEP_FP8.  Errors: as kvp_attention_fp8, KVP_E_STATE.
+ */
+int kvp_step_fp8(kvp_ctx* ctx, const void* x, const kvp_rows* r, void* y, void* ws, size_t ws_bytes,
+                 void* stream);
+
+/* ======================================================================== */
+/* 4-bit weights                                                              */
+/* ======================================================================== */
+/*
+ * A small batch's decode takes the time of reading the weights.  Packed weights hold a code c in
+ * 0..15 for every weight and a bf16 scale s for every `group` inputs of an output:
+ * w[n][k] = (c[n][k] - 8) s[n][k / group].  K a multiple of 128, group 32, 64 or 128, any N (at
+ * most 2^20).  Layout, one buffer: for each 16 outputs (the last block filled up with c = 8, s = 0) and
+ * 128 inputs, 64 runs of 16 bytes, run 16 j + i holding output i; its 32-bit word w holds inputs
+ * 32 w + 8 j + 0..7, input 2 e in bits 4 e .. 4 e + 3, input 2 e + 1 in bits 16 + 4 e .. ; then for
+ * each 16 outputs the scales [K / group][16].
+ */
+
+/* kvp_w4_bytes -- bytes of packed weights [N][K].  Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE. */
+int kvp_w4_bytes(int N, int K, int group, size_t* bytes);
+
+/* kvp_pack_w4 -- packs bf16 weights W [N][K]: s = the group's largest magnitude / 7 rounded to bf16, 0
+ * if that is below 2^-100; c = the nearest to w / s, at most 7 (ties to even), + 8; s = 0 leaves
+ * c = 8.  A group with a weight that is not finite gets a NaN scale.  Buffers on the device, 16-byte aligned.
+ * Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE, KVP_E_HIP. */
+int kvp_pack_w4(const void* W, int N, int K, int group, void* packed, void* stream);
+
+/*
+ * kvp_linear_w4 -- y = res + x w^T: x [M][K], res [M][N] (or NULL) and y [M][N] in bf16, packed
+ * weights [N][K]; fp32 sums, rounded once.  y may be res.  Made for few rows (each 64 of them
+ * read the weights once); M at most 2^20.  A row of x that is not finite makes its own row of y
+ * NaN and no other.  Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE, KVP_E_HIP.
+ */
+int kvp_linear_w4(const void* x, const void* packed, const void* res, void* y, int M, int N, int K,
+                  int group, void* stream);
+
+/*
+ * kvp_set_layer_w4 -- packed weights of layer l, shapes as kvp_set_layer's: the decode steps
+ * (kvp_decode_step and its _noalloc and _paged forms, kvp_step_fp8) take them in place of the bf16
+ * ones, which prefill and training go on using and which need not be set for the steps.  Wk and
+ * Wv are NULL for a consumer.  All NULL with group 0 takes them off again.  The pointers are kept, not
+ * copied.  Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE.
+ */
+int kvp_set_layer_w4(kvp_ctx* ctx, int l, const void* Wq, const void* Wk, const void* Wv,
+                     const void* Wo, int group);
 
 /* ======================================================================== */
 /* Training: forward that keeps activations, and the backward pass           */

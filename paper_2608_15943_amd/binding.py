@@ -31,6 +31,7 @@ KVP_DTYPE_FP32 = 1
 KVP_PHASE_PREFILL = 0
 KVP_PHASE_DECODE = 1
 KVP_PHASE_BACKWARD = 2
+KVP_PHASE_STEP_FP8 = 3
 KVP_STOP_FIR_MET = 0
 KVP_STOP_BUDGET = 1
 KVP_STOP_NO_CONVERTIBLE = 2
@@ -47,6 +48,8 @@ EXPORTS = [
     "kvp_set_kv_pool", "kvp_page_bytes", "kvp_prefill_paged", "kvp_decode_step_paged",
     "kvp_pager_create", "kvp_pager_destroy", "kvp_pager_reserve", "kvp_pager_release",
     "kvp_pager_free_pages", "kvp_pager_rows", "kvp_decode_step_noalloc",
+    "kvp_set_kv_pool_fp8", "kvp_page_bytes_fp8", "kvp_append_fp8", "kvp_attention_fp8", "kvp_step_fp8",
+    "kvp_w4_bytes", "kvp_pack_w4", "kvp_linear_w4", "kvp_set_layer_w4",
     # include/kvp_calib.h: achievable-peak calibration (measurement support)
     "kvp_calib_mfma_bf16", "kvp_calib_stream_read",
 ]
@@ -78,6 +81,14 @@ class kvp_model_desc(C.Structure):
                 ("d_h", C.c_int32), ("dtype", C.c_int32), ("rope_base", C.c_double),
                 ("max_batch", C.c_int32), ("max_seq", C.c_int32), ("kv_capacity", C.c_int32),
                 ("_pad", C.c_int32)]
+
+
+class kvp_rows(C.Structure):
+    """New rows of a call on 8-bit pages; cu, len and pages are device addresses (cu 0: one row a
+    sequence)."""
+    _fields_ = [("cu", C.c_void_p), ("len", C.c_void_p), ("pages", C.c_void_p),
+                ("pages_stride", C.c_int32), ("B", C.c_int32), ("rows", C.c_int32),
+                ("max_new", C.c_int32), ("max_pos", C.c_int32)]
 
 
 class KvpError(RuntimeError):
@@ -126,6 +137,15 @@ def lib() -> C.CDLL:
         "kvp_prefill_paged": ([vp, vp, vp, i32, i32, vp, i32, vp, C.c_size_t, vp], i32),
         "kvp_decode_step_paged": ([vp, vp, vp, i32, vp, i32, vp, i32, vp, C.c_size_t, vp], i32),
         "kvp_decode_step_noalloc": ([vp, vp, vp, i32, vp, i32, vp], i32),
+        "kvp_set_kv_pool_fp8": ([vp, i32, vp, vp, vp, i32], i32),
+        "kvp_page_bytes_fp8": ([vp, C.POINTER(C.c_size_t)], i32),
+        "kvp_append_fp8": ([vp, i32, vp, vp, vp, i32, C.POINTER(kvp_rows), vp, vp], i32),
+        "kvp_attention_fp8": ([vp, i32, vp, C.POINTER(kvp_rows), vp, vp, C.c_size_t, vp], i32),
+        "kvp_step_fp8": ([vp, vp, C.POINTER(kvp_rows), vp, vp, C.c_size_t, vp], i32),
+        "kvp_w4_bytes": ([i32, i32, i32, C.POINTER(C.c_size_t)], i32),
+        "kvp_pack_w4": ([vp, i32, i32, i32, vp, vp], i32),
+        "kvp_linear_w4": ([vp, vp, vp, vp, i32, i32, i32, i32, vp], i32),
+        "kvp_set_layer_w4": ([vp, i32, vp, vp, vp, vp, i32], i32),
         "kvp_pager_create": ([i32, i32, i32, C.POINTER(vp)], i32),
         "kvp_pager_destroy": ([vp], None),
         "kvp_pager_reserve": ([vp, i32, i32], i32),
@@ -323,6 +343,29 @@ class Model:
         _check(lib().kvp_decode_step_paged(self.ctx, x, len_dev, max_len, pages_dev, pages_stride, y, B,
                                            ws, ws_bytes, stream or None), "kvp_decode_step_paged")
 
+    def kvp_set_kv_pool_fp8(self, l, k, v, scales, n_pages):
+        _check(lib().kvp_set_kv_pool_fp8(self.ctx, l, k, v, scales, n_pages), "kvp_set_kv_pool_fp8")
+
+    def kvp_page_bytes_fp8(self) -> int:
+        n = C.c_size_t()
+        _check(lib().kvp_page_bytes_fp8(self.ctx, C.byref(n)), "kvp_page_bytes_fp8")
+        return n.value
+
+    def kvp_append_fp8(self, l, q, k, v, ld, rows, q_out, stream=0):
+        _check(lib().kvp_append_fp8(self.ctx, l, q or None, k or None, v or None, ld, C.byref(rows), q_out or None,
+                                    stream or None), "kvp_append_fp8")
+
+    def kvp_attention_fp8(self, l, q, rows, out, ws, ws_bytes, stream=0):
+        _check(lib().kvp_attention_fp8(self.ctx, l, q, C.byref(rows), out, ws, ws_bytes, stream or None),
+               "kvp_attention_fp8")
+
+    def kvp_step_fp8(self, x, rows, y, ws, ws_bytes, stream=0):
+        _check(lib().kvp_step_fp8(self.ctx, x, C.byref(rows), y, ws, ws_bytes, stream or None), "kvp_step_fp8")
+
+    def kvp_set_layer_w4(self, l, wq, wk, wv, wo, group):
+        _check(lib().kvp_set_layer_w4(self.ctx, l, wq or None, wk or None, wv or None, wo or None, group),
+               "kvp_set_layer_w4")
+
     def kvp_profile_enable(self, enable=True):
         _check(lib().kvp_profile_enable(self.ctx, 1 if enable else 0), "kvp_profile_enable")
 
@@ -338,6 +381,23 @@ class Model:
         tau = (C.c_int32 * self.L)()
         _check(lib().kvp_get_map(self.ctx, tau), "kvp_get_map")
         return list(tau)
+
+
+# ---- 4-bit weights -----------------------------------------------------------------------
+
+def kvp_w4_bytes(N: int, K: int, group: int) -> int:
+    n = C.c_size_t()
+    _check(lib().kvp_w4_bytes(N, K, group, C.byref(n)), "kvp_w4_bytes")
+    return n.value
+
+
+def kvp_pack_w4(w: int, N: int, K: int, group: int, packed: int, stream: int = 0) -> None:
+    _check(lib().kvp_pack_w4(w or None, N, K, group, packed or None, stream or None), "kvp_pack_w4")
+
+
+def kvp_linear_w4(x: int, packed: int, res: int, y: int, M: int, N: int, K: int, group: int, stream: int = 0) -> None:
+    _check(lib().kvp_linear_w4(x or None, packed or None, res or None, y or None, M, N, K, group, stream or None),
+           "kvp_linear_w4")
 
 
 # ---- achievable-peak calibration (include/kvp_calib.h) ---------------------------------

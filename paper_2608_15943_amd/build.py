@@ -34,7 +34,8 @@ HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-ffp-contract=off", "-fno-fast-math
               "-I", CSRC, "-Wall"]
 
 HIP_SOURCES = ["gemm_bf16.hip", "flash_prefill.hip", "decode_attn.hip", "decode_gemm.hip",
-               "small_kernels.hip", "calib.hip", "attn_bwd.hip", "bwd_f32.hip", "noalloc.hip"]
+               "small_kernels.hip", "calib.hip", "attn_bwd.hip", "bwd_f32.hip", "noalloc.hip",
+               "append_fp8.hip", "attention_fp8.hip", "linear_w4.hip"]
 HIP_HOST_SOURCES = ["runtime.cpp"]   # host code that calls the HIP runtime
 HOST_SOURCES = ["planner.cpp", "pager.cpp"]   # pure host C++, no HIP
 

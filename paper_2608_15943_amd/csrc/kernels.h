@@ -183,6 +183,57 @@ hipError_t decode_attn_bf16(const uint16_t* q, const uint16_t* kc, const uint16_
 hipError_t decode_combine_bf16(const float* part, const int32_t* lens, uint16_t* o, int B, int a, int g,
                                int cap, int waves, int max_len, hipStream_t st);   // len_b <= max_len
 
+// ---- 8-bit paged cache (bf16 models) ------------------------------------------
+
+// New rows of a call: sequence b owns rows cu[b] .. cu[b + 1] - 1 (cu == nullptr: row b), at
+// positions len[b], len[b] + 1, ... (len[b] < 0: inactive), in the pages of row b of pt.
+struct NewRows {
+    const int32_t* cu;
+    const int32_t* len;
+    const int32_t* pt;
+    int stride, n_pages, B, rows, max_new, max_pos;
+};
+// theta_i = base^(-2i / 128).
+struct RopeFreqs {
+    double v[64];
+};
+
+// Rows of q (nullable; ldq values apart), k and v (nullable together; ldkv), in bf16: q rotated to
+// q_out [rows][a * 128], k rotated and v into the pools (fp8_cache.h).
+hipError_t append_fp8(const NewRows& r, int a, int g, const uint16_t* q, const uint16_t* k, const uint16_t* v, int ldq,
+                      int ldkv, const RopeFreqs& th, uint16_t* q_out, uint8_t* kc, uint8_t* vc, float* sc, hipStream_t st);
+// The same on the sum of the nsplit planes of part ([rows][N], N = n_q (+ 2 n_kv for a producer)).
+hipError_t append_fp8_planes(const NewRows& r, int a, int g, const float* part, int nsplit, int N, bool producer,
+                             const RopeFreqs& th, uint16_t* q_out, uint8_t* kc, uint8_t* vc, float* sc, hipStream_t st);
+// Zeros in the rows of x [rows][n] (n % 8 == 0) that belong to no sequence.
+hipError_t clear_unowned(const NewRows& r, int n, uint16_t* x, hipStream_t st);
+
+// Attention of the rows of q [rows][a * 128] over the pools; part: attention_fp8_floats of
+// scratch.  waves: SIMDs of the device.
+size_t attention_fp8_floats(int waves);
+hipError_t attention_fp8(const NewRows& r, int a, int g, const uint16_t* q, const uint8_t* kc, const uint8_t* vc,
+                         const float* sc, uint16_t* out, float* part, int waves, hipStream_t st);
+
+// ---- 4-bit weights --------------------------------------------------------------
+
+// Up to three packed weights [rows_i][K] stacked along N (layout: linear_w4.hip).
+struct W4Rows {
+    const void* p[3];
+    int rows[3];
+};
+// res [M][N] (nullable; bf16 or fp32) + the product, to y (bf16, nullable) and yf (fp32, nullable).
+struct LinearOut {
+    const void* res;
+    bool res_f32;
+    uint16_t* y;
+    float* yf;
+};
+constexpr int kMaxW4Rows = 1 << 20;
+bool w4_shape_ok(int K, int group);
+size_t w4_bytes(int N, int K, int group);
+hipError_t pack_w4(const uint16_t* w, int N, int K, int group, uint8_t* packed, hipStream_t st);
+hipError_t linear_w4(const uint16_t* x, const W4Rows& w, int M, int K, int group, const LinearOut& o, hipStream_t st);
+
 // ---- shared by both dtypes -------------------------------------------------
 
 // table[pos][i] = (cos, sin)(pos * base^(-2i/d)), evaluated in double.

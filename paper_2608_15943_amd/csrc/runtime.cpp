@@ -11,6 +11,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <cstdlib>
 #include <cstring>
@@ -44,6 +45,12 @@ struct Layer {
     void* kp = nullptr;     // page pools (kvp_set_kv_pool)
     void* vp = nullptr;
     int n_pages = 0;
+    void* kp8 = nullptr;    // 8-bit page pools (kvp_set_kv_pool_fp8)
+    void* vp8 = nullptr;
+    float* sc8 = nullptr;
+    int n_pages8 = 0;
+    const void* w4[4] = {}; // 4-bit weights Q, K, V, O (kvp_set_layer_w4)
+    int group = 0;          // inputs a scale; 0: none set
     bool weights = false;
     float* dwq = nullptr;   // weight gradients (training), fp32
     float* dwk = nullptr;
@@ -93,6 +100,7 @@ struct kvp_ctx {
     std::vector<int32_t> tau;
     std::vector<Layer> layers;
     int decode_waves = 1024;          // decode attention grid: SIMDs of the device
+    kvp::RopeFreqs freqs{};           // rope_base^(-2i / 128) (8-bit cache)
     bool prof = false;
     bool debug_sync = false;          // KVP_DEBUG_SYNC: wait for and check every launch
     std::vector<ProfRec> recs;        // launches timed since the last read
@@ -112,6 +120,7 @@ struct kvp_ctx {
 
 namespace {
 
+// KVP_PHASE_STEP_FP8: S is the number of rows.
 Workspace layout(const kvp_ctx& c, int phase, int B, int S) {
     Workspace w;
     size_t off = 0;
@@ -121,7 +130,7 @@ Workspace layout(const kvp_ctx& c, int phase, int B, int S) {
         return at;
     };
     const size_t e = c.esize();
-    const size_t rows = phase == KVP_PHASE_PREFILL ? (size_t)B * S : (size_t)B;
+    const size_t rows = phase == KVP_PHASE_PREFILL ? (size_t)B * S : phase == KVP_PHASE_STEP_FP8 ? (size_t)S : (size_t)B;
     const size_t nproj = (size_t)(c.d.a + 2 * c.d.g) * c.d.d_h;
     w.q = take(rows * c.n_q() * e);
     w.o = take(rows * c.n_q() * e);
@@ -132,6 +141,12 @@ Workspace layout(const kvp_ctx& c, int phase, int B, int S) {
             w.rope = take((size_t)S * (c.d.d_h / 2) * sizeof(float2));
         else
             w.proj = take(rows * nproj * sizeof(float));
+    } else if (phase == KVP_PHASE_STEP_FP8) {
+        // Few rows: planes of the skinny projection; more: the rows of Q, K and V in bf16.
+        const size_t few = std::min<size_t>(rows, kDecodeMaxRows);
+        const size_t planes = few * nproj * sizeof(float) * kvp::decode_gemm_splits(c.d.h);
+        w.proj = take(rows > few ? std::max(planes, rows * nproj * 2) : planes);
+        w.part = take(kvp::attention_fp8_floats(c.decode_waves) * sizeof(float));
     } else {
         // bf16: one plane per 512-wide K slice of the projection GEMM (K = h for both GEMMs).
         const size_t planes = c.bf16() ? (size_t)kvp::decode_gemm_splits(c.d.h) : 1;
@@ -223,9 +238,11 @@ int timed(kvp_ctx* c, int kind, hipStream_t st, F&& launch) {
     return debug_check(c, kind, st);
 }
 
-int check_layers(const kvp_ctx* c, int lo, int hi, bool paged = false) {
+// w4: the call runs on a layer's 4-bit weights where it has them.
+int check_layers(const kvp_ctx* c, int lo, int hi, bool paged = false, bool w4 = false) {
     for (int l = lo; l < hi; ++l) {
-        if (!c->layers[l].weights) return fail(KVP_E_STATE, "weights of layer %d were never set", l);
+        if (!c->layers[l].weights && !(w4 && c->layers[l].group))
+            return fail(KVP_E_STATE, "weights of layer %d were never set", l);
         const int p = c->tau[l];
         if (paged ? !c->layers[p].kp || !c->layers[p].vp : !c->layers[p].kc || !c->layers[p].vc)
             return fail(KVP_E_STATE, "KV %s of producer %d (used by layer %d) was never set",
@@ -265,6 +282,23 @@ kvp::WRows proj_rows(const kvp_ctx* c, int l, bool producer) {
         w.rows[2] = c->n_kv();
     }
     return w;
+}
+
+// The 4-bit projections of layer l, stacked as proj_rows does.
+kvp::W4Rows proj_rows_w4(const kvp_ctx* c, int l, bool producer) {
+    const Layer& L = c->layers[l];
+    return {{L.w4[0], producer ? L.w4[1] : nullptr, producer ? L.w4[2] : nullptr},
+            {c->n_q(), producer ? c->n_kv() : 0, producer ? c->n_kv() : 0}};
+}
+
+// Output projection and residual of layer l on its 4-bit weights.
+int oproj_w4(kvp_ctx* c, int l, const LayerIO& io, const void* o, int rows, hipStream_t st) {
+    return timed(c, KVP_K_DEC_OPROJ, st, [&] {
+        const kvp::W4Rows w{{c->layers[l].w4[3], nullptr, nullptr}, {c->d.h, 0, 0}};
+        return check_hip(kvp::linear_w4((const uint16_t*)o, w, rows, c->n_q(), c->layers[l].group,
+                                        kvp::LinearOut{io.res, io.res_f32, (uint16_t*)io.y, io.yf}, st),
+                         "output projection (4-bit)");
+    });
 }
 
 // One prefill layer over rows [B*S]: io.a -> projections, io.res + O W_O^T -> io.y
@@ -360,9 +394,10 @@ int run_decode_layer(kvp_ctx* c, int l, const LayerIO& io, const int32_t* lens,
     void* q = ws + w.q;
     void* o = ws + w.o;
     int rc;
-    const int nsplit = c->bf16() ? kvp::decode_gemm_splits(h) : 1;
+    const bool w4 = c->layers[l].group != 0;     // bf16 models only
+    const int nsplit = c->bf16() && !w4 ? kvp::decode_gemm_splits(h) : 1;
     // Small batches: one kernel per projection with its epilogue fused (same sums, bit for bit).
-    const bool fused = c->bf16() && kvp::decode_fused_ok(B, N, h) && kvp::decode_fused_ok(B, h, nq);
+    const bool fused = c->bf16() && !w4 && kvp::decode_fused_ok(B, N, h) && kvp::decode_fused_ok(B, h, nq);
     if (fused) {
         if ((rc = timed(c, KVP_K_DEC_GEMM, st, [&] {
                  return check_hip(kvp::gemm_decode_qkv_fused_bf16((const uint16_t*)io.a, wr, B, N, h, lens, c->d.a,
@@ -373,6 +408,10 @@ int run_decode_layer(kvp_ctx* c, int l, const LayerIO& io, const int32_t* lens,
              })))
             return rc;
     } else if ((rc = timed(c, KVP_K_DEC_GEMM, st, [&] {
+             if (w4)
+                 return check_hip(kvp::linear_w4((const uint16_t*)io.a, proj_rows_w4(c, l, producer), B, h,
+                                                 c->layers[l].group, kvp::LinearOut{nullptr, false, nullptr, proj}, st),
+                                  "decode projection (4-bit)");
              return c->bf16()
                         ? check_hip(kvp::gemm_decode_bf16((const uint16_t*)io.a, wr, B, N, h, proj, st),
                                     "decode projection GEMM")
@@ -410,6 +449,7 @@ int run_decode_layer(kvp_ctx* c, int l, const LayerIO& io, const int32_t* lens,
                                   "decode combine");
              })))
             return rc;
+        if (w4) return oproj_w4(c, l, io, o, B, st);
         if (fused)
             return timed(c, KVP_K_DEC_OPROJ, st, [&] {
                 return check_hip(kvp::gemm_decode_resid_fused_bf16((const uint16_t*)o, wo, B, h, nq, io.res,
@@ -498,6 +538,7 @@ extern "C" int kvp_create(const kvp_model_desc* desc, const int32_t* tau, kvp_ct
     const char* dbg = std::getenv("KVP_DEBUG_SYNC");
     c->debug_sync = dbg && dbg[0] && std::strcmp(dbg, "0") != 0;
     c->layers.resize(d.L);
+    for (int i = 0; i < 64; ++i) c->freqs.v[i] = std::pow(d.rope_base, -2.0 * i / 128.0);
     // Decode attention runs one wave per SIMD of the device current now; without a
     // device (planning-only use) the MI355X's 256 CUs are assumed.
     int dev = 0, cus = 0;
@@ -728,19 +769,24 @@ BwdWs bwd_layout(const kvp_ctx& c, int B, int S) {
 
 extern "C" int kvp_workspace_size(const kvp_ctx* ctx, int phase, int B, int S, size_t* bytes) {
     if (!ctx || !bytes) return fail(KVP_E_INVALID_ARG, "kvp_workspace_size: NULL argument");
-    if (phase != KVP_PHASE_PREFILL && phase != KVP_PHASE_DECODE && phase != KVP_PHASE_BACKWARD)
+    if (phase != KVP_PHASE_PREFILL && phase != KVP_PHASE_DECODE && phase != KVP_PHASE_BACKWARD &&
+        phase != KVP_PHASE_STEP_FP8)
         return fail(KVP_E_INVALID_ARG, "kvp_workspace_size: unknown phase");
     const bool seq = phase != KVP_PHASE_DECODE;
     if (B < 1 || (seq && S < 1))
         return fail(KVP_E_INVALID_ARG, "kvp_workspace_size: B and S must be >= 1");
     if (B > ctx->d.max_batch) return fail(KVP_E_CAPACITY, "kvp_workspace_size: B > max_batch");
-    if (seq && S > ctx->d.max_seq)
+    if (phase == KVP_PHASE_STEP_FP8) {
+        if (!ctx->bf16()) return fail(KVP_E_SHAPE, "kvp_workspace_size: 8-bit K/V storage needs a bf16 model");
+        if (S > (int64_t)ctx->d.max_batch * ctx->d.max_seq)
+            return fail(KVP_E_CAPACITY, "kvp_workspace_size: S > max_batch * max_seq rows");
+    } else if (seq && S > ctx->d.max_seq)
         return fail(KVP_E_CAPACITY, "kvp_workspace_size: S > max_seq");
     if (phase == KVP_PHASE_BACKWARD) {
         *bytes = bwd_layout(*ctx, B, S).total;
         return ok();
     }
-    *bytes = layout(*ctx, phase, B, phase == KVP_PHASE_PREFILL ? S : 1).total;
+    *bytes = layout(*ctx, phase, B, seq ? S : 1).total;
     return ok();
 }
 
@@ -857,7 +903,7 @@ int decode_impl(kvp_ctx* ctx, const void* x, const int32_t* len_dev, int max_len
         return fail(KVP_E_WORKSPACE, "decode: workspace needs %zu bytes (16-byte aligned), got %zu",
                     wfull.total, ws ? ws_bytes : (size_t)0);
     int rc;
-    if ((rc = check_layers(ctx, 0, ctx->d.L, pt != nullptr))) return rc;
+    if ((rc = check_layers(ctx, 0, ctx->d.L, pt != nullptr, true))) return rc;
     hipStream_t st = (hipStream_t)stream;
     char* base = (char*)ws;
     const int L = ctx->d.L;
@@ -914,6 +960,294 @@ extern "C" int kvp_decode_step_paged(kvp_ctx* ctx, const void* x, const int32_t*
     if ((rc = check_paged(ctx, pages, pages_stride, "kvp_decode_step_paged"))) return rc;
     const PageTable pt{pages, pages_stride};
     return decode_impl(ctx, x, len_dev, max_len, y, B, ws, ws_bytes, stream, &pt);
+}
+
+// ============================================================================
+// 8-bit paged K/V and 4-bit weights
+// ============================================================================
+
+extern "C" int kvp_set_kv_pool_fp8(kvp_ctx* ctx, int l, void* K, void* V, void* scales, int n_pages) {
+    if (!ctx) return fail(KVP_E_INVALID_ARG, "kvp_set_kv_pool_fp8: NULL ctx");
+    if (l < 0 || l >= ctx->d.L) return fail(KVP_E_INVALID_ARG, "kvp_set_kv_pool_fp8: layer %d out of range", l);
+    if (ctx->tau[l] != l)
+        return fail(KVP_E_INVALID_ARG, "kvp_set_kv_pool_fp8: layer %d is a consumer and owns no pool", l);
+    if (!ctx->bf16()) return fail(KVP_E_SHAPE, "kvp_set_kv_pool_fp8: 8-bit K/V storage needs a bf16 model");
+    if (!K || !V || !scales || n_pages < 1)
+        return fail(KVP_E_INVALID_ARG, "kvp_set_kv_pool_fp8: NULL pool or scales, or n_pages < 1");
+    if (!aligned16(K) || !aligned16(V) || !aligned16(scales))
+        return fail(KVP_E_INVALID_ARG, "kvp_set_kv_pool_fp8: pools and scales must be 16-byte aligned");
+    Layer& L = ctx->layers[l];
+    L.kp8 = K;
+    L.vp8 = V;
+    L.sc8 = (float*)scales;
+    L.n_pages8 = n_pages;
+    return ok();
+}
+
+extern "C" int kvp_page_bytes_fp8(const kvp_ctx* ctx, size_t* bytes) {
+    if (!ctx || !bytes) return fail(KVP_E_INVALID_ARG, "kvp_page_bytes_fp8: NULL argument");
+    if (!ctx->bf16()) return fail(KVP_E_SHAPE, "kvp_page_bytes_fp8: 8-bit K/V storage needs a bf16 model");
+    *bytes = (size_t)ctx->d.g * (2 * kvp::kPage * 128 + 2 * (kvp::kPage / 16) * sizeof(float));
+    return ok();
+}
+
+namespace {
+
+int check_rows(const kvp_ctx* ctx, const kvp_rows* r, const char* who) {
+    if (!ctx || !r) return fail(KVP_E_INVALID_ARG, "%s: NULL ctx or rows", who);
+    if (!ctx->bf16()) return fail(KVP_E_SHAPE, "%s: 8-bit K/V storage needs a bf16 model", who);
+    if (!r->len || !r->pages || r->pages_stride < 1)
+        return fail(KVP_E_INVALID_ARG, "%s: NULL len or page table, or stride < 1", who);
+    if ((int64_t)r->pages_stride * kvp::kPage > INT32_MAX / 2)
+        return fail(KVP_E_INVALID_ARG, "%s: page table stride %d too large", who, r->pages_stride);
+    if (r->B < 1 || r->rows < 1 || r->max_new < 1 || r->max_pos < 0)
+        return fail(KVP_E_INVALID_ARG, "%s: B, rows, max_new >= 1 and max_pos >= 0 required", who);
+    if (!r->cu && (r->rows != r->B || r->max_new != 1))
+        return fail(KVP_E_INVALID_ARG, "%s: without cu there is one row a sequence (rows == B, max_new == 1)", who);
+    if (r->B > ctx->d.max_batch || r->max_new > ctx->d.max_seq ||
+        r->rows > (int64_t)ctx->d.max_batch * ctx->d.max_seq)
+        return fail(KVP_E_CAPACITY, "%s: B=%d, max_new=%d, rows=%d exceed max_batch=%d / max_seq=%d", who, r->B, r->max_new,
+                    r->rows, ctx->d.max_batch, ctx->d.max_seq);
+    if (r->max_pos >= kvp::kPage * r->pages_stride)
+        return fail(KVP_E_CAPACITY, "%s: position %d does not fit the page table's reach=%d", who, r->max_pos,
+                    kvp::kPage * r->pages_stride);
+    if ((int64_t)r->rows * (ctx->n_q() + 2 * ctx->n_kv()) > INT32_MAX)
+        return fail(KVP_E_SHAPE, "%s: rows exceed the 32-bit index range", who);
+    return KVP_OK;
+}
+
+int check_pool8(const kvp_ctx* ctx, int l, const char* who) {
+    if (l < 0 || l >= ctx->d.L) return fail(KVP_E_INVALID_ARG, "%s: layer %d out of range", who, l);
+    if (!ctx->layers[ctx->tau[l]].kp8)
+        return fail(KVP_E_STATE, "%s: 8-bit pools of producer %d (used by layer %d) were never set", who, ctx->tau[l], l);
+    return KVP_OK;
+}
+
+int check_step_ws(const kvp_ctx* ctx, const kvp_rows* r, const void* ws, size_t ws_bytes, Workspace* w, const char* who) {
+    *w = layout(*ctx, KVP_PHASE_STEP_FP8, r->B, r->rows);
+    if (!ws || ws_bytes < w->total || !aligned16(ws))
+        return fail(KVP_E_WORKSPACE, "%s: workspace needs %zu bytes (16-byte aligned), got %zu", who, w->total,
+                    ws ? ws_bytes : (size_t)0);
+    return KVP_OK;
+}
+
+kvp::NewRows new_rows(const kvp_ctx* ctx, int p, const kvp_rows* r) {
+    return {r->cu, r->len, r->pages, r->pages_stride, ctx->layers[p].n_pages8, r->B, r->rows, r->max_new, r->max_pos};
+}
+
+int run_attention_fp8(kvp_ctx* c, int l, const void* q, const kvp_rows* r, void* out, float* part, hipStream_t st) {
+    const int p = c->tau[l];
+    const Layer& P = c->layers[p];
+    return timed(c, KVP_K_DEC_ATTN, st, [&] {
+        return check_hip(kvp::attention_fp8(new_rows(c, p, r), c->d.a, c->d.g, (const uint16_t*)q, (const uint8_t*)P.kp8,
+                                            (const uint8_t*)P.vp8, P.sc8, (uint16_t*)out, part, c->decode_waves, st),
+                         "attention (8-bit cache)");
+    });
+}
+
+// One layer of kvp_step_fp8.
+int run_step_layer(kvp_ctx* c, int l, const LayerIO& io, const kvp_rows* r, char* ws, const Workspace& w, hipStream_t st) {
+    const int p = c->tau[l], rows = r->rows, h = c->d.h, nq = c->n_q(), nkv = c->n_kv();
+    const bool producer = p == l, few = rows <= kDecodeMaxRows, w4 = c->layers[l].group != 0;
+    const int N = producer ? nq + 2 * nkv : nq;
+    const Layer& L = c->layers[l];
+    const Layer& P = c->layers[p];
+    const kvp::WRows wr = proj_rows(c, l, producer);
+    const uint16_t* a = (const uint16_t*)io.a;
+    uint16_t* q = (uint16_t*)(ws + w.q);
+    void* o = ws + w.o;
+    float* proj = (float*)(ws + w.proj);
+    uint16_t* raw = (uint16_t*)proj;
+    const kvp::NewRows nr = new_rows(c, p, r);
+    int rc;
+    // Few rows: the sums of the projections stay in fp32 up to the rotation; more: bf16 rows.
+    if ((rc = timed(c, KVP_K_DEC_GEMM, st, [&] {
+             if (w4)
+                 return check_hip(kvp::linear_w4(a, proj_rows_w4(c, l, producer), rows, h, L.group,
+                                                 kvp::LinearOut{nullptr, false, few ? nullptr : raw, few ? proj : nullptr}, st),
+                                  "projection (4-bit)");
+             if (few) return check_hip(kvp::gemm_decode_bf16(a, wr, rows, N, h, proj, st), "projection");
+             int r2 = KVP_OK;
+             size_t at = 0;
+             for (int t = 0; t < 3 && !r2; ++t)
+                 if (wr.rows[t]) {
+                     r2 = check_hip(kvp::gemm_out_bf16(a, (const uint16_t*)wr.p[t], rows, wr.rows[t], h, raw + at, st),
+                                    "projection");
+                     at += (size_t)rows * wr.rows[t];
+                 }
+             return r2;
+         })))
+        return rc;
+    if ((rc = timed(c, KVP_K_DEC_ROPE, st, [&] {
+             uint8_t *k8 = (uint8_t*)P.kp8, *v8 = (uint8_t*)P.vp8;
+             if (few)
+                 return check_hip(kvp::append_fp8_planes(nr, c->d.a, c->d.g, proj, w4 ? 1 : kvp::decode_gemm_splits(h), N,
+                                                         producer, c->freqs, q, k8, v8, P.sc8, st),
+                                  "rotation + cache append");
+             // 4-bit products leave whole rows, the others three matrices.
+             const uint16_t* k = w4 ? raw + nq : raw + (size_t)rows * nq;
+             const uint16_t* v = w4 ? k + nkv : k + (size_t)rows * nkv;
+             return check_hip(kvp::append_fp8(nr, c->d.a, c->d.g, raw, producer ? k : nullptr, producer ? v : nullptr,
+                                              w4 ? N : nq, w4 ? N : nkv, c->freqs, q, k8, v8, P.sc8, st),
+                              "rotation + cache append");
+         })))
+        return rc;
+    if ((rc = run_attention_fp8(c, l, q, r, o, (float*)(ws + w.part), st))) return rc;
+    if (w4) return oproj_w4(c, l, io, o, rows, st);
+    return timed(c, few ? KVP_K_DEC_OPROJ : KVP_K_OPROJ_GEMM, st, [&] {
+        kvp::WRows wo{};
+        wo.p[0] = L.wo;
+        wo.rows[0] = h;
+        if (!few)
+            return check_hip(kvp::gemm_resid_bf16((const uint16_t*)o, (const uint16_t*)L.wo, io.res, io.res_f32,
+                                                  (uint16_t*)io.y, io.yf, rows, h, nq, st),
+                             "output projection");
+        if (kvp::decode_fused_ok(rows, h, nq))
+            return check_hip(kvp::gemm_decode_resid_fused_bf16((const uint16_t*)o, wo, rows, h, nq, io.res, io.res_f32,
+                                                               (uint16_t*)io.y, io.yf, st),
+                             "output projection (fused)");
+        int r2 = check_hip(kvp::gemm_decode_bf16((const uint16_t*)o, wo, rows, h, nq, proj, st), "output projection");
+        if (!r2)
+            r2 = check_hip(kvp::decode_resid_bf16(proj, kvp::decode_gemm_splits(nq), rows, h, io.res, io.res_f32,
+                                                  (uint16_t*)io.y, io.yf, st),
+                           "residual");
+        return r2;
+    });
+}
+
+}  // namespace
+
+extern "C" int kvp_append_fp8(kvp_ctx* ctx, int l, const void* q, const void* k, const void* v, int ld, const kvp_rows* r,
+                              void* q_out, void* stream) {
+    int rc;
+    if ((rc = check_rows(ctx, r, "kvp_append_fp8"))) return rc;
+    if ((rc = check_pool8(ctx, l, "kvp_append_fp8"))) return rc;
+    const bool producer = ctx->tau[l] == l;
+    if (!q != !q_out) return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: q and q_out go together");
+    if (!k != !v) return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: k and v go together");
+    if (!producer && k)
+        return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: layer %d shares K/V of layer %d and appends none", l, ctx->tau[l]);
+    if (!q && !k) return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: neither q nor k and v");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || ld % 8)
+        return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: rows must be 16-byte aligned");
+    if (ld < (q ? ctx->n_q() : ctx->n_kv()) || ld < (k ? ctx->n_kv() : 0))
+        return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: ld=%d is shorter than a row", ld);
+    if (q && q == q_out && ld != ctx->n_q())
+        return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: q in place needs ld == a * d_h");
+    const Layer& P = ctx->layers[ctx->tau[l]];
+    hipStream_t st = (hipStream_t)stream;
+    return timed(ctx, KVP_K_DEC_ROPE, st, [&] {
+        return check_hip(kvp::append_fp8(new_rows(ctx, ctx->tau[l], r), ctx->d.a, ctx->d.g, (const uint16_t*)q,
+                                         (const uint16_t*)k, (const uint16_t*)v, ld, ld, ctx->freqs, (uint16_t*)q_out,
+                                         (uint8_t*)P.kp8, (uint8_t*)P.vp8, P.sc8, st),
+                         "rotation + cache append");
+    });
+}
+
+extern "C" int kvp_attention_fp8(kvp_ctx* ctx, int l, const void* q, const kvp_rows* r, void* out, void* ws,
+                                 size_t ws_bytes, void* stream) {
+    int rc;
+    if ((rc = check_rows(ctx, r, "kvp_attention_fp8"))) return rc;
+    if ((rc = check_pool8(ctx, l, "kvp_attention_fp8"))) return rc;
+    if (!q || !out) return fail(KVP_E_INVALID_ARG, "kvp_attention_fp8: NULL q or out");
+    if (q == out) return fail(KVP_E_INVALID_ARG, "kvp_attention_fp8: q and out must not alias");
+    if (!aligned16(q) || !aligned16(out))
+        return fail(KVP_E_INVALID_ARG, "kvp_attention_fp8: q, out must be 16-byte aligned");
+    Workspace w;
+    if ((rc = check_step_ws(ctx, r, ws, ws_bytes, &w, "kvp_attention_fp8"))) return rc;
+    return run_attention_fp8(ctx, l, q, r, out, (float*)((char*)ws + w.part), (hipStream_t)stream);
+}
+
+extern "C" int kvp_step_fp8(kvp_ctx* ctx, const void* x, const kvp_rows* r, void* y, void* ws, size_t ws_bytes,
+                            void* stream) {
+    int rc;
+    if ((rc = check_rows(ctx, r, "kvp_step_fp8"))) return rc;
+    if (!x || !y) return fail(KVP_E_INVALID_ARG, "kvp_step_fp8: NULL x or y");
+    if (x == y) return fail(KVP_E_INVALID_ARG, "kvp_step_fp8: x and y must not alias");
+    if (!aligned16(x) || !aligned16(y)) return fail(KVP_E_INVALID_ARG, "kvp_step_fp8: x, y must be 16-byte aligned");
+    Workspace w;
+    if ((rc = check_step_ws(ctx, r, ws, ws_bytes, &w, "kvp_step_fp8"))) return rc;
+    for (int l = 0; l < ctx->d.L; ++l) {
+        if ((rc = check_pool8(ctx, l, "kvp_step_fp8"))) return rc;
+        if (!ctx->layers[l].weights && !ctx->layers[l].group)
+            return fail(KVP_E_STATE, "kvp_step_fp8: weights of layer %d were never set", l);
+    }
+    hipStream_t st = (hipStream_t)stream;
+    char* base = (char*)ws;
+    // Rows of no sequence pass through: their attention output is 0 (nothing else writes it).
+    if (r->cu && (rc = timed(ctx, KVP_K_DEC_ROPE, st, [&] {
+                      return check_hip(kvp::clear_unowned(new_rows(ctx, 0, r), ctx->n_q(), (uint16_t*)(base + w.o), st),
+                                       "rows of no sequence");
+                  })))
+        return rc;
+    const int L = ctx->d.L;
+    for (int l = 0; l < L; ++l) {
+        const LayerIO io = stack_io(true, l, L, x, y, base, w);
+        if ((rc = run_step_layer(ctx, l, io, r, base, w, st))) return rc;
+    }
+    return ok();
+}
+
+extern "C" int kvp_w4_bytes(int N, int K, int group, size_t* bytes) {
+    if (!bytes || N < 1) return fail(KVP_E_INVALID_ARG, "kvp_w4_bytes: NULL bytes or N < 1");
+    if (!kvp::w4_shape_ok(K, group))
+        return fail(KVP_E_SHAPE, "kvp_w4_bytes: K=%d must be a multiple of 128, group=%d one of 32, 64, 128", K, group);
+    *bytes = kvp::w4_bytes(N, K, group);
+    return ok();
+}
+
+extern "C" int kvp_pack_w4(const void* W, int N, int K, int group, void* packed, void* stream) {
+    if (!W || !packed || N < 1) return fail(KVP_E_INVALID_ARG, "kvp_pack_w4: NULL pointer or N < 1");
+    if (!aligned16(W) || !aligned16(packed)) return fail(KVP_E_INVALID_ARG, "kvp_pack_w4: buffers must be 16-byte aligned");
+    if (!kvp::w4_shape_ok(K, group) || N > kvp::kMaxW4Rows)
+        return fail(KVP_E_SHAPE, "kvp_pack_w4: K=%d must be a multiple of 128, group=%d one of 32, 64, 128, N=%d at most %d", K,
+                    group, N, kvp::kMaxW4Rows);
+    return check_hip(kvp::pack_w4((const uint16_t*)W, N, K, group, (uint8_t*)packed, (hipStream_t)stream), "packing");
+}
+
+extern "C" int kvp_linear_w4(const void* x, const void* packed, const void* res, void* y, int M, int N, int K, int group,
+                             void* stream) {
+    if (!x || !packed || !y || M < 1 || N < 1) return fail(KVP_E_INVALID_ARG, "kvp_linear_w4: NULL pointer, or M or N < 1");
+    if (x == y) return fail(KVP_E_INVALID_ARG, "kvp_linear_w4: x and y must not alias");
+    if (!aligned16(x) || !aligned16(packed) || !aligned16(y) || !aligned16(res))
+        return fail(KVP_E_INVALID_ARG, "kvp_linear_w4: buffers must be 16-byte aligned");
+    if (!kvp::w4_shape_ok(K, group) || N > kvp::kMaxW4Rows || M > kvp::kMaxW4Rows)
+        return fail(KVP_E_SHAPE,
+                    "kvp_linear_w4: K=%d must be a multiple of 128, group=%d one of 32, 64, 128, M=%d and N=%d at most %d", K,
+                    group, M, N, kvp::kMaxW4Rows);
+    const kvp::W4Rows w{{packed, nullptr, nullptr}, {N, 0, 0}};
+    return check_hip(kvp::linear_w4((const uint16_t*)x, w, M, K, group, kvp::LinearOut{res, false, (uint16_t*)y, nullptr},
+                                    (hipStream_t)stream),
+                     "4-bit product");
+}
+
+extern "C" int kvp_set_layer_w4(kvp_ctx* ctx, int l, const void* Wq, const void* Wk, const void* Wv, const void* Wo,
+                                int group) {
+    if (!ctx) return fail(KVP_E_INVALID_ARG, "kvp_set_layer_w4: NULL ctx");
+    if (l < 0 || l >= ctx->d.L) return fail(KVP_E_INVALID_ARG, "kvp_set_layer_w4: layer %d out of range", l);
+    if (!ctx->bf16()) return fail(KVP_E_SHAPE, "kvp_set_layer_w4: 4-bit weights need a bf16 model");
+    Layer& L = ctx->layers[l];
+    if (!group && !Wq && !Wk && !Wv && !Wo) {     // back to the bf16 weights
+        L.group = 0;
+        return ok();
+    }
+    const bool producer = ctx->tau[l] == l;
+    if (!Wq || !Wo) return fail(KVP_E_INVALID_ARG, "kvp_set_layer_w4: Wq and Wo are required");
+    if (producer && (!Wk || !Wv))
+        return fail(KVP_E_INVALID_ARG, "kvp_set_layer_w4: layer %d is a producer and needs Wk, Wv", l);
+    if (!producer && (Wk || Wv))
+        return fail(KVP_E_INVALID_ARG, "kvp_set_layer_w4: layer %d shares K/V of layer %d and takes no Wk, Wv", l,
+                    ctx->tau[l]);
+    if (!aligned16(Wq) || !aligned16(Wk) || !aligned16(Wv) || !aligned16(Wo))
+        return fail(KVP_E_INVALID_ARG, "kvp_set_layer_w4: weights must be 16-byte aligned");
+    if (!kvp::w4_shape_ok(ctx->d.h, group))
+        return fail(KVP_E_SHAPE, "kvp_set_layer_w4: group=%d is not one of 32, 64, 128", group);
+    L.w4[0] = Wq;
+    L.w4[1] = Wk;
+    L.w4[2] = Wv;
+    L.w4[3] = Wo;
+    L.group = group;
+    return ok();
 }
 
 // ============================================================================

@@ -1,0 +1,636 @@
+"""The 8-bit paged cache on the GPU: kvp_append_fp8, kvp_attention_fp8 and kvp_step_fp8 against 64-bit references
+(lowbit_ref.py).  What was never written in the pools holds NaN codes and scales throughout, so a read behind a sequence's
+end shows."""
+import numpy as np
+import pytest
+import torch
+
+import lowbit_ref as lr
+from gpu_util import say
+from paper_2608_15943_amd import binding as kb
+
+pytestmark = pytest.mark.gpu
+D = lr.D
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    kb.lib()
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _normal(rng, *shape, scale=1.0):
+    return lr.bf16(rng.standard_normal(shape).astype(np.float32) * np.float32(scale))
+
+
+def _dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(torch.bfloat16).cuda()
+
+
+class Case:
+    """A cache with `lens` positions in it and rows of Q | K | V for `new` more."""
+
+    def __init__(self, a, g, lens, new, seed, spare=2, stride=None, kscale=1.0, new_scale=1.0, rows=None):
+        rng = np.random.default_rng(seed)
+        self.a, self.g, self.lens, self.new = a, g, lens, new
+        need = lr.pages_for(lens, new)
+        self.table, n_pages = lr.scattered(need, max(need + [1]) if stride is None else stride, spare, seed)
+        self.cache = lr.Cache(g, n_pages, seed)
+        for b, n in enumerate(lens):
+            if n > 0:
+                self.cache.write(self.table, b, rng.standard_normal((2, n, g, D)) * kscale)
+        self.cu = np.concatenate([[0], np.cumsum(new)])
+        self.rows = int(self.cu[-1]) if rows is None else rows
+        self.x = _normal(rng, max(self.rows, 1), a + 2 * g, D, scale=new_scale)
+
+    def kv64(self):
+        """Rotated K and V of every sequence's new rows, of the bf16 numbers that the device is given."""
+        out = []
+        self.x = lr.bf16(self.x)
+        for b, (n, T) in enumerate(zip(self.lens, self.new)):
+            x = self.x[self.cu[b]: self.cu[b] + T].astype(np.float64)
+            k = np.stack([lr.rotate(x[t, self.a: self.a + self.g], n + t) for t in range(T)]) if T else x[:, : self.g]
+            out.append(np.stack([k, x[:, self.a + self.g:]]))
+        return out
+
+    def q64(self):
+        out = np.zeros((max(self.rows, 1), self.a, D))
+        for b, (n, T) in enumerate(zip(self.lens, self.new)):
+            for t in range(T):
+                out[self.cu[b] + t] = lr.rotate(self.x[self.cu[b] + t, : self.a].astype(np.float64), n + t)
+        return out
+
+
+def _append(c, fused=True, cu=True, with_q=True, **kw):
+    """Runs kvp_append_fp8 on a case; the device's pools and q_out."""
+    dev = c.cache.to_device()
+    m = lr.model8(c.a, c.g, dev, c.cache.n_pages, len(c.lens), max(max(c.new), c.rows, 1))
+    r, keep = lr.rows_of(c.lens, c.new, c.table, cu=cu, rows=c.rows, **kw)
+    x = _dev(c.x)
+    q_out = torch.full((max(c.rows, 1), c.a * D), 77.0, dtype=torch.bfloat16, device="cuda")
+    if fused:
+        p, ld = x.data_ptr(), (c.a + 2 * c.g) * D
+        q, k, v = p, p + 2 * c.a * D, p + 2 * (c.a + c.g) * D
+    else:      # three matrices; q's rows are as far apart as k's, behind a gap
+        ld = max(c.a, c.g) * D + 8
+        parts = [torch.zeros(c.x.shape[0], ld, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+        for t, (lo, hi) in zip(parts, ((0, c.a), (c.a, c.a + c.g), (c.a + c.g, c.a + 2 * c.g))):
+            t[:, : (hi - lo) * D] = x[:, lo:hi].reshape(c.x.shape[0], -1)
+        q, k, v = (t.data_ptr() for t in parts)
+    m.kvp_append_fp8(0, q if with_q else 0, k, v, ld, r, q_out.data_ptr() if with_q else 0, _stream())
+    torch.cuda.synchronize()
+    return c.cache.from_device(dev), q_out
+
+
+def _check_q(c, q_out):
+    got, want = q_out.float().cpu().numpy().reshape(-1, c.a, D), c.q64()
+    owned = np.zeros(max(c.rows, 1), bool)
+    for b, (n, T) in enumerate(zip(c.lens, c.new)):
+        if n >= 0:
+            owned[c.cu[b]: c.cu[b] + T] = True
+    # Half a step of bf16, and 2^-22 of the pair for the 32-bit products.
+    tol = 2.0**-8 * np.abs(want) + 2.0**-22 * np.abs(c.x[:, : c.a]).max() * 2
+    assert (np.abs(got - want) <= tol)[owned].all()
+    assert (got[~owned] == 77.0).all()
+
+
+APPEND = [
+    # a, g, cached, new
+    (4, 2, [0], [1]), (4, 2, [977], [1]), (5, 1, [15, 16, 17, 63, 64, 0], [1] * 6),
+    (8, 4, [0, 1, 15, 16, 47, 48, 63, 64, 65], [1, 15, 16, 17, 33, 1, 2, 64, 65]),
+    (16, 1, [3, 0, 7], [0, 5, 0]), (3, 3, [-1, 20, -5, 0], [3, 2, 1, 4]), (64, 8, [100], [3]),
+    (4, 2, [13], [400]),
+]
+
+
+@pytest.mark.parametrize("a,g,lens,new", APPEND)
+@pytest.mark.parametrize("kscale,new_scale", [(1.0, 1.0), (1e-3, 30.0), (30.0, 1e-3)])
+def test_append(a, g, lens, new, kscale, new_scale):
+    """Blocks that begin, go on and end anywhere; the block's scale grown by the new rows, or kept."""
+    say(f"[append] a={a} g={g} lens={lens} new={new} scales={kscale},{new_scale}")
+    c = Case(a, g, lens, new, seed=len(lens) + sum(new), kscale=kscale, new_scale=new_scale)
+    after, q_out = _append(c)
+    lr.check_append(c.cache, after, c.table, lens, new, c.kv64())
+    _check_q(c, q_out)
+
+
+def test_append_one_row_each_without_cu():
+    c = Case(8, 2, [5, -1, 31, 32, 64, 0], [1] * 6, seed=2)
+    after, q_out = _append(c, cu=False)
+    lr.check_append(c.cache, after, c.table, c.lens, c.new, c.kv64())
+    _check_q(c, q_out)
+
+
+def test_append_separate_matrices_without_q():
+    c = Case(4, 2, [30, 2], [5, 20], seed=3)
+    after, _ = _append(c, fused=False)
+    lr.check_append(c.cache, after, c.table, c.lens, c.new, c.kv64())
+    again, q_out = _append(c, fused=False, with_q=False)
+    lr.check_append(c.cache, again, c.table, c.lens, c.new, c.kv64())
+    assert (q_out == 77.0).all()
+
+
+def test_append_many_sequences():
+    """More sequences than a wave has lanes, with and without rows."""
+    n = 150
+    lens = [(7 * i) % 90 - (1 if i % 11 == 0 else 0) for i in range(n)]
+    new = [i % 4 for i in range(n)]
+    c = Case(2, 1, lens, new, seed=4)
+    after, q_out = _append(c)
+    lr.check_append(c.cache, after, c.table, lens, new, c.kv64())
+    _check_q(c, q_out)
+
+
+def test_append_rows_behind_the_last_sequence_and_past_the_bounds():
+    """Rows of no sequence, rows past max_new, positions past max_pos: nothing is written for them."""
+    c = Case(4, 2, [10, 20], [6, 3], seed=5, rows=14)
+    after, q_out = _append(c)
+    lr.check_append(c.cache, after, c.table, c.lens, c.new, c.kv64())
+    _check_q(c, q_out)
+    after, q_out = _append(c, max_new=4)
+    kv = [x[:, :4] for x in c.kv64()]
+    lr.check_append(c.cache, after, c.table, c.lens, [4, 3], kv)
+    assert (q_out[4:6] == 77.0).all() and (q_out[:4] != 77.0).any() and (q_out[6:9] != 77.0).any()
+    after, q_out = _append(c, max_pos=12)
+    lr.check_append(c.cache, after, c.table, [10, -1], [3, 0], c.kv64())
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_append_not_finite(bad):
+    """A block with such a value is NaN as a whole; a call that fills it from its first position makes it new."""
+    c = Case(4, 2, [10, 32], [3, 40], seed=6)
+    c.x[1, c.a, 5] = bad              # K of sequence 0, head 0
+    c.x[3 + 20, c.a + c.g + 1, 7] = bad    # V of sequence 1, head 1
+    with np.errstate(invalid="ignore"):
+        kv = c.kv64()
+    after, _ = _append(c)
+    lr.check_append(c.cache, after, c.table, c.lens, c.new, kv)
+    assert np.isnan(after.s).sum() >= 2
+    # The poisoned block goes on being NaN when more is appended, and not when it begins again.
+    for n, poisoned in ((13, True), (0, False)):
+        d = Case(4, 2, [n, -1], [3, 0], seed=7)
+        d.cache, d.table = after, c.table
+        later, _ = _append(d)
+        assert np.isnan(later.s[0, c.table[0][0], 0, 0]) == poisoned
+        lr.check_append(after, later, c.table, d.lens, d.new, d.kv64())
+
+
+def test_append_values_at_the_ends_of_the_range():
+    """Zeros (the least scale), bf16's smallest and largest numbers, powers of two times 448 and the next number."""
+    c = Case(2, 1, [0, 0, 16, 0, 0, 0], [16, 16, 1, 3, 3, 3], seed=8, kscale=1e-38)
+    c.x[:16] = 0
+    c.x[16:32] = lr.bf16(np.float32(1e-40))
+    c.x[33:36, 2:] = 0
+    c.x[33, 3, 0] = 3.3e38            # V; a K of that size may leave the range as it turns
+    c.x[36:39, 2:] = 0
+    c.x[36, 3, 0], c.x[37, 3, 1] = 448 * 2.0**-5, -449 * 2.0**-5      # 448 in bf16
+    c.x[39:42, 3] = 0
+    c.x[39, 3, 0], c.x[40, 3, 1] = 448 * 2.0**-5, -450 * 2.0**-5
+    after, _ = _append(c)
+    lr.check_append(c.cache, after, c.table, c.lens, c.new, c.kv64())
+
+
+def test_append_far_positions():
+    """The angle of a position past 2^20 in a table of many pages."""
+    n = (1 << 20) + 77
+    stride = n // 64 + 2
+    c = Case(2, 2, [0], [3], seed=9)
+    c.lens, c.table = [n], np.full((1, stride), -1, np.int32)
+    c.table[0, n // 64], c.table[0, n // 64 + 1] = 1, 0
+    c.cache = lr.Cache(2, 2, 9, garbage=False)
+    after, q_out = _append(c)
+    lr.check_append(c.cache, after, c.table, c.lens, c.new, c.kv64())
+    _check_q(c, q_out)
+
+
+def test_append_table_entries_out_of_range_stay_in_the_pool():
+    """Bad page numbers are taken to the pool's first or last page."""
+    c = Case(4, 2, [5, 70], [2, 2], seed=10)
+    c.cache = lr.Cache(2, c.cache.n_pages, 10, garbage=False)
+    good = c.table.copy()
+    good[0, 0], good[1, 1] = 0, c.cache.n_pages - 1
+    c.table = good.copy()
+    c.table[0, 0], c.table[1, 1] = -7, 1 << 30
+    after, _ = _append(c)
+    lr.check_append(c.cache, after, good, c.lens, c.new, c.kv64())
+
+
+def test_append_queries_of_a_consumer_and_in_place():
+    c = Case(4, 2, [33, 0], [2, 5], seed=11)
+    dev = c.cache.to_device()
+    m = lr.model8(4, 2, {0: dev}, c.cache.n_pages, 2, 8, tau=(0, 0))
+    r, keep = lr.rows_of(c.lens, c.new, c.table)
+    q = _dev(c.x[:, :4].reshape(7, -1))
+    m.kvp_append_fp8(1, q.data_ptr(), 0, 0, 4 * D, r, q.data_ptr(), _stream())
+    torch.cuda.synchronize()
+    _check_q(c, q)
+    after = c.cache.from_device(dev)
+    lr.check_append(c.cache, after, c.table, [-1, -1], [0, 0], c.kv64())
+
+
+# ---- attention -----------------------------------------------------------------------------------
+
+def _attention(c, cu=True, pages=None, **kw):
+    """Runs kvp_attention_fp8 on rotated queries over a cache that holds the new rows too; output and the reference."""
+    rng = np.random.default_rng(99)
+    for b, (n, T) in enumerate(zip(c.lens, c.new)):
+        if n >= 0 and T:
+            c.cache.write(c.table, b, rng.standard_normal((2, n + T, c.g, D)) * (1 + np.arange(n + T) % 5)[None, :, None, None])
+    dev = c.cache.to_device()
+    m = lr.model8(c.a, c.g, dev, c.cache.n_pages, len(c.lens), max(max(c.new), c.rows, 1))
+    r, keep = lr.rows_of(c.lens, c.new, c.table, cu=cu, rows=c.rows, **kw)
+    q = _dev(c.x[:, : c.a].reshape(c.x.shape[0], -1))
+    out = torch.full_like(q, 55.0)
+    n = m.kvp_workspace_size(kb.KVP_PHASE_STEP_FP8, len(c.lens), c.rows)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")      # NaN in whatever is read unwritten
+    m.kvp_attention_fp8(0, q.data_ptr(), r, out.data_ptr(), ws.data_ptr(), n, _stream())
+    torch.cuda.synchronize()
+    return out.float().cpu().numpy().reshape(-1, c.a, D)
+
+
+def _check_attention(c, got):
+    owned = np.zeros(got.shape[0], bool)
+    for b, (n, T) in enumerate(zip(c.lens, c.new)):
+        rows = slice(int(c.cu[b]), int(c.cu[b]) + T)
+        owned[rows] = True
+        if n < 0:
+            assert (got[rows] == 0).all(), b
+        elif T:
+            want, tol = lr.attention(c.x[rows, : c.a].astype(np.float64), c.cache.values(c.table, b, n + T), n, c.a)
+            assert np.isfinite(got[rows]).all() and (np.abs(got[rows] - want) <= tol).all(), \
+                (b, np.abs((got[rows] - want) / tol).max())
+    assert (got[~owned] == 55.0).all()
+
+
+ATTN = [
+    # a, g, cached, new: single tokens
+    (4, 2, [0], [1]), (4, 2, [977], [1]), (5, 1, [14, 15, 16, 62, 63, 64, 127], [1] * 7), (16, 1, [300, 5], [1, 1]),
+    (3, 3, [-1, 200, 0, -3], [1] * 4), (32, 8, [1200, 64, 3], [1] * 3),
+    # a few
+    (8, 2, [100, 63, 0], [4, 3, 2]), (16, 1, [70, 6], [2, 5]), (4, 4, [61, 10, 130], [7, 16, 17]), (12, 4, [50, 0], [6, 11]),
+    # chunks
+    (4, 2, [0], [200]), (8, 2, [70, 0, -1, 5], [90, 130, 3, 0]), (5, 1, [33], [77]), (6, 2, [1], [64]),
+    (7, 1, [500, 9], [20, 40]),
+]
+
+
+@pytest.mark.parametrize("a,g,lens,new", ATTN)
+def test_attention(a, g, lens, new):
+    say(f"[attention] a={a} g={g} lens={lens} new={new}")
+    c = Case(a, g, lens, new, seed=sum(new) + 3 * len(lens))
+    _check_attention(c, _attention(c))
+
+
+def test_attention_one_row_each_without_cu():
+    c = Case(8, 2, [5, -1, 31, 1500, 64, 0], [1] * 6, seed=12)
+    _check_attention(c, _attention(c, cu=False))
+
+
+def test_attention_many_sequences():
+    """More sequences than a wave has lanes: single tokens, and a mix with empty ones."""
+    lens = [(37 * i) % 200 - (1 if i % 13 == 0 else 0) for i in range(150)]
+    c = Case(4, 1, lens, [1] * 150, seed=13)
+    _check_attention(c, _attention(c, cu=False))
+    c = Case(4, 1, lens, [i % 4 for i in range(150)], seed=14)
+    _check_attention(c, _attention(c))
+
+
+def test_attention_long_contexts():
+    """Lengths that share the device unevenly: one long, many short ones."""
+    c = Case(8, 2, [9000, 1, 640, 64, 63, 100, 2047], [1] * 7, seed=15)
+    _check_attention(c, _attention(c))
+    c = Case(8, 2, [6000, 300], [3, 70], seed=16)
+    _check_attention(c, _attention(c))
+
+
+def test_attention_rows_of_no_sequence_and_past_the_bounds():
+    c = Case(4, 2, [100, 20], [6, 30], seed=17, rows=40)
+    _check_attention(c, _attention(c))
+    got = _attention(c, max_new=7)
+    d = Case(4, 2, [100, 20], [6, 7], seed=17, rows=40)
+    d.x, d.cache, d.table = c.x, c.cache, c.table
+    _check_attention(d, got)
+    got = _attention(c, max_pos=102)      # the last three rows of sequence 0 see nothing
+    assert (got[3:6] == 0).all()
+    keep = np.r_[0:3, 6:36]
+    want, tol = lr.attention(c.x[:3, :4].astype(np.float64), c.cache.values(c.table, 0, 103), 100, 4)
+    assert (np.abs(got[:3] - want) <= tol).all() and np.isfinite(got[keep]).all()
+
+
+def test_attention_table_entries_out_of_range_stay_in_the_pool():
+    c = Case(4, 2, [5, 70], [2, 2], seed=18)
+    c.cache = lr.Cache(2, c.cache.n_pages, 18, garbage=False)
+    good = c.table.copy()
+    good[0, 0], good[1, 1] = 0, c.cache.n_pages - 1
+    c.table = good
+    got = _attention(c)
+    _check_attention(c, got)
+    bad = good.copy()
+    bad[0, 0], bad[1, 1] = -7, 1 << 30
+    c.table = good.copy()
+    real = lr.rows_of
+    try:
+        lr.rows_of = lambda lens, new, table, **kw: real(lens, new, bad, **kw)
+        assert np.array_equal(_attention(c), got)
+    finally:
+        lr.rows_of = real
+
+
+def test_attention_not_finite():
+    """A NaN block reaches the rows that see it, and no others: not those before it in the same call, not other sequences."""
+    c = Case(4, 2, [40, 40], [30, 3], seed=19)
+    rng = np.random.default_rng(1)
+    for b, n in ((0, 70), (1, 43)):
+        c.cache.write(c.table, b, rng.standard_normal((2, n, 2, D)))
+    page = c.table[0][0]
+    c.cache.s[0, page, 0, 3] = np.nan          # K, head 0, positions 48 .. 63
+    c.cache.k[0, page, 48:64] = 0
+    page = c.table[0][1]
+    c.cache.s[1, page, 1, 0] = np.nan          # V, head 1, positions 64 .. 79
+    c.cache.v[1, page, 0] = 0
+    write = lr.Cache.write
+    try:
+        lr.Cache.write = lambda *a: None
+        got = _attention(c)
+    finally:
+        lr.Cache.write = write
+    for t in range(30):
+        for h in range(4):
+            seen = 40 + t >= (48 if h < 2 else 64)
+            assert np.isnan(got[t, h]).all() == seen and np.isnan(got[t, h]).any() == seen, (t, h)
+    want, tol = lr.attention(c.x[30:33, :4].astype(np.float64), c.cache.values(c.table, 1, 43), 40, 4)
+    assert (np.abs(got[30:] - want) <= tol).all()
+    want, tol = lr.attention(c.x[:8, :4].astype(np.float64), np.nan_to_num(c.cache.values(c.table, 0, 70))[:, :48], 40, 4)
+    assert (np.abs(got[:8] - want) <= tol).all()
+
+
+def test_attention_sharp_and_flat_scores():
+    """Queries so large that one key takes everything, and zero queries that weigh all keys alike."""
+    c = Case(4, 2, [700, 300], [2, 20], seed=20)
+    c.x[0] *= 60
+    c.x[1] = 0
+    c.x[5] *= 200
+    got = _attention(c)
+    want, tol = lr.attention(c.x[:2, :4].astype(np.float64), c.cache.values(c.table, 0, 702), 700, 4)
+    # Scores of the large queries are some 10^4: their 32-bit sums are off by 128 * 2^-24 of the magnitudes summed, which
+    # shifts a weight by a factor of that exponent.
+    k = c.cache.values(c.table, 0, 702)[0]
+    shift = 2 * 128 * 2.0**-24 * np.abs(c.x[0, :4]).max() * np.abs(k).max() * 128 / np.sqrt(D)
+    v = np.abs(c.cache.values(c.table, 0, 702)[1]).max()
+    assert (np.abs(got[0] - want[0]) <= tol[0] + min(1.0, np.expm1(shift)) * v).all()
+    assert (np.abs(got[1] - want[1]) <= tol[1]).all()
+    assert np.isfinite(got).all()
+
+
+def test_attention_pools_past_4_gib():
+    """Pages whose bytes lie past 2^32 in the pool."""
+    g, n_pages = 8, 70000
+    k = torch.empty(g, n_pages, 64, D, dtype=torch.uint8, device="cuda")
+    v = torch.empty(g, n_pages, 4, D, 16, dtype=torch.uint8, device="cuda")
+    s = torch.empty(g, n_pages, 2, 4, device="cuda")
+    lens, new, pages = [100], [40], [69999, 12, 69990]
+    rng = np.random.default_rng(21)
+    x = _normal(rng, 40, 8 + 2 * g, D)
+    kv0 = rng.standard_normal((2, 100, g, D))
+    small = lr.Cache(g, 3)
+    small.write([[0, 1, 2]], 0, kv0)
+    for z, t in ((small.k, k), (small.v, v), (small.s, s)):
+        for i, p in enumerate(pages):
+            t[:, p] = torch.from_numpy(z[:, i].copy()).cuda()
+    m = lr.model8(8, g, (k, v, s), n_pages, 1, 64)
+    r, keep = lr.rows_of(lens, new, [pages])
+    dx = _dev(x.reshape(40, -1))
+    q = torch.empty(40, 8 * D, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(q)
+    p = dx.data_ptr()
+    m.kvp_append_fp8(0, p, p + 2 * 8 * D, p + 2 * 16 * D, 24 * D, r, q.data_ptr(), _stream())
+    n = m.kvp_workspace_size(kb.KVP_PHASE_STEP_FP8, 1, 40)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    m.kvp_attention_fp8(0, q.data_ptr(), r, out.data_ptr(), ws.data_ptr(), n, _stream())
+    torch.cuda.synchronize()
+    after = small.from_device(tuple(t[:, pages] for t in (k, v, s)))
+    kv = np.stack([np.stack([lr.rotate(x[t, 8:16].astype(np.float64), 100 + t) for t in range(40)]), x[:, 16:].astype(np.float64)])
+    lr.check_append(small, after, [[0, 1, 2]], lens, new, [kv])
+    qd = q.float().cpu().numpy().reshape(40, 8, D).astype(np.float64)
+    want, tol = lr.attention(qd, after.values([[0, 1, 2]], 0, 140), 100, 8)
+    assert (np.abs(out.float().cpu().numpy().reshape(40, 8, D) - want) <= tol).all()
+
+
+def test_equal_calls_give_equal_bits():
+    c = Case(8, 2, [3000, 70, 0], [1, 20, 300], seed=22)
+    a, b = _attention(c), _attention(c)
+    assert np.array_equal(a, b)
+    (x, qx), (y, qy) = _append(c), _append(c)
+    assert np.array_equal(x.k, y.k) and np.array_equal(x.v, y.v) and torch.equal(qx, qy)
+
+
+# ---- the stack -----------------------------------------------------------------------------------
+
+class Stack:
+    """A stack on 8-bit pages on the device, and the same on the host in 64 bits with the same roundings of K and V."""
+
+    def __init__(self, a, g, tau, B, stride, seed, w4=None, max_seq=256):
+        rng = np.random.default_rng(seed)
+        self.a, self.g, self.tau, self.h, self.B, self.w4 = a, g, tau, a * D, B, w4
+        perm = rng.permutation(B * stride + 3)
+        self.table = perm[: B * stride].reshape(B, stride).astype(np.int32)
+        self.n_pages = B * stride + 3
+        self.m = kb.Model(len(tau), self.h, a, g, D, kb.KVP_DTYPE_BF16, list(tau), max_batch=B, max_seq=max_seq, kv_capacity=
+                          max(64 * stride, max_seq))
+        self.dev, self.w, self.keep, self.kv = {}, [], [], {}
+        for l, p in enumerate(tau):
+            w = {"q": _normal(rng, self.h, self.h, scale=0.04), "o": _normal(rng, self.h, self.h, scale=0.04)}
+            if l == p:
+                w["k"], w["v"] = (_normal(rng, g * D, self.h, scale=0.04) for _ in range(2))
+                self.dev[l] = lr.Cache(g, self.n_pages, seed + l).to_device()
+                self.m.kvp_set_kv_pool_fp8(l, *(t.data_ptr() for t in self.dev[l]), self.n_pages)
+                self.kv[l] = [np.zeros((2, 0, g, D)) for _ in range(B)]
+            t = {k: _dev(v) for k, v in w.items()}
+            at = lambda k: t[k].data_ptr() if k in t else 0  # noqa: E731
+            if w4 is None or l % 2:         # with w4, the even layers have 4-bit weights and nothing else
+                self.m.kvp_set_layer(l, at("q"), at("k"), at("v"), at("o"))
+            else:
+                for k, x in list(w.items()):
+                    codes, s = lr.w4_codes(x, w4)
+                    w[k] = lr.w4_weights(codes, s, w4)
+                    buf = torch.empty(kb.kvp_w4_bytes(*x.shape, w4), dtype=torch.uint8, device="cuda")
+                    kb.kvp_pack_w4(t[k].data_ptr(), *x.shape, w4, buf.data_ptr(), _stream())
+                    torch.cuda.synchronize()
+                    t[k] = buf
+                self.m.kvp_set_layer_w4(l, at("q"), at("k"), at("v"), at("o"), w4)
+            self.w.append({k: v.astype(np.float64) for k, v in w.items()})
+            self.keep.append(t)
+
+    def step(self, x, lens, new, cu=True, rows=None):
+        """x [rows][h] (bf16 numbers) -> y of the device."""
+        r, keep = lr.rows_of(lens, new, self.table, cu=cu, rows=rows)
+        n = self.m.kvp_workspace_size(kb.KVP_PHASE_STEP_FP8, len(lens), r.rows)
+        ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+        dx = _dev(x)
+        y = torch.full_like(dx, float("nan"))
+        self.m.kvp_step_fp8(dx.data_ptr(), r, y.data_ptr(), ws.data_ptr(), n, _stream())
+        torch.cuda.synchronize()
+        return y.float().cpu().numpy().astype(np.float64)
+
+    def host(self, x, lens, new):
+        """The same step on the host: K and V of a block are rounded together, as the header says."""
+        y = x.astype(np.float64).copy()
+        cu = np.concatenate([[0], np.cumsum(new)])
+        for l, p in enumerate(self.tau):
+            w = self.w[l]
+            for b, (n, T) in enumerate(zip(lens, new)):
+                if n < 0 or not T:
+                    continue
+                rows = slice(cu[b], cu[b] + T)
+                z = y[rows]
+                q = (z @ w["q"].T).reshape(T, self.a, D)
+                q = np.stack([lr.rotate(q[t], n + t) for t in range(T)])
+                if l == p:
+                    k = (z @ w["k"].T).reshape(T, self.g, D)
+                    k = np.stack([lr.rotate(k[t], n + t) for t in range(T)])
+                    v = (z @ w["v"].T).reshape(T, self.g, D)
+                    self.kv[l][b] = self.requant(self.kv[l][b][:, :n], np.stack([k, v]), n)
+                out, _ = lr.attention(q, self.kv[p][b], n, self.a)
+                y[rows] = z + out.reshape(T, -1) @ w["o"].T
+        return y
+
+    @staticmethod
+    def requant(old, new, n):
+        """Positions 0 .. n - 1 as they are held, then `new`: blocks from the one of position n on."""
+        kv = np.concatenate([old, new], 1)
+        for j in range(n // lr.BLK * lr.BLK, kv.shape[1], lr.BLK):
+            for z in range(2):
+                for h in range(kv.shape[2]):
+                    x = kv[z, j: j + lr.BLK, h]
+                    s = lr.scale_of(np.abs(x).max())
+                    kv[z, j: j + lr.BLK, h] = lr.e4m3(x / s) * s
+        return kv
+
+
+@pytest.mark.parametrize("a,g,tau,w4", [(4, 2, (0, 0, 2), None), (4, 1, (0, 0, 0, 3), None), (4, 2, (0, 0, 2, 2), 64)])
+def test_step_chunks_and_tokens(a, g, tau, w4):
+    """Prompts in chunks beside single tokens, then single tokens: every call against the host's stack."""
+    say(f"[step] a={a} g={g} tau={tau} w4={w4}")
+    B = 3
+    s = Stack(a, g, tau, B, 5, seed=30, w4=w4)
+    rng = np.random.default_rng(31)
+    lens = [0, 0, -1]
+    for new in ([37, 5, 2], [20, 1, 0], [66, 30, 0], [1, 1, 1], [1, 1, 1]):
+        if sum(lens[b] >= 0 for b in range(B)) == 2 and new == [1, 1, 1]:
+            lens[2] = 0 if lens[2] < 0 else lens[2]
+        x = _normal(rng, sum(new), s.h)
+        got, want = s.step(x, lens, new), s.host(x, lens, new)
+        e = np.abs(got - want).max() / np.abs(want).max()
+        say(f"  lens={lens} new={new}: {e:.3e}")
+        assert e <= 2e-2, (lens, new, e)
+        cu = np.cumsum([0] + new)
+        if lens[2] < 0:      # inactive: passes through
+            assert np.array_equal(got[cu[2]: cu[3]], x[cu[2]: cu[3]].astype(np.float64))
+        lens = [n + t if n >= 0 else n for n, t in zip(lens, new)]
+
+
+def test_step_rows_of_no_sequence_pass_through():
+    s = Stack(4, 2, (0, 0), 2, 4, seed=32)
+    rng = np.random.default_rng(33)
+    x = _normal(rng, 80, s.h)
+    got = s.step(x, [0, 0], [30, 45], rows=80)
+    assert np.array_equal(got[75:], x[75:].astype(np.float64))
+    want = s.host(x, [0, 0], [30, 45])
+    assert np.abs(got - want).max() / np.abs(want).max() <= 2e-2
+
+
+def test_step_one_token_each_equals_with_cu():
+    """cu NULL and cu = 0, 1, 2, ... are the same call."""
+    rng = np.random.default_rng(34)
+    x = _normal(rng, 90, 512)
+    x2 = _normal(rng, 3, 512)
+    ys = []
+    for cu in (True, False):
+        s = Stack(4, 2, (0, 0), 3, 4, seed=35)
+        s.step(x, [0, 0, 0], [30, 50, 10])
+        ys.append(s.step(x2, [30, 50, 10], [1, 1, 1], cu=cu))
+    assert np.array_equal(ys[0], ys[1])
+
+
+def test_step_in_two_ways_fills_the_same_cache():
+    """A prompt at once and in chunks: outputs agree as far as the roundings of the cache let them."""
+    rng = np.random.default_rng(36)
+    x = _normal(rng, 70, 512)
+    one = Stack(4, 2, (0, 0), 1, 4, seed=37)
+    y1 = one.step(x, [0], [70])
+    two = Stack(4, 2, (0, 0), 1, 4, seed=37)
+    y2 = np.concatenate([two.step(x[lo:hi], [lo], [hi - lo]) for lo, hi in ((0, 16), (16, 48), (48, 70))])
+    # Chunks that end at block ends: the same scales and codes but for sums that differ in their last bits.
+    assert np.abs(y1 - y2).max() / np.abs(y1).max() <= 2e-2
+
+
+def test_step_and_operators_replay_from_a_graph():
+    """A captured step follows the lengths that the device arrays hold at each replay."""
+    s = Stack(4, 2, (0, 0), 3, 4, seed=38)
+    rng = np.random.default_rng(39)
+    s.step(_normal(rng, 90, s.h), [0, 0, 0], [30, 50, 10])
+    r, keep = lr.rows_of([30, 50, 10], [1, 1, 1], s.table, cu=False, max_pos=200)
+    n = s.m.kvp_workspace_size(kb.KVP_PHASE_STEP_FP8, 3, 3)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    x = _dev(_normal(rng, 3, s.h))
+    y = torch.empty_like(x)
+
+    def run():
+        s.m.kvp_step_fp8(x.data_ptr(), r, y.data_ptr(), ws.data_ptr(), n, _stream())
+
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        run()
+    torch.cuda.current_stream().wait_stream(st)
+    torch.cuda.synchronize()
+    start = {l: [t.clone() for t in d] for l, d in s.dev.items()}
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    for rep in range(4):
+        # No further than what has been appended: 31, 51 and 11 positions.
+        lens = torch.tensor([30 - 7 * rep, 50 - 16 * rep, -1 if rep == 2 else 10], dtype=torch.int32, device="cuda")
+        keep["len"].copy_(lens)
+        x.copy_(_dev(_normal(rng, 3, s.h)))
+        res = []
+        for f in (run, g.replay):
+            for l, d in s.dev.items():
+                for t, u in zip(d, start[l]):
+                    t.copy_(u)
+            y.fill_(float("nan"))
+            f()
+            torch.cuda.synchronize()
+            res.append((y.clone(), [t.clone() for d in s.dev.values() for t in d]))
+        assert torch.equal(res[0][0], res[1][0]), rep
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(res[0][1], res[1][1])), rep
+        if rep == 2:
+            assert torch.equal(res[0][0][2], x[2])
+
+
+def test_calls_on_another_stream():
+    """Everything of a call runs on the stream it is given, behind work that is already there."""
+    c = Case(8, 2, [500, 64], [1, 1], seed=40)
+    want = _attention(c)
+    dev = c.cache.to_device()
+    m = lr.model8(8, 2, dev, c.cache.n_pages, 2, 1)
+    r, keep = lr.rows_of(c.lens, c.new, c.table)
+    q0 = _dev(c.x[:, :8].reshape(2, -1))
+    n = m.kvp_workspace_size(kb.KVP_PHASE_STEP_FP8, 2, 2)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    q, out = torch.zeros_like(q0), torch.zeros_like(q0)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        big = torch.randn(4096, 4096, device="cuda")
+        for _ in range(20):
+            big = big @ big * 1e-3
+        q.copy_(q0)
+        m.kvp_attention_fp8(0, q.data_ptr(), r, out.data_ptr(), ws.data_ptr(), n, st.cuda_stream)
+    st.synchronize()
+    assert np.array_equal(out.float().cpu().numpy().reshape(-1, 8, D), want)
