@@ -87,15 +87,15 @@ __device__ __forceinline__ bool find_item(const NewRows& r, int x, Count count, 
             const int v = __shfl_up(pre, off);
             if (lane >= off) pre += v;
         }
-        const int total = __shfl(pre, 63);
+        const int total = __builtin_amdgcn_readlane(pre, 63);
         if (x < base + total) {
             const int w = __popcll(__ballot(base + pre <= x));   // lanes before the one that holds x
             *b = b0 + w;
-            rows->row0 = __shfl(s.row0, w);
-            rows->n = __shfl(s.n, w);
-            rows->len = __shfl(s.len, w);
-            rows->act = __shfl(s.act, w);
-            *first = base + __shfl(pre - c, w);
+            rows->row0 = __builtin_amdgcn_readlane(s.row0, w);
+            rows->n = __builtin_amdgcn_readlane(s.n, w);
+            rows->len = __builtin_amdgcn_readlane(s.len, w);
+            rows->act = __builtin_amdgcn_readlane(s.act, w);
+            *first = base + __builtin_amdgcn_readlane(pre - c, w);
             return true;
         }
         base += total;
