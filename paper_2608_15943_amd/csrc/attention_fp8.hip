@@ -2,11 +2,9 @@
 // a whole prompt; row i of sequence b sits at position len_b + i and sees positions [0, len_b + i].
 //
 // The rows of a sequence and the r = a / g query heads of a K/V head are the columns of one
-// product: an item is m = 16 NB / r rows of a sequence with the r heads of a K/V head, and a wave
-// runs over the item's 64-position tiles (a page each) once, with the running maximum and sum of
-// the softmax, without LDS or barriers: K and V go from memory to registers in 16-byte runs, are
-// widened to bf16 there (exactly: e4m3 has 4 significant bits) and multiplied on
-// v_mfma_f32_16x16x32_bf16.
+// product.  A wave takes 16 or 32 of them over the 64-position tiles (a page each) of their K/V head,
+// each once, with the running maximum and sum of the softmax; codes are widened to bf16 in
+// registers (exactly: e4m3 has 4 significant bits) and multiplied on v_mfma_f32_16x16x32_bf16.
 //
 //   S^T = K Q^T  Row rho of score block tb is position 16 (rho / 4) + 4 tb + rho % 4 of the tile, so
 //                that lane group grp ends with positions 16 grp .. 16 grp + 15: one scale block, and
@@ -16,10 +14,16 @@
 //                bf16 (8 bits); the sum of the weights is taken from the rounded P, so that its
 //                rounding cancels where it is common.
 //
-// Work: the tiles of all items in one list, in the order (sequence, K/V head, block of rows, tile),
-// which W waves share evenly: an item that begins and ends with one wave is written by it, the others
-// leave their pieces (running maximum, sum, unnormalised O) to a second kernel.  Where there are many
-// more items than waves they run one by one instead, the longest first.
+// attention_few_kernel: sequences with at most 16 columns (single tokens, a few proposed ones).  Bound
+// by reading the cache; K and V go straight to registers.  attention_many_kernel: more columns.  Four
+// waves share each tile through LDS; bound by the vector instructions (widening, softmax) beside the
+// matrix ones.
+//
+// Work: the tiles of all items (a sequence's block of rows and a K/V head) in one list, in the order
+// (sequence, K/V head, block, tile), which the waves (workgroups) share evenly: an item that begins
+// and ends with one of them is written by it, the others leave their pieces (running maximum, sum,
+// unnormalised O) to a second kernel.  Where there are many more items than workgroups they run one by
+// one instead, the longest first.
 #include <math.h>
 
 #include <algorithm>
@@ -43,13 +47,8 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-struct KTile {
-    u32x4 k[4][2];     // [score block][64-dimension half]
-    float s;           // scale of the lane group's 16 positions
-};
-struct VTile {
-    u32x4 v[8];        // [16-dimension block]
-    float s;
+struct CutItem {
+    int np, row, n, act, head, pad[3];     // pieces; first row in the tensors, rows (of them act see something), first head
 };
 
 struct AttnArgs {
@@ -59,10 +58,16 @@ struct AttnArgs {
     const uint8_t* vc;
     const float* sc;
     uint16_t* out;
-    float* part;       // [2 waves][cols][PSTRIDE]: slot 2 w: wave w's piece of an item that began before it,
+    float* part;       // [2 W][cols][PSTRIDE]: slot 2 w: share w's piece of an item that began before it,
                        // 2 w + 1: of one that begins with it and goes on
     int a, g;
     int m, cols;       // rows of an item, columns that they make
+    int mw;            // rows of a wave of attention_many_kernel: m / 4
+    // What the join reads: of attention_few_kernel, for each sequence and K/V head the share that
+    // begins it and how many shares have a part; of attention_many_kernel, for each share the item that it
+    // begins and does not end (np 0: none).
+    int2* cut;
+    struct CutItem* cut_many;
     float scale_log2;
 };
 
@@ -96,10 +101,17 @@ __device__ __forceinline__ uint32_t tiles_before(const SeqRows& s, int m, int c)
     return n;
 }
 __device__ __forceinline__ int blocks_of(const SeqRows& s, int m) { return (s.n + m - 1) / m; }
+// FEW: every sequence has one block at most.
+template <bool FEW>
+__device__ __forceinline__ uint32_t seq_tiles(const SeqRows& s, int m) {
+    if (FEW) return s.n ? tiles_of(s, m, 0) : 0;
+    return tiles_before(s, m, blocks_of(s, m));
+}
 
 // The list shared by W waves: wave w starts at tile floor(w T / W).  T < 2^31, W <= 4096.
 struct Split {
     uint32_t T, W, q, rem;
+    Split() = default;
     __device__ __forceinline__ Split(uint32_t T_, uint32_t waves) : T(T_), W(min(T_, waves)), q(T_ / max(W, 1u)), rem(T_ % max(W, 1u)) {}
     __device__ __forceinline__ uint32_t start(uint32_t w) const { return w * q + w * rem / W; }
     // The wave that holds tile x: ceil((x + 1) W / T) - 1; exact in double.
@@ -110,6 +122,7 @@ struct Split {
 
 // 64 sequences at a time, one a lane: their rows, tiles for one K/V head, and the tiles of the list
 // before each.
+template <bool FEW>
 struct Lanes {
     int b0;
     SeqRows s;
@@ -122,7 +135,7 @@ struct Lanes {
         n = 0;
         if (b0 + lane < A.r.B) {
             s = seq_rows(A.r, b0 + lane);
-            n = tiles_before(s, A.m, blocks_of(s, A.m));
+            n = seq_tiles<FEW>(s, A.m);
         }
         uint32_t p = n * A.g;
 #pragma unroll
@@ -138,7 +151,8 @@ struct Lanes {
                 __builtin_amdgcn_readlane(s.len, w), __builtin_amdgcn_readlane(s.act, w)};
     }
 };
-__device__ __forceinline__ uint32_t list_tiles(const AttnArgs& A, Lanes& L) {
+template <bool FEW>
+__device__ __forceinline__ uint32_t list_tiles(const AttnArgs& A, Lanes<FEW>& L) {
     uint32_t T = 0;
     for (int b0 = 0; b0 < A.r.B; b0 += 64) {
         L.load(A, b0, T);
@@ -154,7 +168,8 @@ struct Item {
     int t, n;            // tile, tiles
 };
 // The item that holds tile x of the list (x < T).
-__device__ __forceinline__ Item find_tile(const AttnArgs& A, Lanes& L, uint32_t x) {
+template <bool FEW>
+__device__ __forceinline__ Item find_tile(const AttnArgs& A, Lanes<FEW>& L, uint32_t x) {
     if (A.r.B > 64) {
         uint32_t base = 0;
         for (int b0 = 0;; b0 += 64) {
@@ -172,148 +187,138 @@ __device__ __forceinline__ Item find_tile(const AttnArgs& A, Lanes& L, uint32_t 
     uint32_t rem = x - __builtin_amdgcn_readlane(L.pre, w);
     it.kvh = rem / n;
     rem %= n;
-    int lo = 0, hi = blocks_of(it.s, A.m) - 1;         // the last block with tiles_before <= rem
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (tiles_before(it.s, A.m, mid) <= rem)
-            lo = mid;
-        else
-            hi = mid - 1;
+    it.c = 0;
+    it.t = rem;
+    if (!FEW) {
+        // The last block with tiles_before <= rem.  About c (1 + (len + m / 2) / 64) + c^2 m / 128 tiles lie
+        // before block c: its root, then exactly.
+        const float al = A.m / 128.f, be = 1.f + (max(it.s.len, 0) + 0.5f * A.m) / 64.f;
+        const int cmax = blocks_of(it.s, A.m) - 1;
+        int c = (int)((sqrtf(be * be + 4.f * al * rem) - be) / (2.f * al));
+        c = __builtin_amdgcn_readfirstlane(min(max(c, 0), cmax));
+        uint32_t n0 = tiles_before(it.s, A.m, c);
+        while (c > 0 && n0 > rem) n0 -= tiles_of(it.s, A.m, --c);
+        for (; c < cmax; ++c) {
+            const uint32_t k = tiles_of(it.s, A.m, c);
+            if (n0 + k > rem) break;
+            n0 += k;
+        }
+        it.c = c;
+        it.t = rem - n0;
     }
-    it.c = lo;
-    it.t = rem - (lo ? tiles_before(it.s, A.m, lo) : 0);
-    it.n = tiles_of(it.s, A.m, lo);
+    it.n = tiles_of(it.s, A.m, it.c);
     return it;
 }
 
-// LIST: the wave's share of the list; else item blockIdx.x, counted from the last.
-template <int NB, bool LIST>
-__global__ __launch_bounds__(64, NB == 1 ? 3 : 2) void attention_kernel(AttnArgs A) {
-    const int lane = threadIdx.x, col = lane & 15, grp = lane >> 4;
-    const int r = A.a / A.g;
-    Item it;
-    Lanes L;
-    uint32_t w = 0, left;                       // tiles left of the wave's share
-    if constexpr (LIST) {
-        const Split sp(list_tiles(A, L), gridDim.x);
-        if (blockIdx.x >= sp.W) return;
-        w = xcd_remap(blockIdx.x, sp.W);
-        const uint32_t x = sp.start(w);
-        left = sp.start(w + 1) - x;
-        it = find_tile(A, L, x);
-    } else {
-        // K/V heads change fastest: with 8 of them each XCD reads one of them only.
-        int first;
-        const int x = blockIdx.x / A.g;
-        auto blocks = [&](const SeqRows& s) { return blocks_of(s, A.m); };
-        if (!find_item(A.r, x, blocks, &it.b, &it.s, &first)) return;
-        it.c = blocks_of(it.s, A.m) - 1 - (x - first);
-        it.kvh = blockIdx.x % A.g;
-        it.t = 0;
-        it.n = tiles_of(it.s, A.m, it.c);
-        left = it.n;
+// A share of the list: where it begins and ends.
+template <bool FEW>
+__device__ __forceinline__ bool take_share(const AttnArgs& A, Split* sp, uint32_t* w, uint32_t* left, Item* it) {
+    Lanes<FEW> L;
+    *sp = Split(list_tiles(A, L), gridDim.x);
+    if (blockIdx.x >= sp->W) return false;
+    // Shares in one block on one XCD: neighbours read the same K/V head.
+    *w = xcd_remap(blockIdx.x, sp->W);
+    const uint32_t x = sp->start(*w);
+    *left = sp->start(*w + 1) - x;
+    *it = find_tile(A, L, x);
+    return true;
+}
+// The item behind `it` in the list; false past the end.
+__device__ __forceinline__ bool next_item(const AttnArgs& A, Item& it) {
+    it.t = 0;
+    if (++it.c == blocks_of(it.s, A.m)) {
+        it.c = 0;
+        if (++it.kvh == A.g) {
+            it.kvh = 0;
+            for (++it.b; it.b < A.r.B; ++it.b) {       // sequences without rows have no tiles
+                it.s = seq_rows(A.r, it.b);
+                if (it.s.n) break;
+            }
+            if (it.b >= A.r.B) return false;
+        }
     }
+    it.n = tiles_of(it.s, A.m, it.c);
+    return true;
+}
 
-    // Columns: head tj of row tc of a block; a lane's column of block cb.
-    int tc[NB], tj[NB];
-    bool valid[NB];
-#pragma unroll
-    for (int cb = 0; cb < NB; ++cb) {
-        const int c = 16 * cb + col;
-        valid[cb] = c < A.cols;
-        tc[cb] = valid[cb] ? c / r : 0;
-        tj[cb] = valid[cb] ? c % r : 0;
+// Index of the page of tile it.t, for it.kvh.  A wave keeps 64 entries of a table row, so that one
+// dependent load serves 64 tiles.
+struct Table {
+    int b = -1, c = -1, v = 0;
+    __device__ __forceinline__ size_t page(const AttnArgs& A, const Item& i) {
+        if (i.b != b || (i.t >> 6) != c) {
+            b = i.b;
+            c = i.t >> 6;
+            const int e = 64 * c + (threadIdx.x & 63);
+            v = e < A.r.stride ? A.r.pt[(size_t)i.b * A.r.stride + e] : 0;
+        }
+        const int pg = min(max(__builtin_amdgcn_readlane(v, i.t & 63), 0), A.r.n_pages - 1);
+        return (size_t)i.kvh * A.r.n_pages + pg;
     }
-    // The last position that a column sees, -1 where there is none.
-    auto limit = [&](const Item& i, int cb) {
-        const int t = i.c * A.m + tc[cb];
-        return valid[cb] && t < i.s.act ? i.s.len + t : -1;
-    };
+};
+
+// 16 NB columns of an item, from row t0 of the sequence on: a lane's column of block cb is head tj of
+// row t0 + tc.
+template <int NB>
+struct Columns {
+    bf16x8 q[NB][4];
+    int lim[NB];             // the last position that the column sees, -1 where there is none
+    float m[NB], l[NB];      // running maximum (log2 domain) and sum of the weights
+    f32x4 o[NB][8];          // O^T: dimensions 16 db + 4 grp + 0..3 of the column
+    int all, last;           // positions up to `all` every row sees, past `last` none does
+
+    // Column of block cb: its row, from the item's or wave's first on (past every row where the column
+    // is none of the `rows` rows'), and its head.
+    static __device__ __forceinline__ int row_of(int cb, int rows, int r) {
+        const int c = 16 * cb + (threadIdx.x & 15);
+        return c < rows * r ? c / r : 1 << 30;
+    }
+    static __device__ __forceinline__ int head_of(int cb, int r) { return (16 * cb + (threadIdx.x & 15)) % r; }
+    static __device__ __forceinline__ int limit(const SeqRows& s, int t0, int rows, int r, int cb) {
+        const int t = row_of(cb, rows, r);
+        return t < s.act - t0 ? s.len + t0 + t : -1;
+    }
     // Contraction order of S: step ks of lane group grp holds dimensions 64 (ks / 2) + 16 grp +
     // 8 (ks % 2) .. + 7, the order of the K codes' 16-byte runs.
-    auto load_q = [&](const Item& i, bf16x8 (&qf)[NB][4]) {
+    __device__ __forceinline__ void load_q(const AttnArgs& A, const Item& it, int t0, int rows) {
+        const int grp = (threadIdx.x >> 4) & 3, r = A.a / A.g;
 #pragma unroll
         for (int cb = 0; cb < NB; ++cb) {
-            const bool real = limit(i, cb) >= 0;
-            const size_t row = i.s.row0 + (real ? i.c * A.m + tc[cb] : 0);
-            const uint16_t* p = A.q + (row * A.a + i.kvh * r + tj[cb]) * D + 16 * grp;
+            const bool real = limit(it.s, t0, rows, r, cb) >= 0;
+            const size_t row = it.s.row0 + (real ? t0 + row_of(cb, rows, r) : 0);
+            const uint16_t* p = A.q + (row * A.a + it.kvh * r + head_of(cb, r)) * D + 16 * grp;
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) {
                 u32x4 v = u32x4{0, 0, 0, 0};
                 if (real) v = *(const u32x4*)(p + 64 * (ks >> 1) + 8 * (ks & 1));
-                qf[cb][ks] = as_bf16x8(v);
+                q[cb][ks] = as_bf16x8(v);
             }
         }
-    };
-    // The wave keeps 64 entries of a table row, so that one dependent load serves 64 tiles.
-    int pb = -1, pc = -1, pgv = 0;
-    auto page_at = [&](const Item& i) {
-        if (i.b != pb || (i.t >> 6) != pc) {
-            pb = i.b;
-            pc = i.t >> 6;
-            const int e = 64 * pc + lane;
-            pgv = e < A.r.stride ? A.r.pt[(size_t)i.b * A.r.stride + e] : 0;
-        }
-        const int pg = min(max(__builtin_amdgcn_readlane(pgv, i.t & 63), 0), A.r.n_pages - 1);
-        return (size_t)i.kvh * A.r.n_pages + pg;
-    };
-    const int koff = (16 * (col >> 2) + (col & 3)) * D + 16 * grp, voff = grp * kBlkBytes + col * kBlk;
-    auto load_k = [&](size_t at, KTile& k) {
-        const uint8_t* p = A.kc + at * kPageBytes8 + koff;
-#pragma unroll
-        for (int tb = 0; tb < 4; ++tb)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) k.k[tb][j] = *(const u32x4*)(p + 4 * tb * D + 64 * j);
-        k.s = A.sc[at * 2 * kPageBlks + grp];
-    };
-    auto load_v = [&](size_t at, VTile& v) {
-        const uint8_t* p = A.vc + at * kPageBytes8 + voff;
-#pragma unroll
-        for (int db = 0; db < 8; ++db) v.v[db] = *(const u32x4*)(p + 16 * db * kBlk);
-        v.s = A.sc[at * 2 * kPageBlks + kPageBlks + grp];
-    };
-
-    bf16x8 qf[NB][4];
-    f32x4 o[NB][8];
-    float m_run[NB], l_run[NB];
-    int lim[NB], all = 0, last = 0;
-    // Begins an item (qf loaded).
-    auto begin = [&](const Item& i) {
+    }
+    // Begins rows t0 .. t0 + rows - 1 of a sequence (their queries are loaded).
+    __device__ __forceinline__ void begin(const SeqRows& s, int t0, int rows, int r) {
 #pragma unroll
         for (int cb = 0; cb < NB; ++cb) {
-            lim[cb] = limit(i, cb);
-            m_run[cb] = kNoScore;
-            l_run[cb] = 0.f;
+            lim[cb] = limit(s, t0, rows, r, cb);
+            m[cb] = kNoScore;
+            l[cb] = 0.f;
 #pragma unroll
             for (int db = 0; db < 8; ++db) o[cb][db] = f32x4{};
         }
-        // Positions up to `all` every row sees, past `last` none does.
-        const int rows = min(i.s.act - i.c * A.m, A.m);
-        all = rows > 0 ? i.s.len + i.c * A.m : -1;
-        last = rows > 0 ? i.s.len + i.c * A.m + rows - 1 : -1;
-    };
-
-    KTile kt;
-    VTile vt;
-    f32x4 sc[NB][4];
-    bf16x8 pb16[NB][2];
-    auto scores = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int tb = 0; tb < 4; ++tb)
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                const bf16x8 kf = widen(kt.k[tb][ks >> 1][2 * (ks & 1)], kt.k[tb][ks >> 1][2 * (ks & 1) + 1]);
-#pragma unroll
-                for (int cb = 0; cb < NB; ++cb) sc[cb][tb] = mfma16x16x32(kf, qf[cb][ks], ks ? sc[cb][tb] : f32x4{});
-            }
-    };
-    // Lane (col, grp) holds its column's scores at positions p0 + 4 tb + i.  edge: some column does not
-    // see all of the tile (one branch for all of it: two copies of this code would not fit the registers).
-    auto softmax = [&](bool edge, int p0, float ks) __attribute__((always_inline)) {
+        const int n = min(s.act - t0, rows);
+        all = n > 0 ? s.len + t0 : -1;
+        last = n > 0 ? s.len + t0 + n - 1 : -1;
+    }
+    // Weights of a tile from its scores: lane (column, grp) holds positions p0 + 4 tb + i, whose scales
+    // are ks (times the score factor) and vs; out: the rows of P, pb.  edge: some column does not see all
+    // of the tile (branches around the masks: two copies of this code would not fit the registers).
+    __device__ __forceinline__ void softmax(f32x4 (&sc)[NB][4], bool edge, int p0, float ks, float vs, bf16x8 (&pb)[NB][2]) {
+        // The scales of blocks that no column sees may hold anything.
+        if (edge && p0 > last) ks = vs = 1.f;
         // P 2^e for a V scale of 2^e.
-        const int e = (int)(__float_as_uint(vt.s) >> 23) - 127;
-        const float vexp = vt.s == vt.s ? (float)e : vt.s;
-        const float vinv = vt.s == vt.s ? __uint_as_float((uint32_t)(127 - e) << 23) : 1.f;
+        const int e = (int)(__float_as_uint(vs) >> 23) - 127;
+        const float vexp = vs == vs ? (float)e : vs;
+        const float vinv = vs == vs ? __uint_as_float((uint32_t)(127 - e) << 23) : 1.f;
 #pragma unroll
         for (int cb = 0; cb < NB; ++cb) {
             if (edge) {
@@ -329,20 +334,22 @@ __global__ __launch_bounds__(64, NB == 1 ? 3 : 2) void attention_kernel(AttnArgs
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[cb][tb][i]);
             const float mt = pair32_max(pair16_max(mx * ks));
-            if (__any(mt > m_run[cb] + kLazy)) {
-                const float m_new = fmaxf(m_run[cb], mt);
-                const float alpha = __builtin_amdgcn_exp2f(m_run[cb] - m_new);
-                m_run[cb] = m_new;
-                l_run[cb] *= alpha;
+            if (__any(mt > m[cb] + kLazy)) {
+                const float m_new = fmaxf(m[cb], mt);
+                const float alpha = __builtin_amdgcn_exp2f(m[cb] - m_new);
+                m[cb] = m_new;
+                l[cb] *= alpha;
 #pragma unroll
                 for (int db = 0; db < 8; ++db) o[cb][db] *= alpha;
             }
-            const float sub = vexp - m_run[cb];
+            const float sub = vexp - m[cb];
             uint32_t pw[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                pw[i] = pack2bf(__builtin_amdgcn_exp2f(fmaf(sc[cb][i >> 1][2 * (i & 1)], ks, sub)),
-                                __builtin_amdgcn_exp2f(fmaf(sc[cb][i >> 1][2 * (i & 1) + 1], ks, sub)));
+            for (int tb = 0; tb < 4; ++tb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sc[cb][tb][i] = __builtin_amdgcn_exp2f(fmaf(sc[cb][tb][i], ks, sub));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pw[i] = pack2bf(sc[cb][i >> 1][2 * (i & 1)], sc[cb][i >> 1][2 * (i & 1) + 1]);
             if (edge) {
                 // Whatever a hidden position's scales hold (NaN perhaps), it weighs nothing.
                 const int n = lim[cb] + 1 - p0;       // positions of the lane's 16 that the column sees
@@ -354,41 +361,86 @@ __global__ __launch_bounds__(64, NB == 1 ? 3 : 2) void attention_kernel(AttnArgs
             for (int i = 0; i < 8; ++i)
                 lt = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw[i]),
                                                      __builtin_bit_cast(bf16x2, 0x3F803F80u), lt, false);
-            l_run[cb] += lt * vinv;
-            pb16[cb][0] = as_bf16x8(u32x4{pw[0], pw[1], pw[2], pw[3]});
-            pb16[cb][1] = as_bf16x8(u32x4{pw[4], pw[5], pw[6], pw[7]});
+            l[cb] += lt * vinv;
+            pb[cb][0] = as_bf16x8(u32x4{pw[0], pw[1], pw[2], pw[3]});
+            pb[cb][1] = as_bf16x8(u32x4{pw[4], pw[5], pw[6], pw[7]});
         }
-        if (edge) {
-            // Codes past the last position that a column sees (never written, perhaps) must be finite:
-            // they count as 0.
-            const int n = last + 1 - p0;
+    }
+    // Masks of the words of a lane's V runs at an edge: codes past `last` (never written, perhaps) must be
+    // finite, and count as 0.
+    __device__ __forceinline__ uint32_t v_mask(int p0, int word) const {
+        const int k = last + 1 - p0 - 4 * word;       // bytes of the word that are seen
+        return k >= 4 ? 0xFFFFFFFFu : k <= 0 ? 0u : (1u << (8 * k)) - 1u;
+    }
+    // The end of an item (or of a share inside it): out, or a piece.
+    __device__ __forceinline__ void finish(const AttnArgs& A, const Item& it, int t0, int rows, bool whole, float* piece) {
+        const int grp = (threadIdx.x >> 4) & 3, col = threadIdx.x & 15, r = A.a / A.g;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = n - 4 * i;              // bytes of word i that are seen
-                const uint32_t mask = k >= 4 ? 0xFFFFFFFFu : k <= 0 ? 0u : (1u << (8 * k)) - 1u;
+        for (int cb = 0; cb < NB; ++cb) {
+            const float lsum = pair32_sum(pair16_sum(l[cb]));
+            const int t = row_of(cb, rows, r);
+            if (t >= it.s.n - t0) continue;
+            if (whole) {
+                const float inv = 1.f / lsum;
+                uint16_t* op = A.out + ((size_t)(it.s.row0 + t0 + t) * A.a + it.kvh * r + head_of(cb, r)) * D + 4 * grp;
 #pragma unroll
-                for (int db = 0; db < 8; ++db) vt.v[db][i] &= mask;
+                for (int db = 0; db < 8; ++db) {
+                    u32x2 v = {pack2bf(o[cb][db][0] * inv, o[cb][db][1] * inv),
+                               pack2bf(o[cb][db][2] * inv, o[cb][db][3] * inv)};
+                    if (lim[cb] < 0) v = u32x2{0, 0};      // sees nothing
+                    *(u32x2*)(op + 16 * db) = v;
+                }
+            } else {
+                float* pr = piece + (size_t)(16 * cb + col) * PSTRIDE;
+#pragma unroll
+                for (int db = 0; db < 8; ++db) *(f32x4*)(pr + 16 * db + 4 * grp) = o[cb][db];
+                if (grp == 0) {
+                    pr[D] = m[cb];
+                    pr[D + 1] = lsum;
+                }
             }
         }
-    };
-    auto values = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int db = 0; db < 8; ++db)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const bf16x8 vf = widen(vt.v[db][2 * h], vt.v[db][2 * h + 1]);
-#pragma unroll
-                for (int cb = 0; cb < NB; ++cb) o[cb][db] = mfma16x16x32(vf, pb16[cb][h], o[cb][db]);
-            }
-    };
+    }
+};
 
-    bool whole = it.t == 0;        // the wave has the item from its first tile on
-    load_q(it, qf);
+__global__ __launch_bounds__(64, 3) void attention_few_kernel(AttnArgs A) {
+    const int lane = threadIdx.x, col = lane & 15, grp = lane >> 4;
+    Item it;
+    Split sp;
+    uint32_t w, left;
+    if (!take_share<true>(A, &sp, &w, &left, &it)) return;
+    Columns<1> C;
+    const int r = A.a / A.g;
+    Table tab;
+    u32x4 k[4][2], v[8];         // [score block][64-dimension half], [16-dimension block]
+    float ks, vs;                // scales of the lane group's 16 positions
+    const int koff = (16 * (col >> 2) + (col & 3)) * D + 16 * grp, voff = grp * kBlkBytes + col * kBlk;
+    auto load_k = [&](size_t at) {
+        const uint8_t* p = A.kc + at * kPageBytes8 + koff;
+#pragma unroll
+        for (int tb = 0; tb < 4; ++tb)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) k[tb][j] = *(const u32x4*)(p + 4 * tb * D + 64 * j);
+        ks = A.sc[at * 2 * kPageBlks + grp];
+    };
+    auto load_v = [&](size_t at) {
+        const uint8_t* p = A.vc + at * kPageBytes8 + voff;
+        vs = A.sc[at * 2 * kPageBlks + kPageBlks + grp];
+#pragma unroll
+        for (int db = 0; db < 8; ++db) v[db] = *(const u32x4*)(p + 16 * db * kBlk);
+    };
+    bool whole = it.t == 0;        // the share has the item from its first tile on
+    uint32_t x = sp.start(w);      // the list's tile
+    auto begin = [&](const Item& i) {
+        C.begin(i.s, i.c * A.m, A.m, r);
+        if (whole && lane == 0) A.cut[i.b * A.g + i.kvh] = make_int2(w, sp.wave_of(x + i.n - 1) - w + 1);
+    };
+    C.load_q(A, it, it.c * A.m, A.m);
     begin(it);
     {
-        const size_t at = page_at(it);
-        load_k(at, kt);
-        load_v(at, vt);
+        const size_t at = tab.page(A, it);
+        load_k(at);
+        load_v(at);
     }
     for (;;) {
         // The next tile of the share, perhaps in the next item.
@@ -396,126 +448,268 @@ __global__ __launch_bounds__(64, NB == 1 ? 3 : 2) void attention_kernel(AttnArgs
         bool more = left > 1;
         Item nx = it;
         if (more) {
-            ++nx.t;
-            if (LIST && ends) {
-                nx.t = 0;
-                if (++nx.c == blocks_of(nx.s, A.m)) {
-                    nx.c = 0;
-                    if (++nx.kvh == A.g) {
-                        nx.kvh = 0;
-                        for (++nx.b; nx.b < A.r.B; ++nx.b) {       // sequences without rows have no tiles
-                            if (nx.b - L.b0 == 64) L.load(A, nx.b, 0);
-                            if (__builtin_amdgcn_readlane(L.n, nx.b - L.b0)) break;
-                        }
-                        more = nx.b < A.r.B;
-                        if (more) nx.s = L.rows(nx.b - L.b0);
-                    }
-                }
-                nx.n = tiles_of(nx.s, A.m, nx.c);
-            }
+            if (ends)
+                more = next_item(A, nx);
+            else
+                ++nx.t;
         }
-        const size_t at = more ? page_at(nx) : 0;
-        const int t0 = TILE * it.t, p0 = t0 + 16 * grp;
-        scores();
-        const float ks = kt.s * A.scale_log2;
+        const size_t at = more ? tab.page(A, nx) : 0;
+        const int p0 = TILE * it.t + 16 * grp;
+        const bool edge = TILE * it.t + TILE - 1 > C.all;
+        f32x4 sc[1][4];
+#pragma unroll
+        for (int tb = 0; tb < 4; ++tb)
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                sc[0][tb] = mfma16x16x32(widen(k[tb][s >> 1][2 * (s & 1)], k[tb][s >> 1][2 * (s & 1) + 1]), C.q[0][s],
+                                         s ? sc[0][tb] : f32x4{});
+        const float kf = ks * A.scale_log2;
         __builtin_amdgcn_sched_barrier(0);
         // A part of a tile (and the queries) is requested again as soon as it has been multiplied: 16
         // KB a wave are always under way, without a second set of registers.
         if (more) {
-            load_k(at, kt);
-            if (LIST && ends) load_q(nx, qf);
+            load_k(at);
+            if (ends) C.load_q(A, nx, nx.c * A.m, A.m);
         }
         __builtin_amdgcn_sched_barrier(0);
-        const bool edge = t0 + TILE - 1 > all;
-        // The scales of blocks that no column sees may hold anything.
-        if (edge && p0 > last) vt.s = 1.f;
-        softmax(edge, p0, edge && p0 > last ? A.scale_log2 : ks);
+        bf16x8 pb[1][2];
+        C.softmax(sc, edge, p0, kf, vs, pb);
+        if (edge) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t mask = C.v_mask(p0, i);
+#pragma unroll
+                for (int db = 0; db < 8; ++db) v[db][i] &= mask;
+            }
+        }
         __builtin_amdgcn_sched_barrier(0);
-        values();
+#pragma unroll
+        for (int db = 0; db < 8; ++db)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                C.o[0][db] = mfma16x16x32(widen(v[db][2 * h], v[db][2 * h + 1]), pb[0][h], C.o[0][db]);
         __builtin_amdgcn_sched_barrier(0);
-        if (more) load_v(at, vt);
+        if (more) load_v(at);
         if (ends || !more) {
-            // O^T block db: lane holds dimensions 16 db + 4 grp + 0..3 of its column.
-#pragma unroll
-            for (int cb = 0; cb < NB; ++cb) {
-                const float l = pair32_sum(pair16_sum(l_run[cb]));
-                const int t = it.c * A.m + tc[cb];
-                if (!valid[cb] || t >= it.s.n) continue;
-                if (whole && ends) {
-                    const float inv = 1.f / l;
-                    uint16_t* op = A.out + ((size_t)(it.s.row0 + t) * A.a + it.kvh * r + tj[cb]) * D + 4 * grp;
-#pragma unroll
-                    for (int db = 0; db < 8; ++db) {
-                        u32x2 v = {pack2bf(o[cb][db][0] * inv, o[cb][db][1] * inv),
-                                   pack2bf(o[cb][db][2] * inv, o[cb][db][3] * inv)};
-                        if (lim[cb] < 0) v = u32x2{0, 0};      // sees nothing
-                        *(u32x2*)(op + 16 * db) = v;
-                    }
-                } else if constexpr (LIST) {
-                    float* pr = A.part + ((size_t)(2 * w + (whole ? 1 : 0)) * A.cols + 16 * cb + col) * PSTRIDE;
-#pragma unroll
-                    for (int db = 0; db < 8; ++db) *(f32x4*)(pr + 16 * db + 4 * grp) = o[cb][db];
-                    if (grp == 0) {
-                        pr[D] = m_run[cb];
-                        pr[D + 1] = l;
-                    }
+            C.finish(A, it, it.c * A.m, A.m, whole && ends, A.part + (2 * (size_t)w + (whole ? 1 : 0)) * A.cols * PSTRIDE);
+            if (!more) break;
+            whole = true;
+            ++x;
+            begin(nx);
+            --x;
+        }
+        it = nx;
+        ++x;
+        --left;
+    }
+}
+
+typedef __attribute__((address_space(1))) void gvoid_t;
+typedef __attribute__((address_space(3))) void lvoid_t;
+
+// N 16-byte LDS reads at addr (or a0, a1 in turn) + OFF, STEP apart, and their wait: written by hand, since
+// the compiler would first wait for the loads that go into the other stage.
+template <int OFF>
+__device__ __forceinline__ void lds_pair(uint32_t a0, uint32_t a1, u32x4 (&f)[2]) {
+    asm volatile("ds_read_b128 %0, %2 offset:%4\n\tds_read_b128 %1, %3 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1])
+                 : "v"(a0), "v"(a1), "i"(OFF)
+                 : "memory");
+}
+template <int OFF, int STEP>
+__device__ __forceinline__ void lds_run(uint32_t a, u32x4 (&f)[4]) {
+    asm volatile("ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%6\n\tds_read_b128 %2, %4 offset:%7\n\t"
+                 "ds_read_b128 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+                 : "v"(a), "i"(OFF), "i"(OFF + STEP), "i"(OFF + 2 * STEP), "i"(OFF + 3 * STEP)
+                 : "memory");
+}
+
+// Workgroup: an item of 4 mw rows, wave v's 32 columns are its rows v mw .. (v + 1) mw - 1.  The tiles
+// go from memory to LDS directly, two stages of 16 KB, one barrier a tile: it ends the loads of the
+// tile that comes and the reads of the one before it, whose stage is then loaded again.  Three
+// workgroups a CU run in each other's waits.
+// LIST: a share of the list; else one item, counted from a sequence's last.
+template <bool LIST>
+__global__ __launch_bounds__(256, 3) void attention_many_kernel(AttnArgs A) {
+    constexpr int NB = 2;
+    // K rows of 8 chunks of 16 bytes: chunk c of row R at place c ^ key(R), so that the 16 rows of a
+    // fragment read (R % 4 and R / 16 run) fall on all banks; V as it is in memory.
+    __shared__ u32x4 kl[2][512], vl[2][512];
+    auto key = [](int R) { return ((R >> 1) & 1) | (((R >> 4) & 3) << 1); };
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, grp = lane >> 4;
+    Item it;
+    uint32_t w = 0, left;
+    if constexpr (LIST) {
+        Split sp;
+        if (!take_share<false>(A, &sp, &w, &left, &it)) {
+            if (tid == 0) A.cut_many[blockIdx.x].np = 0;
+            return;
+        }
+        // The item that the share begins and does not end: that of its last tile.
+        if (tid < 64) {
+            CutItem cut{};
+            if (w + 1 < sp.W) {
+                const uint32_t xe = sp.start(w + 1) - 1;
+                Lanes<false> L;
+                list_tiles(A, L);
+                const Item e = find_tile(A, L, xe);
+                if (e.t + 1 < e.n && xe - e.t >= sp.start(w)) {
+                    cut.np = sp.wave_of(xe - e.t + e.n - 1) - w + 1;
+                    cut.row = e.s.row0 + e.c * A.m;
+                    cut.n = e.s.n - e.c * A.m;
+                    cut.act = e.s.act - e.c * A.m;
+                    cut.head = e.kvh * (A.a / A.g);
                 }
             }
-            if (LIST && more) {
-                whole = true;
-                begin(nx);
-            }
+            if (tid == 0) A.cut_many[w] = cut;
         }
-        if (!more) break;
+    } else {
+        // The last block of every sequence first, as the longest, and so on; K/V heads change fastest: with
+        // 8 of them each XCD reads one of them only.
+        const int x = blockIdx.x / A.g;
+        it.kvh = blockIdx.x % A.g;
+        it.b = x % A.r.B;
+        it.c = gridDim.x / (A.r.B * A.g) - 1 - x / A.r.B;
+        it.s = seq_rows(A.r, it.b);
+        if (it.c >= blocks_of(it.s, A.m)) return;
+        it.t = 0;
+        it.n = tiles_of(it.s, A.m, it.c);
+        left = it.n;
+    }
+    const int r = A.a / A.g, wcols = A.mw * r;
+    Columns<NB> C;
+    Table tab;
+    // The lane's 16 bytes of this wave's two KB of K and of V.
+    int ksrc[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int p = 128 * wave + 64 * i + lane, R = p >> 3;
+        ksrc[i] = R * D + 16 * ((p & 7) ^ key(R));
+    }
+    float kn, vn;          // scales of the tile that comes
+    auto issue = [&](const Item& i, int stg) {
+        const size_t at = tab.page(A, i);
+        const uint8_t *kp = A.kc + at * kPageBytes8, *vp = A.vc + at * kPageBytes8 + 16 * (128 * wave + lane);
+        kn = A.sc[at * 2 * kPageBlks + grp];
+        vn = A.sc[at * 2 * kPageBlks + kPageBlks + grp];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            __builtin_amdgcn_global_load_lds((gvoid_t*)(kp + ksrc[i]), (lvoid_t*)&kl[stg][128 * wave + 64 * i], 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((gvoid_t*)(vp + 1024 * i), (lvoid_t*)&vl[stg][128 * wave + 64 * i], 16, 0, 0);
+        }
+    };
+    bool whole = it.t == 0;
+    int t0 = it.c * A.m + wave * A.mw;        // the wave's first row
+    issue(it, 0);
+    C.load_q(A, it, t0, A.mw);
+    C.begin(it.s, t0, A.mw, r);
+    // LDS addresses of the lane's K chunks (dimension halves 0, 1; key(R) is the same for all four rows R) and
+    // V runs.
+    const int krow = 16 * (col >> 2) + (col & 3);
+    const uint32_t ka0 = (uint32_t)(uintptr_t)&kl[0][krow * 8 + (grp ^ key(krow))],
+                   ka1 = (uint32_t)(uintptr_t)&kl[0][krow * 8 + ((4 + grp) ^ key(krow))],
+                   va = (uint32_t)(uintptr_t)&vl[0][128 * grp + col];
+    for (int stg = 0;; stg ^= 1) {
+        const bool ends = it.t + 1 == it.n;
+        bool more = left > 1;
+        Item nx = it;
+        if (more) {
+            if (LIST && ends)
+                more = next_item(A, nx);
+            else
+                ++nx.t;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // this wave's part of the tile is in LDS
+        __syncthreads();
+        const float ks = kn * A.scale_log2, vs = vn;
+        if (more) issue(nx, stg ^ 1);
+        const int p0 = TILE * it.t + 16 * grp;
+        if (TILE * it.t <= C.last) {          // the wave's rows see some of it
+            const bool edge = TILE * it.t + TILE - 1 > C.all;
+            f32x4 sc[NB][4];
+            auto block = [&](auto tb_t) __attribute__((always_inline)) {
+                constexpr int tb = decltype(tb_t)::value;
+                u32x4 kv[2];
+                lds_pair<tb * 4 * D>(ka0 + 8192 * stg, ka1 + 8192 * stg, kv);
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const bf16x8 f = widen(kv[s >> 1][2 * (s & 1)], kv[s >> 1][2 * (s & 1) + 1]);
+#pragma unroll
+                    for (int cb = 0; cb < NB; ++cb) sc[cb][tb] = mfma16x16x32(f, C.q[cb][s], s ? sc[cb][tb] : f32x4{});
+                }
+            };
+            block(std::integral_constant<int, 0>{});
+            block(std::integral_constant<int, 1>{});
+            block(std::integral_constant<int, 2>{});
+            block(std::integral_constant<int, 3>{});
+            bf16x8 pb[NB][2];
+            C.softmax(sc, edge, p0, ks, vs, pb);
+            auto vals = [&](auto d0_t) __attribute__((always_inline)) {
+                constexpr int d0 = decltype(d0_t)::value;
+                u32x4 v[4];
+                lds_run<d0 * 256, 256>(va + 8192 * stg, v);
+                if (edge) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t mask = C.v_mask(p0, j);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i][j] &= mask;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const bf16x8 f = widen(v[i][2 * h], v[i][2 * h + 1]);
+#pragma unroll
+                        for (int cb = 0; cb < NB; ++cb) C.o[cb][d0 + i] = mfma16x16x32(f, pb[cb][h], C.o[cb][d0 + i]);
+                    }
+                }
+            };
+            vals(std::integral_constant<int, 0>{});
+            vals(std::integral_constant<int, 4>{});
+        }
+        if (ends || !more) {
+            float* piece = A.part + ((2 * (size_t)w + (whole ? 1 : 0)) * A.cols + wave * wcols) * PSTRIDE;
+            C.finish(A, it, t0, A.mw, whole && ends, piece);
+            if (!more) break;
+            whole = true;
+            t0 = nx.c * A.m + wave * A.mw;
+            C.load_q(A, nx, t0, A.mw);
+            C.begin(nx.s, t0, A.mw, r);
+        }
         it = nx;
         --left;
     }
 }
 
-// Where the pieces of an item are joined: waves w0 (from the item's first tile on) .. w0 + np - 1.
-struct Pieces {
-    uint32_t w0;
-    int np;
-    __device__ __forceinline__ size_t slot(int i) const { return 2 * (size_t)(w0 + i) + (i == 0 ? 1 : 0); }
-};
+// Slot of piece i of an item that share w0 begins.
+__device__ __forceinline__ size_t slot_of(int w0, int i) { return 2 * (size_t)(w0 + i) + (i == 0 ? 1 : 0); }
 
 constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
 
 // One new row a sequence or a few (an item is a sequence and K/V head): a workgroup a column.  Wave
 // v takes pieces v, v + 4, ...: lane i holds the maximum and sum of its i-th, every lane two of the
 // 128 dimensions; the waves meet in LDS.
-__global__ __launch_bounds__(kJoinThreads) void join_few_kernel(AttnArgs A, int waves) {
+__global__ __launch_bounds__(kJoinThreads) void join_few_kernel(AttnArgs A) {
     __shared__ float num_s[kJoinWaves][D], m_s[kJoinWaves], den_s[kJoinWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int x = blockIdx.x / A.cols, c = blockIdx.x % A.cols, b = x / A.g, kvh = x % A.g, r = A.a / A.g;
-    // The sequence's place in the list.
-    Lanes L;
-    uint32_t T = 0, n = 0, x0 = 0;
-    SeqRows s{};
-    for (int b0 = 0; b0 < A.r.B; b0 += 64) {
-        L.load(A, b0, T);
-        T += L.total;
-        if (b >= b0 && b < b0 + 64) {
-            s = L.rows(b - b0);
-            n = __builtin_amdgcn_readlane(L.n, b - b0);
-            x0 = __builtin_amdgcn_readlane(L.pre, b - b0) + kvh * n;
-        }
-    }
+    const SeqRows s = seq_rows(A.r, b);
     const int t = c / r;
     if (t >= s.n) return;
-    const Split sp(T, waves);
-    Pieces pc;
-    pc.w0 = __builtin_amdgcn_readfirstlane((int)sp.wave_of(x0));
-    pc.np = __builtin_amdgcn_readfirstlane((int)sp.wave_of(x0 + n - 1)) - pc.w0 + 1;
-    if (pc.np == 1) return;                       // written by its wave
+    const int w0 = A.cut[x].x, np = A.cut[x].y;
+    if (np == 1) return;                       // written by its wave
     const size_t step = (size_t)A.cols * PSTRIDE;
     const float* part = A.part + (size_t)c * PSTRIDE;
-    const int mine = (pc.np - wave + kJoinWaves - 1) / kJoinWaves;
+    const int mine = (np - wave + kJoinWaves - 1) / kJoinWaves;
     float M = -INFINITY, den = 0.f;
     f32x2 num = {0.f, 0.f};
     for (int s0 = 0; s0 < mine; s0 += 64) {
         const int k = min(mine - s0, 64);
-        auto piece = [&](int i) { return part + pc.slot(wave + kJoinWaves * (s0 + i)) * step; };
+        auto piece = [&](int i) { return part + slot_of(w0, wave + kJoinWaves * (s0 + i)) * step; };
         float m = -INFINITY, l = 0.f;
         if (lane < k) {
             const float* p = piece(lane);
@@ -563,72 +757,95 @@ __global__ __launch_bounds__(kJoinThreads) void join_few_kernel(AttnArgs A, int 
     A.out[((size_t)(s.row0 + t) * A.a + kvh * r + c % r) * D + tid] = t < s.act ? f2bf(ns / ds) : (uint16_t)0;
 }
 
-// Many rows: a workgroup a boundary of the list between two waves, which joins the item that the
-// boundary cuts if it is the first to cut it; a wave a column in turn.
-__global__ __launch_bounds__(kJoinThreads) void join_many_kernel(AttnArgs A, int waves) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = A.a / A.g;
-    Lanes L;
-    const Split sp(list_tiles(A, L), waves);
-    const uint32_t w = blockIdx.x + 1;
-    if (w >= sp.W) return;
-    const uint32_t x = sp.start(w);
-    const Item it = find_tile(A, L, x);
-    const uint32_t x0 = x - it.t;
-    if (it.t == 0 || sp.start(w - 1) > x0) return;
-    Pieces pc;
-    pc.w0 = w - 1;
-    pc.np = sp.wave_of(x0 + it.n - 1) - pc.w0 + 1;
+// Many rows: workgroups for each share, which join the item that it begins and does not end; a wave a pair
+// of columns, with the pieces of both requested together.
+constexpr int kJoinCols = 2 * kJoinWaves;
+__global__ __launch_bounds__(kJoinThreads) void join_many_kernel(AttnArgs A) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = A.a / A.g, w0 = blockIdx.x;
+    const CutItem it = A.cut_many[w0];
+    if (it.np == 0) return;
     const size_t step = (size_t)A.cols * PSTRIDE;
-    for (int c = wave; c < A.cols; c += kJoinWaves) {
-        const int t = it.c * A.m + c / r;
-        if (t >= it.s.n) break;
-        float M = -INFINITY, den = 0.f;
-        f32x2 num = {0.f, 0.f};
-        for (int i = 0; i < pc.np; ++i) {
-            const float* p = A.part + pc.slot(i) * step + (size_t)c * PSTRIDE;
-            const f32x2 v = *(const f32x2*)(p + 2 * lane);
-            const float m = p[D], Mn = fmaxf(M, m), f = exp2f(M - Mn), wt = exp2f(m - Mn);
-            den = den * f + wt * p[D + 1];
-            num[0] = num[0] * f + wt * v[0];
-            num[1] = num[1] * f + wt * v[1];
-            M = Mn;
-        }
-        const uint32_t o = t < it.s.act ? pack2bf(num[0] / den, num[1] / den) : 0u;
-        *(uint32_t*)(A.out + ((size_t)(it.s.row0 + t) * A.a + it.kvh * r + c % r) * D + 2 * lane) = o;
+    const int c0 = kJoinCols * blockIdx.y + 2 * wave;
+    const int cols = min(A.cols, it.n * r);
+    if (c0 >= cols) return;
+    float M[2] = {-INFINITY, -INFINITY}, den[2] = {0.f, 0.f};
+    f32x2 num[2] = {{0.f, 0.f}, {0.f, 0.f}};
+    for (int i0 = 0; i0 < it.np; i0 += 2) {
+        f32x2 v[2][2], ml[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                // A piece past the last and a column past the item's repeat the last one.
+                const float* p = A.part + slot_of(w0, min(i0 + i, it.np - 1)) * step + (size_t)min(c0 + j, cols - 1) * PSTRIDE;
+                v[i][j] = *(const f32x2*)(p + 2 * lane);
+                ml[i][j] = *(const f32x2*)(p + D);
+            }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (i0 + i >= it.np) continue;
+                const float Mn = fmaxf(M[j], ml[i][j][0]), f = exp2f(M[j] - Mn), wt = exp2f(ml[i][j][0] - Mn);
+                den[j] = den[j] * f + wt * ml[i][j][1];
+                num[j][0] = num[j][0] * f + wt * v[i][j][0];
+                num[j][1] = num[j][1] * f + wt * v[i][j][1];
+                M[j] = Mn;
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int c = c0 + j, t = c / r;
+        if (c >= cols) break;
+        const uint32_t o = t < it.act ? pack2bf(num[j][0] / den[j], num[j][1] / den[j]) : 0u;
+        *(uint32_t*)(A.out + ((size_t)(it.row + t) * A.a + it.head + c % r) * D + 2 * lane) = o;
     }
 }
 
-// Two waves a SIMD.
-int list_waves(int simds) { return std::min(2 * simds, kMaxDecodeSplits); }
+// Shares of the list: three waves a SIMD, or three workgroups of four a CU.
+int few_shares(int simds) { return std::min(3 * simds, kMaxDecodeSplits); }
+int many_shares(int simds) { return std::max(1, 3 * simds / 4); }
 
 }  // namespace
 
-size_t attention_fp8_floats(int simds) { return (size_t)2 * list_waves(simds) * 32 * PSTRIDE; }
+// Pieces, then what the join reads.
+size_t attention_fp8_bytes(int B, int g, int simds) {
+    const size_t pieces = (size_t)2 * PSTRIDE * sizeof(float) * std::max(16 * few_shares(simds), 128 * many_shares(simds));
+    return pieces + std::max((size_t)B * g * sizeof(int2), (size_t)many_shares(simds) * sizeof(CutItem));
+}
 
 hipError_t attention_fp8(const NewRows& r, int a, int g, const uint16_t* q, const uint8_t* kc, const uint8_t* vc,
-                         const float* sc, uint16_t* out, float* part, int simds, hipStream_t st) {
+                         const float* sc, uint16_t* out, void* ws, int simds, hipStream_t st) {
     if (r.B < 1 || r.rows < 1 || r.n_pages < 1 || r.stride < 1 || a % g || a / g > 16) return hipErrorInvalidValue;
-    const int q_heads = a / g, waves = list_waves(simds);
-    const bool few = r.max_new * q_heads <= 16;
-    // Rows an item: what 16 or 32 columns hold, no more than a sequence has.
-    const int m = std::min((few ? 16 : 32) / q_heads, r.max_new);
-    const AttnArgs A{r, q, kc, vc, sc, out, part, a, g, m, m * q_heads, (float)(1.4426950408889634 / sqrt((double)D))};
-    if (few) {
-        hipLaunchKernelGGL((attention_kernel<1, true>), dim3(waves), dim3(64), 0, st, A);
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(join_few_kernel, dim3(r.B * g * A.cols), dim3(kJoinThreads), 0, st, A, waves);
+    const int heads = a / g;
+    AttnArgs A{r, q, kc, vc, sc, out, (float*)ws, a, g, 0, 0, 0, nullptr, nullptr, (float)(1.4426950408889634 / sqrt((double)D))};
+    hipError_t e;
+    if (r.max_new * heads <= 16) {
+        A.m = r.max_new;
+        A.cols = A.m * heads;
+        const int shares = few_shares(simds);
+        A.cut = (int2*)(A.part + (size_t)2 * shares * A.cols * PSTRIDE);
+        hipLaunchKernelGGL(attention_few_kernel, dim3(shares), dim3(64), 0, st, A);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        hipLaunchKernelGGL(join_few_kernel, dim3(r.B * g * A.cols), dim3(kJoinThreads), 0, st, A);
         return hipGetLastError();
     }
-    const int items = g * (r.rows / m + r.B);
-    if (items >= 2 * waves) {
-        hipLaunchKernelGGL((attention_kernel<2, false>), dim3(items), dim3(64), 0, st, A);
+    // Rows of a wave: what 32 columns hold, and no more than a quarter of the longest sequence's.
+    A.mw = std::min(32 / heads, (r.max_new + 3) / 4);
+    A.m = 4 * A.mw;
+    A.cols = A.m * heads;
+    // One by one: at least two a workgroup that the device holds, and few blocks that are none (the grid
+    // has as many for every sequence as the longest may have).
+    const int shares = many_shares(simds);
+    const int64_t items = (int64_t)g * (r.rows / A.m + r.B), grid = (int64_t)g * r.B * ((r.max_new + A.m - 1) / A.m);
+    if (items >= 2 * shares && grid <= 4 * items) {
+        hipLaunchKernelGGL(attention_many_kernel<false>, dim3((unsigned)grid), dim3(256), 0, st, A);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((attention_kernel<2, true>), dim3(waves), dim3(64), 0, st, A);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(join_many_kernel, dim3(waves - 1), dim3(kJoinThreads), 0, st, A, waves);
+    A.cut_many = (CutItem*)(A.part + (size_t)2 * shares * A.cols * PSTRIDE);
+    hipLaunchKernelGGL(attention_many_kernel<true>, dim3(shares), dim3(256), 0, st, A);
+    if ((e = hipGetLastError()) != hipSuccess || shares == 1) return e;
+    hipLaunchKernelGGL(join_many_kernel, dim3(shares - 1, (A.cols + kJoinCols - 1) / kJoinCols), dim3(kJoinThreads), 0, st, A);
     return hipGetLastError();
 }
 

@@ -208,11 +208,11 @@ hipError_t append_fp8_planes(const NewRows& r, int a, int g, const float* part, 
 // Zeros in the rows of x [rows][n] (n % 8 == 0) that belong to no sequence.
 hipError_t clear_unowned(const NewRows& r, int n, uint16_t* x, hipStream_t st);
 
-// Attention of the rows of q [rows][a * 128] over the pools; part: attention_fp8_floats of
-// scratch.  waves: SIMDs of the device.
-size_t attention_fp8_floats(int waves);
+// Attention of the rows of q [rows][a * 128] over the pools; ws: attention_fp8_bytes of scratch
+// (16-byte aligned).  simds: of the device.
+size_t attention_fp8_bytes(int B, int g, int simds);
 hipError_t attention_fp8(const NewRows& r, int a, int g, const uint16_t* q, const uint8_t* kc, const uint8_t* vc,
-                         const float* sc, uint16_t* out, float* part, int waves, hipStream_t st);
+                         const float* sc, uint16_t* out, void* ws, int simds, hipStream_t st);
 
 // ---- 4-bit weights --------------------------------------------------------------
 

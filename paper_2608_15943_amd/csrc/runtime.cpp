@@ -146,7 +146,7 @@ Workspace layout(const kvp_ctx& c, int phase, int B, int S) {
         const size_t few = std::min<size_t>(rows, kDecodeMaxRows);
         const size_t planes = few * nproj * sizeof(float) * kvp::decode_gemm_splits(c.d.h);
         w.proj = take(rows > few ? std::max(planes, rows * nproj * 2) : planes);
-        w.part = take(kvp::attention_fp8_floats(c.decode_waves) * sizeof(float));
+        w.part = take(kvp::attention_fp8_bytes(B, c.d.g, c.decode_waves));
     } else {
         // bf16: one plane per 512-wide K slice of the projection GEMM (K = h for both GEMMs).
         const size_t planes = c.bf16() ? (size_t)kvp::decode_gemm_splits(c.d.h) : 1;
@@ -1035,7 +1035,7 @@ kvp::NewRows new_rows(const kvp_ctx* ctx, int p, const kvp_rows* r) {
     return {r->cu, r->len, r->pages, r->pages_stride, ctx->layers[p].n_pages8, r->B, r->rows, r->max_new, r->max_pos};
 }
 
-int run_attention_fp8(kvp_ctx* c, int l, const void* q, const kvp_rows* r, void* out, float* part, hipStream_t st) {
+int run_attention_fp8(kvp_ctx* c, int l, const void* q, const kvp_rows* r, void* out, void* part, hipStream_t st) {
     const int p = c->tau[l];
     const Layer& P = c->layers[p];
     return timed(c, KVP_K_DEC_ATTN, st, [&] {
@@ -1092,7 +1092,7 @@ int run_step_layer(kvp_ctx* c, int l, const LayerIO& io, const kvp_rows* r, char
                               "rotation + cache append");
          })))
         return rc;
-    if ((rc = run_attention_fp8(c, l, q, r, o, (float*)(ws + w.part), st))) return rc;
+    if ((rc = run_attention_fp8(c, l, q, r, o, ws + w.part, st))) return rc;
     if (w4) return oproj_w4(c, l, io, o, rows, st);
     return timed(c, few ? KVP_K_DEC_OPROJ : KVP_K_OPROJ_GEMM, st, [&] {
         kvp::WRows wo{};
@@ -1155,7 +1155,7 @@ extern "C" int kvp_attention_fp8(kvp_ctx* ctx, int l, const void* q, const kvp_r
         return fail(KVP_E_INVALID_ARG, "kvp_attention_fp8: q, out must be 16-byte aligned");
     Workspace w;
     if ((rc = check_step_ws(ctx, r, ws, ws_bytes, &w, "kvp_attention_fp8"))) return rc;
-    return run_attention_fp8(ctx, l, q, r, out, (float*)((char*)ws + w.part), (hipStream_t)stream);
+    return run_attention_fp8(ctx, l, q, r, out, (char*)ws + w.part, (hipStream_t)stream);
 }
 
 extern "C" int kvp_step_fp8(kvp_ctx* ctx, const void* x, const kvp_rows* r, void* y, void* ws, size_t ws_bytes,
