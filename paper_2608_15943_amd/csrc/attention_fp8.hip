@@ -257,11 +257,18 @@ struct Table {
     }
 };
 
+// The thread's index, unknown to the compiler: what is computed from it where an item begins or ends is not
+// held in registers (or spilled) through the loop over its tiles.
+__device__ __forceinline__ int thread_now() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+
 // 16 NB columns of an item, from row t0 of the sequence on: a lane's column of block cb is head tj of
 // row t0 + tc.
 template <int NB>
 struct Columns {
-    bf16x8 q[NB][4];
     int lim[NB];             // the last position that the column sees, -1 where there is none
     float m[NB], l[NB];      // running maximum (log2 domain) and sum of the weights
     f32x4 o[NB][8];          // O^T: dimensions 16 db + 4 grp + 0..3 of the column
@@ -270,30 +277,28 @@ struct Columns {
     // Column of block cb: its row, from the item's or wave's first on (past every row where the column
     // is none of the `rows` rows'), and its head.
     static __device__ __forceinline__ int row_of(int cb, int rows, int r) {
-        const int c = 16 * cb + (threadIdx.x & 15);
+        const int c = 16 * cb + (thread_now() & 15);
         return c < rows * r ? c / r : 1 << 30;
     }
-    static __device__ __forceinline__ int head_of(int cb, int r) { return (16 * cb + (threadIdx.x & 15)) % r; }
+    static __device__ __forceinline__ int head_of(int cb, int r) { return (16 * cb + (thread_now() & 15)) % r; }
     static __device__ __forceinline__ int limit(const SeqRows& s, int t0, int rows, int r, int cb) {
         const int t = row_of(cb, rows, r);
         return t < s.act - t0 ? s.len + t0 + t : -1;
     }
-    // Contraction order of S: step ks of lane group grp holds dimensions 64 (ks / 2) + 16 grp +
-    // 8 (ks % 2) .. + 7, the order of the K codes' 16-byte runs.
-    __device__ __forceinline__ void load_q(const AttnArgs& A, const Item& it, int t0, int rows) {
-        const int grp = (threadIdx.x >> 4) & 3, r = A.a / A.g;
+    // Dimensions 16 grp .. + 15 (j = 0) and 64 + 16 grp .. + 15 (j = 1) of the query of column cb, in two words
+    // of 8 each: the order of the K codes' 16-byte runs.
+    static __device__ __forceinline__ void load_q(const AttnArgs& A, const Item& it, int t0, int rows, int cb, u32x4 (&v)[2][2]) {
+        const int grp = (thread_now() >> 4) & 3, r = A.a / A.g;
+        const bool real = limit(it.s, t0, rows, r, cb) >= 0;
+        const size_t row = it.s.row0 + (real ? t0 + row_of(cb, rows, r) : 0);
+        const uint16_t* p = A.q + (row * A.a + it.kvh * r + head_of(cb, r)) * D + 16 * grp;
 #pragma unroll
-        for (int cb = 0; cb < NB; ++cb) {
-            const bool real = limit(it.s, t0, rows, r, cb) >= 0;
-            const size_t row = it.s.row0 + (real ? t0 + row_of(cb, rows, r) : 0);
-            const uint16_t* p = A.q + (row * A.a + it.kvh * r + head_of(cb, r)) * D + 16 * grp;
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                u32x4 v = u32x4{0, 0, 0, 0};
-                if (real) v = *(const u32x4*)(p + 64 * (ks >> 1) + 8 * (ks & 1));
-                q[cb][ks] = as_bf16x8(v);
+            for (int h = 0; h < 2; ++h) {
+                v[j][h] = u32x4{0, 0, 0, 0};
+                if (real) v[j][h] = *(const u32x4*)(p + 64 * j + 8 * h);
             }
-        }
     }
     // Begins rows t0 .. t0 + rows - 1 of a sequence (their queries are loaded).
     __device__ __forceinline__ void begin(const SeqRows& s, int t0, int rows, int r) {
@@ -310,11 +315,12 @@ struct Columns {
         last = n > 0 ? s.len + t0 + n - 1 : -1;
     }
     // Weights of a tile from its scores: lane (column, grp) holds positions p0 + 4 tb + i, whose scales
-    // are ks (times the score factor) and vs; out: the rows of P, pb.  edge: some column does not see all
+    // are ks (times the score factor and, qs[cb], the column's) and vs; out: the rows of P, pb.  edge: some column does not see all
     // of the tile (branches around the masks: two copies of this code would not fit the registers).
-    __device__ __forceinline__ void softmax(f32x4 (&sc)[NB][4], bool edge, int p0, float ks, float vs, bf16x8 (&pb)[NB][2]) {
+    __device__ __forceinline__ void softmax(f32x4 (&sc)[NB][4], bool edge, int p0, float ks_, const float (&qs)[NB], float vs,
+                                            bf16x8 (&pb)[NB][2]) {
         // The scales of blocks that no column sees may hold anything.
-        if (edge && p0 > last) ks = vs = 1.f;
+        if (edge && p0 > last) ks_ = vs = 1.f;
         // P 2^e for a V scale of 2^e.
         const int e = (int)(__float_as_uint(vs) >> 23) - 127;
         const float vexp = vs == vs ? (float)e : vs;
@@ -328,6 +334,7 @@ struct Columns {
                     for (int i = 0; i < 4; ++i)
                         if (p0 + 4 * tb + i > lim[cb]) sc[cb][tb][i] = -INFINITY;
             }
+            const float ks = ks_ * qs[cb];
             float mx = -INFINITY;
 #pragma unroll
             for (int tb = 0; tb < 4; ++tb)
@@ -374,7 +381,7 @@ struct Columns {
     }
     // The end of an item (or of a share inside it): out, or a piece.
     __device__ __forceinline__ void finish(const AttnArgs& A, const Item& it, int t0, int rows, bool whole, float* piece) {
-        const int grp = (threadIdx.x >> 4) & 3, col = threadIdx.x & 15, r = A.a / A.g;
+        const int grp = (thread_now() >> 4) & 3, col = thread_now() & 15, r = A.a / A.g;
 #pragma unroll
         for (int cb = 0; cb < NB; ++cb) {
             const float lsum = pair32_sum(pair16_sum(l[cb]));
@@ -410,32 +417,34 @@ __global__ __launch_bounds__(64, 3) void attention_few_kernel(AttnArgs A) {
     uint32_t w, left;
     if (!take_share<true>(A, &sp, &w, &left, &it)) return;
     Columns<1> C;
+    u32x4 q[2][2];
     const int r = A.a / A.g;
     Table tab;
     u32x4 k[4][2], v[8];         // [score block][64-dimension half], [16-dimension block]
     float ks, vs;                // scales of the lane group's 16 positions
-    const int koff = (16 * (col >> 2) + (col & 3)) * D + 16 * grp, voff = grp * kBlkBytes + col * kBlk;
+    const uint32_t koff = (16 * (col >> 2) + (col & 3)) * D + 16 * grp, voff = grp * kBlkBytes + col * kBlk;
     auto load_k = [&](size_t at) {
-        const uint8_t* p = A.kc + at * kPageBytes8 + koff;
+        const uint8_t* p = A.kc + at * kPageBytes8;
+        ks = (A.sc + at * 2 * kPageBlks)[(uint32_t)grp];
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) k[tb][j] = *(const u32x4*)(p + 4 * tb * D + 64 * j);
-        ks = A.sc[at * 2 * kPageBlks + grp];
+            for (int j = 0; j < 2; ++j) k[tb][j] = *(const u32x4*)(p + 4 * tb * D + 64 * j + koff);
     };
     auto load_v = [&](size_t at) {
-        const uint8_t* p = A.vc + at * kPageBytes8 + voff;
-        vs = A.sc[at * 2 * kPageBlks + kPageBlks + grp];
+        const uint8_t* p = A.vc + at * kPageBytes8;
+        vs = (A.sc + at * 2 * kPageBlks + kPageBlks)[(uint32_t)grp];
 #pragma unroll
-        for (int db = 0; db < 8; ++db) v[db] = *(const u32x4*)(p + 16 * db * kBlk);
+        for (int db = 0; db < 8; ++db) v[db] = *(const u32x4*)(p + 16 * db * kBlk + voff);
     };
+    const float one[1] = {1.f};
     bool whole = it.t == 0;        // the share has the item from its first tile on
     uint32_t x = sp.start(w);      // the list's tile
     auto begin = [&](const Item& i) {
         C.begin(i.s, i.c * A.m, A.m, r);
         if (whole && lane == 0) A.cut[i.b * A.g + i.kvh] = make_int2(w, sp.wave_of(x + i.n - 1) - w + 1);
     };
-    C.load_q(A, it, it.c * A.m, A.m);
+    C.load_q(A, it, it.c * A.m, A.m, 0, q);
     begin(it);
     {
         const size_t at = tab.page(A, it);
@@ -461,19 +470,19 @@ __global__ __launch_bounds__(64, 3) void attention_few_kernel(AttnArgs A) {
         for (int tb = 0; tb < 4; ++tb)
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                sc[0][tb] = mfma16x16x32(widen(k[tb][s >> 1][2 * (s & 1)], k[tb][s >> 1][2 * (s & 1) + 1]), C.q[0][s],
-                                         s ? sc[0][tb] : f32x4{});
+                sc[0][tb] = mfma16x16x32(widen(k[tb][s >> 1][2 * (s & 1)], k[tb][s >> 1][2 * (s & 1) + 1]),
+                                         as_bf16x8(q[s >> 1][s & 1]), s ? sc[0][tb] : f32x4{});
         const float kf = ks * A.scale_log2;
         __builtin_amdgcn_sched_barrier(0);
         // A part of a tile (and the queries) is requested again as soon as it has been multiplied: 16
         // KB a wave are always under way, without a second set of registers.
         if (more) {
             load_k(at);
-            if (ends) C.load_q(A, nx, nx.c * A.m, A.m);
+            if (ends) C.load_q(A, nx, nx.c * A.m, A.m, 0, q);
         }
         __builtin_amdgcn_sched_barrier(0);
         bf16x8 pb[1][2];
-        C.softmax(sc, edge, p0, kf, vs, pb);
+        C.softmax(sc, edge, p0, kf, one, vs, pb);
         if (edge) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -504,16 +513,71 @@ __global__ __launch_bounds__(64, 3) void attention_few_kernel(AttnArgs A) {
     }
 }
 
-typedef __attribute__((address_space(1))) void gvoid_t;
 typedef __attribute__((address_space(3))) void lvoid_t;
+
+// Buffer resource of `bytes` bytes at p, the same for the wave (word 3: a valid 32-bit data format).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, int bytes) {
+    const uint64_t a = (uint64_t)p;
+    const uint64_t u = (uint32_t)__builtin_amdgcn_readfirstlane((int)a) |
+                       (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(a >> 32)) << 32;
+    return __builtin_amdgcn_make_buffer_rsrc((void*)u, 0, bytes, 0x00020000);
+}
+
+// The queries of a wave's columns as sums of two e4m3 numbers, times a power of two s for each column: 8
+// significant bits in two times 4, exact but for what lies below 2^-19 of the column's largest value.  Scores
+// are then products of 8-bit numbers as they are in memory, K with both halves, at twice the rate of bf16
+// and without widening K.
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+template <int NB>
+struct Queries8 {
+    i32x8 hi[NB], lo[NB];
+    float s[NB];
+    __device__ __forceinline__ void load(const AttnArgs& A, const Item& it, int t0, int rows) {
+#pragma unroll
+        for (int cb = 0; cb < NB; ++cb) {
+            u32x4 v[2][2];
+            Columns<NB>::load_q(A, it, t0, rows, cb, v);
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        m = max(m, max((v[j][h][i] << 16) & 0x7FFFFFFFu, v[j][h][i] & 0x7FFF0000u));
+            m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+            m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+            s[cb] = e4m3_scale(m);
+            const float inv = 1.f / s[cb];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t a = v[j][h][2 * i], b = v[j][h][2 * i + 1];
+                        const float x0 = __uint_as_float(a << 16) * inv, x1 = __uint_as_float(a & 0xFFFF0000u) * inv,
+                                    x2 = __uint_as_float(b << 16) * inv, x3 = __uint_as_float(b & 0xFFFF0000u) * inv;
+                        const uint32_t c = e4m3_pack(x0, x1, x2, x3);
+                        const f32x2 y0 = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), y1 = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+                        hi[cb][4 * j + 2 * h + i] = (int)c;
+                        lo[cb][4 * j + 2 * h + i] = (int)e4m3_pack(x0 - y0[0], x1 - y0[1], x2 - y1[0], x3 - y1[1]);
+                    }
+        }
+    }
+};
+__device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+}
 
 // N 16-byte LDS reads at addr (or a0, a1 in turn) + OFF, STEP apart, and their wait: written by hand, since
 // the compiler would first wait for the loads that go into the other stage.
-template <int OFF>
-__device__ __forceinline__ void lds_pair(uint32_t a0, uint32_t a1, u32x4 (&f)[2]) {
-    asm volatile("ds_read_b128 %0, %2 offset:%4\n\tds_read_b128 %1, %3 offset:%4\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(f[0]), "=&v"(f[1])
-                 : "v"(a0), "v"(a1), "i"(OFF)
+template <int OFF, int STEP>
+__device__ __forceinline__ void lds_pairs(uint32_t a0, uint32_t a1, u32x4 (&f)[4]) {
+    asm volatile("ds_read_b128 %0, %4 offset:%6\n\tds_read_b128 %1, %5 offset:%6\n\tds_read_b128 %2, %4 offset:%7\n\t"
+                 "ds_read_b128 %3, %5 offset:%7\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+                 : "v"(a0), "v"(a1), "i"(OFF), "i"(OFF + STEP)
                  : "memory");
 }
 template <int OFF, int STEP>
@@ -580,37 +644,31 @@ __global__ __launch_bounds__(256, 3) void attention_many_kernel(AttnArgs A) {
     }
     const int r = A.a / A.g, wcols = A.mw * r;
     Columns<NB> C;
+    Queries8<NB> Q;
     Table tab;
-    // The lane's 16 bytes of this wave's two KB of K and of V.
-    int ksrc[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int p = 128 * wave + 64 * i + lane, R = p >> 3;
-        ksrc[i] = R * D + 16 * ((p & 7) ^ key(R));
-    }
     float kn, vn;          // scales of the tile that comes
     auto issue = [&](const Item& i, int stg) {
         const size_t at = tab.page(A, i);
-        const uint8_t *kp = A.kc + at * kPageBytes8, *vp = A.vc + at * kPageBytes8 + 16 * (128 * wave + lane);
-        kn = A.sc[at * 2 * kPageBlks + grp];
-        vn = A.sc[at * 2 * kPageBlks + kPageBlks + grp];
+        // Buffer resources of the two pages: a lane's address is one offset.
+        const __amdgpu_buffer_rsrc_t kr = buffer_of(A.kc + at * kPageBytes8, kPageBytes8),
+                                     vr = buffer_of(A.vc + at * kPageBytes8, kPageBytes8);
+        const __amdgpu_buffer_rsrc_t sr = buffer_of(A.sc + at * 2 * kPageBlks, 2 * kPageBlks * sizeof(float));
+        // The lane's 16 bytes of the first of this wave's two KB of K and V (the second's key is the same).
+        const int now = thread_now() & 63;
+        const uint32_t ksrc = (now >> 3) * D + 16 * ((now & 7) ^ ((now >> 4) & 1) ^ (2 * wave)), vsrc = 16 * now, ssrc = 4 * (now >> 4);
+        kn = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sr, ssrc, 0, 0));
+        vn = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sr, ssrc, 4 * kPageBlks, 0));
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            __builtin_amdgcn_global_load_lds((gvoid_t*)(kp + ksrc[i]), (lvoid_t*)&kl[stg][128 * wave + 64 * i], 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((gvoid_t*)(vp + 1024 * i), (lvoid_t*)&vl[stg][128 * wave + 64 * i], 16, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lvoid_t*)&kl[stg][128 * wave + 64 * i], 16, ksrc, 2048 * wave + 1024 * i, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lvoid_t*)&vl[stg][128 * wave + 64 * i], 16, vsrc, 2048 * wave + 1024 * i, 0, 0);
         }
     };
     bool whole = it.t == 0;
     int t0 = it.c * A.m + wave * A.mw;        // the wave's first row
     issue(it, 0);
-    C.load_q(A, it, t0, A.mw);
+    Q.load(A, it, t0, A.mw);
     C.begin(it.s, t0, A.mw, r);
-    // LDS addresses of the lane's K chunks (dimension halves 0, 1; key(R) is the same for all four rows R) and
-    // V runs.
-    const int krow = 16 * (col >> 2) + (col & 3);
-    const uint32_t ka0 = (uint32_t)(uintptr_t)&kl[0][krow * 8 + (grp ^ key(krow))],
-                   ka1 = (uint32_t)(uintptr_t)&kl[0][krow * 8 + ((4 + grp) ^ key(krow))],
-                   va = (uint32_t)(uintptr_t)&vl[0][128 * grp + col];
     for (int stg = 0;; stg ^= 1) {
         const bool ends = it.t + 1 == it.n;
         bool more = left > 1;
@@ -629,27 +687,34 @@ __global__ __launch_bounds__(256, 3) void attention_many_kernel(AttnArgs A) {
         if (TILE * it.t <= C.last) {          // the wave's rows see some of it
             const bool edge = TILE * it.t + TILE - 1 > C.all;
             f32x4 sc[NB][4];
-            auto block = [&](auto tb_t) __attribute__((always_inline)) {
-                constexpr int tb = decltype(tb_t)::value;
-                u32x4 kv[2];
-                lds_pair<tb * 4 * D>(ka0 + 8192 * stg, ka1 + 8192 * stg, kv);
+            // The lane's K chunks of the two dimension halves (key(R) is the same for its four rows R).
+            const int now = thread_now(), krow = 16 * ((now >> 2) & 3) + (now & 3);
+            const uint32_t ka0 = (uint32_t)(uintptr_t)&kl[stg][krow * 8 + (((now >> 4) & 3) ^ key(krow))], ka1 = ka0 ^ 64;
+            auto scores = [&](auto tb_t) __attribute__((always_inline)) {
+                constexpr int tb0 = decltype(tb_t)::value;
+                u32x4 kv[4];
+                lds_pairs<tb0 * 4 * D, 4 * D>(ka0, ka1, kv);
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const bf16x8 f = widen(kv[s >> 1][2 * (s & 1)], kv[s >> 1][2 * (s & 1) + 1]);
+                for (int i = 0; i < 2; ++i) {
+                    const u32x4 x = kv[2 * i], y = kv[2 * i + 1];
+                    const i32x8 f = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
 #pragma unroll
-                    for (int cb = 0; cb < NB; ++cb) sc[cb][tb] = mfma16x16x32(f, C.q[cb][s], s ? sc[cb][tb] : f32x4{});
+                    for (int cb = 0; cb < NB; ++cb) sc[cb][tb0 + i] = mfma_e4m3(f, Q.hi[cb], f32x4{});
+#pragma unroll
+                    for (int cb = 0; cb < NB; ++cb) sc[cb][tb0 + i] = mfma_e4m3(f, Q.lo[cb], sc[cb][tb0 + i]);
                 }
             };
-            block(std::integral_constant<int, 0>{});
-            block(std::integral_constant<int, 1>{});
-            block(std::integral_constant<int, 2>{});
-            block(std::integral_constant<int, 3>{});
+            __builtin_amdgcn_s_setprio(1);
+            scores(std::integral_constant<int, 0>{});
+            scores(std::integral_constant<int, 2>{});
+            __builtin_amdgcn_s_setprio(0);
             bf16x8 pb[NB][2];
-            C.softmax(sc, edge, p0, ks, vs, pb);
+            C.softmax(sc, edge, p0, ks, Q.s, vs, pb);
+            const uint32_t va = (uint32_t)(uintptr_t)&vl[stg][128 * ((now >> 4) & 3) + (now & 15)];
             auto vals = [&](auto d0_t) __attribute__((always_inline)) {
                 constexpr int d0 = decltype(d0_t)::value;
                 u32x4 v[4];
-                lds_run<d0 * 256, 256>(va + 8192 * stg, v);
+                lds_run<d0 * 256, 256>(va, v);
                 if (edge) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -668,8 +733,10 @@ __global__ __launch_bounds__(256, 3) void attention_many_kernel(AttnArgs A) {
                     }
                 }
             };
+            __builtin_amdgcn_s_setprio(1);
             vals(std::integral_constant<int, 0>{});
             vals(std::integral_constant<int, 4>{});
+            __builtin_amdgcn_s_setprio(0);
         }
         if (ends || !more) {
             float* piece = A.part + ((2 * (size_t)w + (whole ? 1 : 0)) * A.cols + wave * wcols) * PSTRIDE;
@@ -677,7 +744,7 @@ __global__ __launch_bounds__(256, 3) void attention_many_kernel(AttnArgs A) {
             if (!more) break;
             whole = true;
             t0 = nx.c * A.m + wave * A.mw;
-            C.load_q(A, nx, t0, A.mw);
+            Q.load(A, nx, t0, A.mw);
             C.begin(nx.s, t0, A.mw, r);
         }
         it = nx;
