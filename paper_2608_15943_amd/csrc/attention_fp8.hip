@@ -410,7 +410,7 @@ struct Columns {
     }
 };
 
-__global__ __launch_bounds__(64, 3) void attention_few_kernel(AttnArgs A) {
+__global__ __launch_bounds__(64, 2) void attention_few_kernel(AttnArgs A) {
     const int lane = threadIdx.x, col = lane & 15, grp = lane >> 4;
     Item it;
     Split sp;
@@ -869,8 +869,11 @@ __global__ __launch_bounds__(kJoinThreads) void join_many_kernel(AttnArgs A) {
     }
 }
 
-// Shares of the list: three waves a SIMD, or three workgroups of four a CU.
-int few_shares(int simds) { return std::min(3 * simds, kMaxDecodeSplits); }
+// Shares of the list.  Few: one wave a SIMD (of 1, 1.5, 2 and 3 a SIMD, us: 64 x 32768 positions 738, 743,
+// 746, 761; 8 x 64K-128K 287, 290, 292, 299; 16 x 4 rows over 1500-8000 positions 44, 46, 47, 52; 3/4 of a wave
+// 739, 289, 45; half a wave 930, 359, 50; requesting two tiles ahead changes none of them).  Many: three
+// workgroups a CU (two, without a limit on the registers: prompts of 4 x 4096 rows 6 % slower).
+int few_shares(int simds) { return std::min(simds, kMaxDecodeSplits); }
 int many_shares(int simds) { return std::max(1, 3 * simds / 4); }
 
 }  // namespace
