@@ -18,79 +18,145 @@
 namespace kvp {
 namespace {
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
-
-// Codes of one word as bf16 numbers 1 + c / 16, in the order of their inputs.
-__device__ __forceinline__ bf16x8 widen4(uint32_t w) {
-    constexpr uint32_t M = 0x00780078u, One = 0x3F803F80u;
+// Codes of one word as bf16 numbers 1 + c / 16, in the order of their inputs.  mask and one (0x00780078,
+// 0x3F803F80) come in registers: with literals the and-or is two instructions.
+__device__ __forceinline__ bf16x8 widen4(uint32_t w, uint32_t mask, uint32_t one) {
     u32x4 r;
-    r[0] = ((w << 3) & M) | One;
-    r[1] = ((w >> 1) & M) | One;
-    r[2] = ((w >> 5) & M) | One;
-    r[3] = ((w >> 9) & M) | One;
+    r[0] = ((w << 3) & mask) | one;
+    r[1] = ((w >> 1) & mask) | one;
+    r[2] = ((w >> 5) & mask) | one;
+    r[3] = ((w >> 9) & mask) | one;
     return as_bf16x8(r);
 }
 
 __device__ __forceinline__ float bf(uint32_t u) { return __uint_as_float(u << 16); }
 
-// Workgroup: 16 outputs, its waves every kWaves-th 128 inputs; GS groups of scales in 128 inputs.
-template <int NMB, int GS>
-__global__ __launch_bounds__(kThreads) void linear_kernel(const uint16_t* __restrict__ X, W4Rows W, int M, int N, int K,
-                                                          LinearOut out) {
-    __shared__ f32x4 red[kWaves][NMB][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
-    const int m0 = blockIdx.y * 16 * NMB;
-    int nb = blockIdx.x, t = 0;
-    while (t < 2 && nb >= (W.rows[t] + 15) / 16) nb -= (W.rows[t++] + 15) / 16;
-    const size_t nblocks = (W.rows[t] + 15) / 16, KB = K / 128;
-    const uint8_t* codes = (const uint8_t*)W.p[t];
-    const uint16_t* scales = (const uint16_t*)(codes + nblocks * 8 * K) + (size_t)nb * (KB * GS) * 16 + 4 * kg;
-    codes += (size_t)nb * KB * 1024 + 16 * lane;
+typedef __attribute__((address_space(1))) void gvoid_t;
+typedef __attribute__((address_space(3))) void lvoid_t;
 
-    f32x4 acc[NMB];
-    const uint16_t* xr[NMB];
+// Workgroup: 16 NT outputs and 16 NMB rows, of them at most ROWS of x; its waves take every NW-th 128 inputs, U of
+// them at a time, all of their loads ahead of the products.  A wave's x goes through a part of LDS of its own, in
+// whole lines of memory: fragments read from memory would touch 16 half lines each, which bounded everything from 4
+// rows on (64 rows, 6144 x 4096: 19 us).  GS: groups of scales in 128 inputs.
+template <int NMB, int ROWS, int NT, int U, int NW, int GS>
+__global__ __launch_bounds__(64 * NW, NW / 4) void linear_kernel(const uint16_t* __restrict__ X, W4Rows W, int M, int N,
+                                                                 int K, LinearOut out) {
+    constexpr int XS = U * ROWS * 16, RS = NT * NMB * 64;          // 16-byte words of a wave: x, partial sums
+    __shared__ u32x4 lds[NW * (XS > RS ? XS : RS)];
+    f32x4* red = (f32x4*)lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, kg = lane >> 4;
+    const int m0 = blockIdx.y * 16 * NMB, KB = K / 128;
+    // The workgroup's blocks of 16 outputs, each in its part; one past the last repeats it.
+    const uint8_t* codes[NT];
+    const uint16_t* scales[NT];
 #pragma unroll
-    for (int mb = 0; mb < NMB; ++mb) {
-        acc[mb] = f32x4{};
-        xr[mb] = X + (size_t)min(m0 + 16 * mb + col, M - 1) * K + 8 * kg;
+    for (int i = 0; i < NT; ++i) {
+        int nb = min((int)blockIdx.x * NT + i, (N + 15) / 16 - 1), t = 0;
+        while (t < 2 && nb >= (W.rows[t] + 15) / 16) nb -= (W.rows[t++] + 15) / 16;
+        const uint8_t* p = (const uint8_t*)W.p[t];
+        codes[i] = p + (size_t)nb * KB * 1024;
+        scales[i] = (const uint16_t*)(p + (size_t)((W.rows[t] + 15) / 16) * 8 * K) + (size_t)nb * (KB * GS) * 16;
     }
+    f32x4 acc[NT][NMB];
+#pragma unroll
+    for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+        for (int i = 0; i < NT; ++i) acc[i][mb] = f32x4{};
+    // x of 128 inputs in LDS: rows of 16 chunks of 16 bytes, chunk c of row r at place c ^ (r & 15).  A load is 4
+    // rows; rows past M repeat the last one.
+    u32x4* xl = lds + wave * XS;
+    const uint16_t* xb = X + (size_t)m0 * K;
+    const int rows = min(ROWS, M - m0);
+    const int xr = ROWS == 4 ? col & 3 : col;          // the lane's row of a block
+    uint32_t mask = 0x00780078u, one = 0x3F803F80u;
+    asm("" : "+s"(mask), "+v"(one));
     const bf16x8 off = as_bf16x8(u32x4{0xBFC0BFC0u, 0xBFC0BFC0u, 0xBFC0BFC0u, 0xBFC0BFC0u});   // -1.5
-    for (int kb = wave; kb < (int)KB; kb += kWaves) {
-        const u32x4 c = *(const u32x4*)(codes + (size_t)kb * 1024);
+    for (int kb0 = wave; kb0 < KB; kb0 += U * NW) {
+        u32x4 c[U][NT];
+        u32x2 sw[U][NT][GS];
 #pragma unroll
-        for (int gs = 0; gs < GS; ++gs) {
-            const u32x2 sw = *(const u32x2*)(scales + (size_t)(kb * GS + gs) * 16);
-            const f32x4 sf = {bf(sw[0] & 0xFFFFu), bf(sw[0] >> 16), bf(sw[1] & 0xFFFFu), bf(sw[1] >> 16)};
-            f32x4 part[NMB];
+        for (int u = 0; u < U; ++u) {
+            const int kb = min(kb0 + u * NW, KB - 1);       // past the last: weighs nothing
 #pragma unroll
-            for (int mb = 0; mb < NMB; ++mb) part[mb] = f32x4{};
-#pragma unroll
-            for (int w = gs * (4 / GS); w < (gs + 1) * (4 / GS); ++w) {
-                const bf16x8 wf = widen4(c[w]);
-#pragma unroll
-                for (int mb = 0; mb < NMB; ++mb) {
-                    const bf16x8 xf = as_bf16x8(*(const u32x4*)(xr[mb] + kb * 128 + 32 * w));
-                    part[mb] = mfma16x16x32(wf, xf, part[mb]);
-                    part[mb] = mfma16x16x32(off, xf, part[mb]);
-                }
+            for (int j = 0; j < ROWS / 4; ++j) {
+                if (j && 4 * j >= rows) break;
+                const int r = 4 * j + (lane >> 4);
+                __builtin_amdgcn_global_load_lds(
+                    (gvoid_t*)(xb + (size_t)kb * 128 + (uint32_t)(min(r, rows - 1) * K + 8 * ((lane & 15) ^ (r & 15)))),
+                    (lvoid_t*)(xl + (u * ROWS + 4 * j) * 16), 16, 0, 0);
             }
 #pragma unroll
-            for (int mb = 0; mb < NMB; ++mb) acc[mb] += sf * part[mb];
+            for (int i = 0; i < NT; ++i) {
+                c[u][i] = *(const u32x4*)(codes[i] + (size_t)kb * 1024 + (uint32_t)(16 * lane));
+#pragma unroll
+                for (int g = 0; g < GS; ++g)
+                    sw[u][i][g] = *(const u32x2*)(scales[i] + (size_t)(kb * GS + g) * 16 + (uint32_t)(4 * kg));
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // x is in LDS
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t live = U == 1 || kb0 + u * NW < KB ? 0xFFFFFFFFu : 0u;
+            u32x4 x[NMB][4];
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) x[mb][w] = xl[(u * ROWS + 16 * mb + xr) * 16 + ((4 * w + kg) ^ xr)];
+#pragma unroll
+            for (int g = 0; g < GS; ++g) {
+                f32x4 none[NMB];          // -1.5 sum_k x, for all outputs
+#pragma unroll
+                for (int w = g * (4 / GS); w < (g + 1) * (4 / GS); ++w)
+#pragma unroll
+                    for (int mb = 0; mb < NMB; ++mb)
+                        none[mb] = mfma16x16x32(off, as_bf16x8(x[mb][w]), w % (4 / GS) ? none[mb] : f32x4{});
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    f32x4 part[NMB];
+#pragma unroll
+                    for (int w = g * (4 / GS); w < (g + 1) * (4 / GS); ++w) {
+                        const bf16x8 wf = widen4(c[u][i][w], mask, one);
+#pragma unroll
+                        for (int mb = 0; mb < NMB; ++mb)
+                            part[mb] = mfma16x16x32(wf, as_bf16x8(x[mb][w]), w % (4 / GS) ? part[mb] : none[mb]);
+                    }
+                    const u32x2 s = U == 1 ? sw[u][i][g] : sw[u][i][g] & live;
+                    const f32x4 sf = {bf(s[0]), __uint_as_float(s[0] & 0xFFFF0000u), bf(s[1]), __uint_as_float(s[1] & 0xFFFF0000u)};
+#pragma unroll
+                    for (int mb = 0; mb < NMB; ++mb) acc[i][mb] += sf * part[mb];
+                }
+            }
         }
     }
+    __syncthreads();       // x has been read
 #pragma unroll
-    for (int mb = 0; mb < NMB; ++mb) red[wave][mb][lane] = acc[mb];
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb) red[wave * RS + (i * NMB + mb) * 64 + lane] = acc[i][mb];
     __syncthreads();
-    // Lane (col, kg) of block mb: row 16 mb + col, outputs 4 kg .. + 3.
-    for (int i = threadIdx.x; i < 64 * NMB; i += kThreads) {
-        const int mb = i >> 6, ln = i & 63, m = m0 + 16 * mb + (ln & 15);
-        const int n = blockIdx.x * 16 + 4 * (ln >> 4);
-        if (m >= M) continue;
-        f32x4 v = red[0][mb][ln];
+    // Lane (col, kg) of block (i, mb): row 16 mb + col, outputs 4 kg .. + 3.
+    for (int j = threadIdx.x; j < 64 * NT * NMB; j += 64 * NW) {
+        const int ib = j >> 6, ln = j & 63, m = m0 + 16 * (ib % NMB) + (ln & 15);
+        const int n = (blockIdx.x * NT + ib / NMB) * 16 + 4 * (ln >> 4);
+        if (m >= M || n >= N) continue;
+        f32x4 v = red[j];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) v += red[w][mb][ln];
+        for (int w = 1; w < NW; ++w) v += red[w * RS + j];
         v *= 16.f;
         const size_t at = (size_t)m * N + n;
+        if (N % 4 == 0) {
+            if (out.res) {
+                if (out.res_f32) {
+                    v += *(const f32x4*)((const float*)out.res + at);
+                } else {
+                    const u32x2 r = *(const u32x2*)((const uint16_t*)out.res + at);
+                    v += f32x4{bf(r[0] & 0xFFFFu), bf(r[0] >> 16), bf(r[1] & 0xFFFFu), bf(r[1] >> 16)};
+                }
+            }
+            if (out.y) *(u32x2*)(out.y + at) = u32x2{pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};
+            if (out.yf) *(f32x4*)(out.yf + at) = v;
+            continue;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (n + e >= N) break;
@@ -149,17 +215,21 @@ __global__ __launch_bounds__(64) void pack_kernel(const uint16_t* __restrict__ W
     *(u32x4*)(out + ((size_t)nb * KB + kb) * 1024 + 16 * lane) = c;
 }
 
-template <int GS>
-hipError_t launch(const uint16_t* x, const W4Rows& w, int M, int N, int K, const LinearOut& o, int blocks, hipStream_t st) {
-    const int nmb = M > 48 ? 4 : (M + 15) / 16;
-    const dim3 grid(blocks, (M + 16 * nmb - 1) / (16 * nmb)), block(kThreads);
-    switch (nmb) {
-        case 1: hipLaunchKernelGGL((linear_kernel<1, GS>), grid, block, 0, st, x, w, M, N, K, o); break;
-        case 2: hipLaunchKernelGGL((linear_kernel<2, GS>), grid, block, 0, st, x, w, M, N, K, o); break;
-        case 3: hipLaunchKernelGGL((linear_kernel<3, GS>), grid, block, 0, st, x, w, M, N, K, o); break;
-        default: hipLaunchKernelGGL((linear_kernel<4, GS>), grid, block, 0, st, x, w, M, N, K, o); break;
-    }
+template <int NMB, int ROWS, int NT, int U, int NW, int GS>
+hipError_t launch(const uint16_t* x, const W4Rows& w, int M, int N, int K, const LinearOut& o, hipStream_t st) {
+    const dim3 grid(((N + 15) / 16 + NT - 1) / NT, (M + 16 * NMB - 1) / (16 * NMB)), block(64 * NW);
+    hipLaunchKernelGGL((linear_kernel<NMB, ROWS, NT, U, NW, GS>), grid, block, 0, st, x, w, M, N, K, o);
     return hipGetLastError();
+}
+template <int GS>
+hipError_t launch(const uint16_t* x, const W4Rows& w, int M, int N, int K, const LinearOut& o, hipStream_t st) {
+    // 16 outputs a workgroup while x is short, then 32, which share what is read of x: 1 row, 4096 x 4096, 3.9
+    // us (32 outputs: 5.3; 16 waves: 4.1); 16 rows, 8192 x 8192, 10.9 us (16 outputs: 14.2), 64 rows, 6144 x
+    // 4096, 11.0 us (16 outputs: 16.8).
+    if (M <= 4) return launch<1, 4, 1, 2, 8, GS>(x, w, M, N, K, o, st);
+    if (M <= 16) return launch<1, 16, 2, 2, 8, GS>(x, w, M, N, K, o, st);
+    if (M <= 32) return launch<2, 32, 2, 1, 8, GS>(x, w, M, N, K, o, st);
+    return launch<4, 64, 2, 1, 8, GS>(x, w, M, N, K, o, st);
 }
 
 }  // namespace
@@ -186,17 +256,16 @@ hipError_t pack_w4(const uint16_t* w, int N, int K, int group, uint8_t* packed, 
 
 hipError_t linear_w4(const uint16_t* x, const W4Rows& w, int M, int K, int group, const LinearOut& o, hipStream_t st) {
     if (M < 1 || !w4_shape_ok(K, group)) return hipErrorInvalidValue;
-    int N = 0, blocks = 0;
+    int N = 0;
     for (int t = 0; t < 3; ++t) {
         // Outputs are counted in blocks of 16 across the parts: only the last may end inside one.
         if (w.rows[t] < 0 || (t < 2 && w.rows[t + 1] && w.rows[t] % 16)) return hipErrorInvalidValue;
         N += w.rows[t];
-        blocks += (w.rows[t] + 15) / 16;
     }
     if (!N) return hipErrorInvalidValue;
-    if (group == 32) return launch<4>(x, w, M, N, K, o, blocks, st);
-    if (group == 64) return launch<2>(x, w, M, N, K, o, blocks, st);
-    return launch<1>(x, w, M, N, K, o, blocks, st);
+    if (group == 32) return launch<4>(x, w, M, N, K, o, st);
+    if (group == 64) return launch<2>(x, w, M, N, K, o, st);
+    return launch<1>(x, w, M, N, K, o, st);
 }
 
 }  // namespace kvp
