@@ -1,12 +1,17 @@
 // New K and V rows into the 8-bit paged cache, rotated to their positions on the way (RoPE), and
 // the call's Q rows rotated beside them.
 //
-// A workgroup owns the rows that fall into one block of 16 positions of one sequence (a scale's
-// extent), for some of the heads: it evaluates the rotation of its at most 16 x 64 angles once,
-// in double precision, and its waves take the head vectors (Q, K, V) in turn.  A block that holds
-// earlier positions keeps its scale or takes a larger one, and then its earlier codes are
-// rescaled.  Only one workgroup ever touches a block and head, so nothing is shared between them
-// and the result does not depend on the order in which they run.
+// Many rows (append_kernel): a workgroup owns the rows that fall into one block of 16 positions of
+// one sequence (a scale's extent), for some of the heads: it evaluates the rotation of its at most
+// 16 x 64 angles once, in double precision, and its waves take the head vectors (Q, K, V) in turn.
+// One row a sequence (append_one_kernel): a wave a head vector.  A block that holds earlier
+// positions keeps its scale or takes a larger one, and then its earlier codes are rescaled.  Only
+// one wave ever touches a block and head, so nothing is shared between waves and the result does
+// not depend on the order in which they run.
+//
+// Bound by memory: prompts of 4 x 4096 rows (16 query heads, 8 K/V heads, 235 MB) 57 us, 4.1 TB/s; 2560 rows in
+// 7 chunks (64, 8; 100 MB) 27.6 us; one row of each of 64 sequences 3.8 us, the latency of three loads that
+// depend on each other (length, page, scale).
 #include "fp8_cache.h"
 
 namespace kvp {
@@ -27,6 +32,35 @@ __device__ __forceinline__ uint32_t wave_maxu(uint32_t v) {
     return step(q[0], q[1]);
 }
 
+// Cosine and sine of pos turns * 2 pi, turns = hi + lo (double each): the product's whole turns go exactly, and
+// the series of the rest, at most an eighth of a turn, is off by less than 2^-50.  (The library's sincos takes
+// any double and most of the time of a call for few rows.)
+__device__ __forceinline__ float2 rotation(int pos, double hi, double lo) {
+    const double p = pos, t = p * hi, e = fma(p, hi, -t) + p * lo;
+    const double k = rint(4.0 * t);                       // quarter turns
+    const double x = (fma(-0.25, k, t) + e) * 6.283185307179586, z = x * x;
+    // sum of (-z)^n / (2 n + 1)! and / (2 n)!
+    double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;
+    s = fma(s, z, 1.0 / 6227020800.0);
+    s = fma(s, z, -1.0 / 39916800.0);
+    s = fma(s, z, 1.0 / 362880.0);
+    s = fma(s, z, -1.0 / 5040.0);
+    s = fma(s, z, 1.0 / 120.0);
+    s = fma(s, z, -1.0 / 6.0);
+    s = x * fma(s, z, 1.0);
+    c = fma(c, z, -1.0 / 87178291200.0);
+    c = fma(c, z, 1.0 / 479001600.0);
+    c = fma(c, z, -1.0 / 3628800.0);
+    c = fma(c, z, 1.0 / 40320.0);
+    c = fma(c, z, -1.0 / 720.0);
+    c = fma(c, z, 1.0 / 24.0);
+    c = fma(c, z, -0.5);
+    c = fma(c, z, 1.0);
+    const int q = (int)(long long)k & 3;
+    const float cf = (float)(q & 1 ? s : c), sf = (float)(q & 1 ? c : s);
+    return make_float2(q == 1 || q == 2 ? -cf : cf, q >= 2 ? -sf : sf);
+}
+
 // Rotates the pairs (x1[i], x2[i]); each product and sum rounded by itself.
 __device__ __forceinline__ void rotate(float& x1, float& x2, float2 cs) {
 #pragma clang fp contract(off)
@@ -42,10 +76,8 @@ struct Bf16Src {
     template <int N>
     __device__ __forceinline__ void load(int row, int z, int col, float* x) const {
         const uint16_t* p = z == 0 ? q + (size_t)row * ldq + col : (z == 1 ? k : v) + (size_t)row * ldkv + col;
-        if constexpr (N == 2) {
-            const uint32_t w = *(const uint32_t*)p;
-            x[0] = __uint_as_float(w << 16);
-            x[1] = __uint_as_float(w & 0xFFFF0000u);
+        if constexpr (N == 1) {
+            x[0] = __uint_as_float((uint32_t)p[0] << 16);
         } else {
 #pragma unroll
             for (int c = 0; c < N / 8; ++c) {
@@ -89,10 +121,28 @@ struct Args {
     int first;         // 0: from the first Q vector, a: from the first K vector
 };
 
+// The scale of a block whose new values reach m (float bits) and whose earlier ones have scale old (kept: there
+// are any): the new scale, and what the earlier codes are multiplied by.
+struct NewScale {
+    float s, f, inv;
+    bool bad;
+    __device__ __forceinline__ NewScale(uint32_t m, bool kept, float old) {
+        s = e4m3_scale(m);
+        f = 1.f;
+        if (kept) {
+            if (!(s > old)) s = s == s ? old : s;      // the larger; NaN if either is
+            f = old / s;
+        }
+        bad = s != s;
+        inv = bad ? 0.f : 1.f / s;
+    }
+};
+
+// Many rows: workgroup = the new rows of one block of 16 positions, for some of the head vectors.
 template <class Src>
 __global__ __launch_bounds__(kThreads) void append_kernel(Src src, Args A, RopeFreqs th) {
     __shared__ float2 cs[kBlk][kHead / 2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int b, first;
     SeqRows s;
     auto blocks = [](const SeqRows& s) { return s.act > 0 ? (s.len + s.act - 1) / kBlk - s.len / kBlk + 1 : 0; };
@@ -100,14 +150,12 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Src src, Args A, RopeF
     const int blk = s.len / kBlk + (int)blockIdx.x - first, pos0 = blk * kBlk;
     const int lo = max(s.len - pos0, 0), hi = min(s.len + s.act - pos0, kBlk);   // new: lo <= place < hi
     const int row0 = s.row0 + pos0 - s.len;                                       // row of place 0 (if new)
+    const int page = page_of(A.r, b, pos0), pblk = blk % kPageBlks;
     for (int i = tid; i < (hi - lo) * (kHead / 2); i += kThreads) {
         const int p = lo + i / (kHead / 2), f = i % (kHead / 2);
-        double sd, cd;
-        sincos((double)(pos0 + p) * th.v[f], &sd, &cd);
-        cs[p][f] = make_float2((float)cd, (float)sd);
+        cs[p][f] = rotation(pos0 + p, th.hi[f], th.lo[f]);
     }
     __syncthreads();
-    const int page = page_of(A.r, b, pos0), pblk = blk % kPageBlks;
     for (int hv = A.first + blockIdx.y * kWaves + wave; hv < A.first + A.vectors; hv += gridDim.y * kWaves) {
         if (hv < A.a + A.g) {
             // Q and K: lane (place, quarter) holds dimensions 16 quarter .. + 15 and the same of
@@ -137,84 +185,147 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Src src, Args A, RopeF
                 }
                 continue;
             }
+            float* scp = A.sc + ((size_t)h * A.r.n_pages + page) * 2 * kPageBlks + pblk;
+            const float old = lo > 0 ? *scp : 0.f;
             uint32_t m = 0;
 #pragma unroll
             for (int i = 0; i < 32; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-            float* scp = A.sc + (((size_t)h * A.r.n_pages + page) * 2 + 0) * kPageBlks + pblk;
-            float sn = e4m3_scale(wave_maxu(m)), f = 1.f;
-            if (lo > 0) {
-                const float so = *scp;
-                if (!(sn > so)) sn = sn == sn ? so : sn;     // keeps the larger; NaN if either is
-                f = so / sn;
-            }
-            const bool bad = sn != sn;
-            const float inv = bad ? 0.f : 1.f / sn;
+            const NewScale n(wave_maxu(m), lo > 0, old);
             uint8_t* row = A.kc + ((size_t)h * A.r.n_pages + page) * kPageBytes8 + (pblk * kBlk + p) * kHead + 16 * qd;
-            if (fresh || (p < lo && f != 1.f)) {
+            if (fresh || (p < lo && n.f != 1.f)) {
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     u32x4 w;
                     if (fresh) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            w[e] = bad ? 0u : e4m3_pack(x[16 * c + 4 * e] * inv, x[16 * c + 4 * e + 1] * inv,
-                                                        x[16 * c + 4 * e + 2] * inv, x[16 * c + 4 * e + 3] * inv);
+                            w[e] = n.bad ? 0u : e4m3_pack(x[16 * c + 4 * e] * n.inv, x[16 * c + 4 * e + 1] * n.inv,
+                                                          x[16 * c + 4 * e + 2] * n.inv, x[16 * c + 4 * e + 3] * n.inv);
                     } else {
                         w = *(const u32x4*)(row + 64 * c);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] = bad ? 0u : e4m3_rescale(w[e], f);
+                        for (int e = 0; e < 4; ++e) w[e] = n.bad ? 0u : e4m3_rescale(w[e], n.f);
                     }
                     *(u32x4*)(row + 64 * c) = w;
                 }
             }
-            if (lane == 0) *scp = sn;
+            if (lane == 0) *scp = n.s;
         } else {
-            // V: a lane holds dimensions 2 lane and 2 lane + 1 of all 16 places, which are two
-            // 16-byte runs of the block.
-            const int h = hv - A.a - A.g;
-            float x[kBlk][2];
+            // V: lane (grp, c) holds dimensions 8 c .. 8 c + 7 of places 4 grp .. 4 grp + 3, whose codes are word
+            // grp of the dimensions' 16-byte runs; lanes of the four groups exchange words until each has two
+            // whole runs, of dimensions 8 c + grp and 8 c + 4 + grp.
+            const int h = hv - A.a - A.g, grp = lane >> 4, c = lane & 15;
+            float x[4][8];
             uint32_t m = 0;
 #pragma unroll
-            for (int p = 0; p < kBlk; ++p) {
-                x[p][0] = x[p][1] = 0.f;
-                if (p >= lo && p < hi) src.template load<2>(row0 + p, 2, h * kHead + 2 * lane, x[p]);
-                m = max(m, max(__float_as_uint(x[p][0]) & 0x7FFFFFFFu, __float_as_uint(x[p][1]) & 0x7FFFFFFFu));
-            }
-            float* scp = A.sc + (((size_t)h * A.r.n_pages + page) * 2 + 1) * kPageBlks + pblk;
-            float sn = e4m3_scale(wave_maxu(m)), f = 1.f;
-            if (lo > 0) {
-                const float so = *scp;
-                if (!(sn > so)) sn = sn == sn ? so : sn;
-                f = so / sn;
-            }
-            const bool bad = sn != sn;
-            const float inv = bad ? 0.f : 1.f / sn;
-            uint8_t* blkp = A.vc + ((size_t)h * A.r.n_pages + page) * kPageBytes8 + pblk * kBlkBytes + 2 * lane * kBlk;
+            for (int j = 0; j < 4; ++j) {
+                const int p = 4 * grp + j;
 #pragma unroll
-            for (int d = 0; d < 2; ++d) {
-                u32x4* run = (u32x4*)(blkp + d * kBlk);
-                u32x4 old = u32x4{0, 0, 0, 0}, w;
-                if (lo > 0 || hi < kBlk) old = *run;
+                for (int e = 0; e < 8; ++e) x[j][e] = 0.f;
+                if (p >= lo && p < hi) src.template load<8>(row0 + p, 2, h * kHead + 8 * c, x[j]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[j][e]) & 0x7FFFFFFFu);
+            }
+            float* scp = A.sc + ((size_t)h * A.r.n_pages + page) * 2 * kPageBlks + kPageBlks + pblk;
+            const float old = lo > 0 ? *scp : 0.f;
+            const NewScale n(wave_maxu(m), lo > 0, old);
+            uint8_t* blkp = A.vc + ((size_t)h * A.r.n_pages + page) * kPageBytes8 + pblk * kBlkBytes;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                uint32_t w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t nw = bad ? 0u : e4m3_pack(x[4 * e][d] * inv, x[4 * e + 1][d] * inv,
-                                                             x[4 * e + 2][d] * inv, x[4 * e + 3][d] * inv);
-                    uint32_t ow = old[e];
-                    if (f != 1.f) ow = bad ? 0u : e4m3_rescale(ow, f);
-                    uint32_t fresh = 0, kept = 0;       // masks of this word's bytes
+                    const int d = 4 * q + e;
+                    w[e] = n.bad ? 0u : e4m3_pack(x[0][d] * n.inv, x[1][d] * n.inv, x[2][d] * n.inv, x[3][d] * n.inv);
+                }
+                const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+                const auto b2 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+                const auto r0 = __builtin_amdgcn_permlane16_swap(a[0], b2[0], false, false);
+                const auto r1 = __builtin_amdgcn_permlane16_swap(a[1], b2[1], false, false);
+                u32x4 run = {r0[0], r0[1], r1[0], r1[1]};
+                u32x4* dst = (u32x4*)(blkp + (8 * c + 4 * q + grp) * kBlk);
+                if (lo > 0 || hi < kBlk) {
+                    const u32x4 was = *dst;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int p = 4 * e + i;
-                        if (p >= lo && p < hi) fresh |= 0xFFu << (8 * i);
-                        if (p < lo) kept |= 0xFFu << (8 * i);
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t kept = 0, fresh = 0;       // masks of this word's bytes
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int p = 4 * e + i;
+                            if (p < lo) kept |= 0xFFu << (8 * i);
+                            if (p >= lo && p < hi) fresh |= 0xFFu << (8 * i);
+                        }
+                        uint32_t o = was[e];
+                        if (n.f != 1.f) o = (n.bad ? 0u : e4m3_rescale(o, n.f) & kept) | (o & ~kept);
+                        run[e] = (run[e] & fresh) | (o & ~fresh);
                     }
-                    w[e] = (nw & fresh) | (ow & kept) | (old[e] & ~(fresh | kept));
+                }
+                *dst = run;
+            }
+            if (lane == 0) *scp = n.s;
+        }
+    }
+}
+
+// One row a sequence at most: a wave a head vector of a row, lane i dimensions i and i + 64; everything that does
+// not depend on the position is requested ahead of it.
+template <class Src>
+__global__ __launch_bounds__(kThreads) void append_one_kernel(Src src, Args A, RopeFreqs th) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int groups = (A.vectors + kWaves - 1) / kWaves;
+    const int b = blockIdx.x / groups, hv = A.first + blockIdx.x % groups * kWaves + wave;
+    if (hv >= A.first + A.vectors) return;
+    const SeqRows s = seq_rows(A.r, b);
+    if (s.act < 1) return;
+    const int z = hv < A.a ? 0 : hv < A.a + A.g ? 1 : 2, h = z == 0 ? hv : z == 1 ? hv - A.a : hv - A.a - A.g;
+    float x1, x2;
+    src.template load<1>(s.row0, z, h * kHead + lane, &x1);
+    src.template load<1>(s.row0, z, h * kHead + 64 + lane, &x2);
+    const double thi = th.hi[lane], tlo = th.lo[lane];
+    const int pos = s.len, page = page_of(A.r, b, pos), pblk = pos / kBlk % kPageBlks, p = pos % kBlk;
+    const size_t at = (size_t)h * A.r.n_pages + page;
+    float* scp = A.sc + at * 2 * kPageBlks + (z == 2 ? kPageBlks : 0) + pblk;
+    const float old = z && p ? *scp : 0.f;
+    if (z < 2) rotate(x1, x2, rotation(pos, thi, tlo));
+    if (z == 0) {
+        uint16_t* o = A.q_out + ((size_t)s.row0 * A.a + h) * kHead + lane;
+        o[0] = f2bf(x1);
+        o[64] = f2bf(x2);
+        return;
+    }
+    const NewScale n(wave_maxu(max(__float_as_uint(x1) & 0x7FFFFFFFu, __float_as_uint(x2) & 0x7FFFFFFFu)), p > 0, old);
+    const uint32_t c = n.bad ? 0u : e4m3_pack(x1 * n.inv, x2 * n.inv, 0.f, 0.f);
+    if (z == 1) {
+        uint8_t* blkp = A.kc + at * kPageBytes8 + pblk * kBlkBytes;
+        if (n.f != 1.f)        // the block's earlier rows, 16 bytes a lane
+            for (int i = lane; i < 8 * p; i += 64) {
+                u32x4 w = ((u32x4*)blkp)[i];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = n.bad ? 0u : e4m3_rescale(w[e], n.f);
+                ((u32x4*)blkp)[i] = w;
+            }
+        blkp[p * kHead + lane] = (uint8_t)c;
+        blkp[p * kHead + 64 + lane] = (uint8_t)(c >> 8);
+    } else {
+        uint8_t* blkp = A.vc + at * kPageBytes8 + pblk * kBlkBytes;
+        if (n.f != 1.f) {      // the earlier places of the lane's two runs
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                u32x4* run = (u32x4*)(blkp + (lane + 64 * d) * kBlk);
+                u32x4 w = *run;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int k = p - 4 * e;
+                    const uint32_t kept = k >= 4 ? 0xFFFFFFFFu : k <= 0 ? 0u : (1u << (8 * k)) - 1u;
+                    w[e] = (n.bad ? 0u : e4m3_rescale(w[e], n.f) & kept) | (w[e] & ~kept);
                 }
                 *run = w;
             }
-            if (lane == 0) *scp = sn;
         }
+        blkp[lane * kBlk + p] = (uint8_t)c;
+        blkp[(lane + 64) * kBlk + p] = (uint8_t)(c >> 8);
     }
+    if (lane == 0) *scp = n.s;
 }
 
 // Row x of no sequence: before the first, behind the last, or past max_new of its own.
@@ -233,9 +344,14 @@ template <class Src>
 hipError_t launch(const Src& src, const Args& A, const RopeFreqs& th, hipStream_t st) {
     const NewRows& r = A.r;
     if (r.B < 1 || r.rows < 1 || r.n_pages < 1 || r.stride < 1 || A.vectors < 1) return hipErrorInvalidValue;
-    const int per = 4 * kWaves;      // head vectors a workgroup
+    if (r.max_new == 1) {
+        const dim3 grid((A.vectors + kWaves - 1) / kWaves * r.B);
+        hipLaunchKernelGGL(append_one_kernel<Src>, grid, dim3(kThreads), 0, st, src, A, th);
+        return hipGetLastError();
+    }
+    const int per = 2 * kWaves;      // head vectors a workgroup
     // n rows lie in at most n / 16 + 2 blocks.
-    const dim3 grid(r.cu ? r.rows / kBlk + 2 * r.B : r.B, (A.vectors + per - 1) / per);
+    const dim3 grid(r.rows / kBlk + 2 * r.B, (A.vectors + per - 1) / per);
     hipLaunchKernelGGL(append_kernel<Src>, grid, dim3(kThreads), 0, st, src, A, th);
     return hipGetLastError();
 }

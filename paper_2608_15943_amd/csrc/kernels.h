@@ -193,9 +193,9 @@ struct NewRows {
     const int32_t* pt;
     int stride, n_pages, B, rows, max_new, max_pos;
 };
-// theta_i = base^(-2i / 128).
+// base^(-2i / 128) / (2 pi) = hi + lo: the turns of a position.
 struct RopeFreqs {
-    double v[64];
+    double hi[64], lo[64];
 };
 
 // Rows of q (nullable; ldq values apart), k and v (nullable together; ldkv), in bf16: q rotated to

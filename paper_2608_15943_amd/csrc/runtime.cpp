@@ -100,7 +100,7 @@ struct kvp_ctx {
     std::vector<int32_t> tau;
     std::vector<Layer> layers;
     int decode_waves = 1024;          // decode attention grid: SIMDs of the device
-    kvp::RopeFreqs freqs{};           // rope_base^(-2i / 128) (8-bit cache)
+    kvp::RopeFreqs freqs{};           // of rope_base (8-bit cache)
     bool prof = false;
     bool debug_sync = false;          // KVP_DEBUG_SYNC: wait for and check every launch
     std::vector<ProfRec> recs;        // launches timed since the last read
@@ -538,7 +538,11 @@ extern "C" int kvp_create(const kvp_model_desc* desc, const int32_t* tau, kvp_ct
     const char* dbg = std::getenv("KVP_DEBUG_SYNC");
     c->debug_sync = dbg && dbg[0] && std::strcmp(dbg, "0") != 0;
     c->layers.resize(d.L);
-    for (int i = 0; i < 64; ++i) c->freqs.v[i] = std::pow(d.rope_base, -2.0 * i / 128.0);
+    for (int i = 0; i < 64; ++i) {
+        const long double turns = powl((long double)d.rope_base, -2.0L * i / 128.0L) / 6.283185307179586476925286766559L;
+        c->freqs.hi[i] = (double)turns;
+        c->freqs.lo[i] = (double)(turns - c->freqs.hi[i]);
+    }
     // Decode attention runs one wave per SIMD of the device current now; without a
     // device (planning-only use) the MI355X's 256 CUs are assumed.
     int dev = 0, cus = 0;
