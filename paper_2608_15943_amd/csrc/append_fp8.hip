@@ -32,11 +32,26 @@ __device__ __forceinline__ uint32_t wave_maxu(uint32_t v) {
     return step(q[0], q[1]);
 }
 
+// Turns of a position at frequency i, to some 2^-100.
+struct Turns {
+    double hi, lo;
+    __device__ __forceinline__ Turns(const RopeFreqs& th, int i) : hi(th.hi[0]), lo(th.lo[0]) {
+#pragma unroll
+        for (int j = 0; j < 6; ++j) {
+            const bool on = i >> j & 1;
+            const double fh = on ? th.hi[1 + j] : 1.0, fl = on ? th.lo[1 + j] : 0.0;
+            const double p = hi * fh, e = fma(hi, fh, -p) + (hi * fl + lo * fh);
+            hi = p + e;
+            lo = e - (hi - p);
+        }
+    }
+};
+
 // Cosine and sine of pos turns * 2 pi, turns = hi + lo (double each): the product's whole turns go exactly, and
 // the series of the rest, at most an eighth of a turn, is off by less than 2^-50.  (The library's sincos takes
 // any double and most of the time of a call for few rows.)
-__device__ __forceinline__ float2 rotation(int pos, double hi, double lo) {
-    const double p = pos, t = p * hi, e = fma(p, hi, -t) + p * lo;
+__device__ __forceinline__ float2 rotation(int pos, const Turns& turns) {
+    const double p = pos, t = p * turns.hi, e = fma(p, turns.hi, -t) + p * turns.lo;
     const double k = rint(4.0 * t);                       // quarter turns
     const double x = (fma(-0.25, k, t) + e) * 6.283185307179586, z = x * x;
     // sum of (-z)^n / (2 n + 1)! and / (2 n)!
@@ -151,9 +166,10 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Src src, Args A, RopeF
     const int lo = max(s.len - pos0, 0), hi = min(s.len + s.act - pos0, kBlk);   // new: lo <= place < hi
     const int row0 = s.row0 + pos0 - s.len;                                       // row of place 0 (if new)
     const int page = page_of(A.r, b, pos0), pblk = blk % kPageBlks;
+    const Turns turns(th, tid % (kHead / 2));       // kThreads is a multiple of that
     for (int i = tid; i < (hi - lo) * (kHead / 2); i += kThreads) {
-        const int p = lo + i / (kHead / 2), f = i % (kHead / 2);
-        cs[p][f] = rotation(pos0 + p, th.hi[f], th.lo[f]);
+        const int p = lo + i / (kHead / 2);
+        cs[p][i % (kHead / 2)] = rotation(pos0 + p, turns);
     }
     __syncthreads();
     for (int hv = A.first + blockIdx.y * kWaves + wave; hv < A.first + A.vectors; hv += gridDim.y * kWaves) {
@@ -281,12 +297,12 @@ __global__ __launch_bounds__(kThreads) void append_one_kernel(Src src, Args A, R
     float x1, x2;
     src.template load<1>(s.row0, z, h * kHead + lane, &x1);
     src.template load<1>(s.row0, z, h * kHead + 64 + lane, &x2);
-    const double thi = th.hi[lane], tlo = th.lo[lane];
+    const Turns turns(th, lane);
     const int pos = s.len, page = page_of(A.r, b, pos), pblk = pos / kBlk % kPageBlks, p = pos % kBlk;
     const size_t at = (size_t)h * A.r.n_pages + page;
     float* scp = A.sc + at * 2 * kPageBlks + (z == 2 ? kPageBlks : 0) + pblk;
     const float old = z && p ? *scp : 0.f;
-    if (z < 2) rotate(x1, x2, rotation(pos, thi, tlo));
+    if (z < 2) rotate(x1, x2, rotation(pos, turns));
     if (z == 0) {
         uint16_t* o = A.q_out + ((size_t)s.row0 * A.a + h) * kHead + lane;
         o[0] = f2bf(x1);

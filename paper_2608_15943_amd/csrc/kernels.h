@@ -193,9 +193,10 @@ struct NewRows {
     const int32_t* pt;
     int stride, n_pages, B, rows, max_new, max_pos;
 };
-// base^(-2i / 128) / (2 pi) = hi + lo: the turns of a position.
+// Turns of a position, base^(-2i / 128) / (2 pi) for i = 0 .. 63, as factors: hi + lo of index 0 is 1 / (2 pi), of
+// index 1 + j base^(-2^(j + 1) / 128), which i has where its bit j is set.
 struct RopeFreqs {
-    double hi[64], lo[64];
+    double hi[7], lo[7];
 };
 
 // Rows of q (nullable; ldq values apart), k and v (nullable together; ldkv), in bf16: q rotated to

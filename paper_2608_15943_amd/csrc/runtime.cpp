@@ -538,10 +538,11 @@ extern "C" int kvp_create(const kvp_model_desc* desc, const int32_t* tau, kvp_ct
     const char* dbg = std::getenv("KVP_DEBUG_SYNC");
     c->debug_sync = dbg && dbg[0] && std::strcmp(dbg, "0") != 0;
     c->layers.resize(d.L);
-    for (int i = 0; i < 64; ++i) {
-        const long double turns = powl((long double)d.rope_base, -2.0L * i / 128.0L) / 6.283185307179586476925286766559L;
-        c->freqs.hi[i] = (double)turns;
-        c->freqs.lo[i] = (double)(turns - c->freqs.hi[i]);
+    for (int j = 0; j < 7; ++j) {
+        const long double f = j ? powl((long double)d.rope_base, -(long double)(1 << j) / 128.0L)
+                                : 1.0L / 6.283185307179586476925286766559L;
+        c->freqs.hi[j] = (double)f;
+        c->freqs.lo[j] = (double)(f - c->freqs.hi[j]);
     }
     // Decode attention runs one wave per SIMD of the device current now; without a
     // device (planning-only use) the MI355X's 256 CUs are assumed.
