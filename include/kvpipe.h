@@ -540,7 +540,7 @@ int kvp_step_fp8(kvp_ctx* ctx, const void* x, const kvp_rows* r, void* y, void* 
 /*
  * A small batch's decode takes the time of reading the weights.  Packed weights hold a code c in
  * 0..15 for every weight and a bf16 scale s for every `group` inputs of an output:
- * w[n][k] = (c[n][k] - 8) s[n][k / group].  K a multiple of 128, group 32, 64 or 128, any N (at
+ * w[n][k] = (c[n][k] - 8) s[n][k / group].  K a multiple of 128, group 32, 64 or 128, any N (both at
  * most 2^20).  Layout, one buffer: for each 16 outputs (the last block filled up with c = 8, s = 0) and
  * 128 inputs, 64 runs of 16 bytes, run 16 j + i holding output i; its 32-bit word w holds inputs
  * 32 w + 8 j + 0..7, input 2 e in bits 4 e .. 4 e + 3, input 2 e + 1 in bits 16 + 4 e .. ; then for
@@ -560,7 +560,8 @@ int kvp_pack_w4(const void* W, int N, int K, int group, void* packed, void* stre
  * kvp_linear_w4 -- y = res + x w^T: x [M][K], res [M][N] (or NULL) and y [M][N] in bf16, packed
  * weights [N][K]; fp32 sums, rounded once.  y may be res.  Made for few rows (each 64 of them
  * read the weights once); M at most 2^20.  A row of x that is not finite makes its own row of y
- * NaN and no other.  Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE, KVP_E_HIP.
+ * NaN and no other; so may one of magnitudes above 2^118, whose sums over a group can pass the
+ * range of fp32.  Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE, KVP_E_HIP.
  */
 int kvp_linear_w4(const void* x, const void* packed, const void* res, void* y, int M, int N, int K,
                   int group, void* stream);

@@ -172,7 +172,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void linear_kernel(const uint16_t*
 template <int GS>
 __global__ __launch_bounds__(64) void pack_kernel(const uint16_t* __restrict__ W, int N, int K, uint8_t* __restrict__ out) {
     const int lane = threadIdx.x, i = lane & 15, j = lane >> 4;
-    const int kb = blockIdx.x, nb = blockIdx.y, n = 16 * nb + i;
+    const int kb = blockIdx.y, nb = blockIdx.x, n = 16 * nb + i;
     const size_t KB = K / 128;
     float x[4][8];
     uint32_t m[4];
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(64) void pack_kernel(const uint16_t* __restrict__ W
         m[w] = max(m[w], (uint32_t)__shfl_xor((int)m[w], 16));
         m[w] = max(m[w], (uint32_t)__shfl_xor((int)m[w], 32));
     }
-    uint16_t* scales = (uint16_t*)(out + (size_t)gridDim.y * 8 * K) + (nb * KB + kb) * GS * 16;
+    uint16_t* scales = (uint16_t*)(out + (size_t)gridDim.x * 8 * K) + (nb * KB + kb) * GS * 16;
     u32x4 c;
 #pragma unroll
     for (int gs = 0; gs < GS; ++gs) {
@@ -239,12 +239,13 @@ size_t w4_bytes(int N, int K, int group) {
     return nb * 8 * K + nb * 32 * (K / group);
 }
 
-bool w4_shape_ok(int K, int group) { return K >= 128 && K % 128 == 0 && (group == 32 || group == 64 || group == 128); }
+bool w4_shape_ok(int K, int group) {
+    return K >= 128 && K <= kMaxW4Rows && K % 128 == 0 && (group == 32 || group == 64 || group == 128);
+}
 
 hipError_t pack_w4(const uint16_t* w, int N, int K, int group, uint8_t* packed, hipStream_t st) {
     if (N < 1 || !w4_shape_ok(K, group)) return hipErrorInvalidValue;
-    const dim3 grid(K / 128, (N + 15) / 16), block(64);
-    if (grid.y > 65535) return hipErrorInvalidValue;
+    const dim3 grid((N + 15) / 16, K / 128), block(64);
     if (group == 32)
         hipLaunchKernelGGL(pack_kernel<4>, grid, block, 0, st, w, N, K, packed);
     else if (group == 64)

@@ -54,6 +54,29 @@ def test_pack(N, K, group):
     assert np.array_equal(_packed(w, group).cpu().numpy(), lr.w4_pack(codes, s))
 
 
+@pytest.mark.parametrize("N,K", [((1 << 20), 128), ((1 << 20) - 16, 128), (1, 1 << 20)])
+def test_pack_and_linear_of_the_largest_sizes(N, K):
+    """The first and last outputs of the longest matrices; the rest repeats 16 outputs."""
+    rng = np.random.default_rng(8)
+    w = lr.bf16(_normal(rng, min(N, 16), K) * np.float32(0.05))
+    codes, s = lr.w4_codes(w, 128)
+    t = _dev(w).repeat(max(N // 16, 1), 1)
+    n = kb.kvp_w4_bytes(N, K, 128)
+    buf = torch.full((n + 64,), 0xAB, dtype=torch.uint8, device="cuda")
+    kb.kvp_pack_w4(t.data_ptr(), N, K, 128, buf.data_ptr(), _stream())
+    torch.cuda.synchronize()
+    assert (buf[-64:] == 0xAB).all()
+    one = torch.from_numpy(lr.w4_pack(codes, s)).cuda()
+    nb, cb = (N + 15) // 16, 8 * K          # blocks, bytes of one's codes
+    assert torch.equal(buf[: nb * cb].view(nb, cb), one[:cb].expand(nb, cb))
+    assert torch.equal(buf[nb * cb: n].view(nb, K // 4), one[cb:].expand(nb, K // 4))
+    x = _normal(rng, 3, K)
+    got = _linear(x, buf[:n], N, 128)
+    y = x.astype(np.float64) @ lr.w4_weights(codes, s, 128).T
+    tol = lr.linear_bound(x.astype(np.float64), y, s, 128)
+    assert (np.abs(got.reshape(3, -1, min(N, 16)) - y[:, None]) <= tol[:, None]).all()
+
+
 def test_pack_not_finite():
     w = _normal(np.random.default_rng(1), 20, 256)
     w[3, 100], w[4, 7], w[5, 255] = np.nan, np.inf, -np.inf

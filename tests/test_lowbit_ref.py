@@ -161,6 +161,9 @@ def test_w4_refusals():
     for args in ((0, 16, 128, 32, P), (P, 16, 128, 32, 0), (P, 0, 128, 32, P), (P + 2, 16, 128, 32, P), (P, 16, 128, 32, P + 2)):
         assert _code(kb.kvp_pack_w4, *args) == kb.KVP_E_INVALID_ARG, args
     assert _code(kb.kvp_pack_w4, P, (1 << 20) + 1, 128, 32, P) == kb.KVP_E_SHAPE
+    assert _code(kb.kvp_w4_bytes, 16, (1 << 20) + 128, 32) == kb.KVP_E_SHAPE
+    assert _code(kb.kvp_pack_w4, P, 16, (1 << 20) + 128, 32, P) == kb.KVP_E_SHAPE
+    assert _code(kb.kvp_linear_w4, P, P, 0, P + 16, 1, 16, (1 << 20) + 128, 32) == kb.KVP_E_SHAPE
     for x, w, res, y, M, N in ((0, P, 0, P, 1, 16), (P, 0, 0, P + 16, 1, 16), (P, P, 0, 0, 1, 16), (P, P, 0, P + 16, 0, 16),
                                (P, P, 0, P + 16, 1, 0), (P, P, 0, P, 1, 16), (P + 2, P, 0, P, 1, 16), (P, P + 2, 0, P + 16, 1, 16),
                                (P, P, P + 2, P + 16, 1, 16), (P, P, 0, P + 2, 1, 16)):
