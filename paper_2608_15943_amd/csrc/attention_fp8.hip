@@ -321,7 +321,7 @@ struct Columns {
                                             bf16x8 (&pb)[NB][2]) {
         // The scales of blocks that no column sees may hold anything.
         if (edge && p0 > last) ks_ = vs = 1.f;
-        // P 2^e for a V scale of 2^e.
+        // P 2^e for a V scale of 2^e >= 2^-100: weights down to 2^-26 of the largest stay normal numbers.
         const int e = (int)(__float_as_uint(vs) >> 23) - 127;
         const float vexp = vs == vs ? (float)e : vs;
         const float vinv = vs == vs ? __uint_as_float((uint32_t)(127 - e) << 23) : 1.f;
@@ -410,12 +410,23 @@ struct Columns {
     }
 };
 
+// LIST: a share of the list; else one item.
+template <bool LIST>
 __global__ __launch_bounds__(64, 2) void attention_few_kernel(AttnArgs A) {
     const int lane = threadIdx.x, col = lane & 15, grp = lane >> 4;
     Item it;
     Split sp;
-    uint32_t w, left;
-    if (!take_share<true>(A, &sp, &w, &left, &it)) return;
+    uint32_t w = 0, left;
+    if constexpr (LIST) {
+        if (!take_share<true>(A, &sp, &w, &left, &it)) return;
+    } else {
+        it.b = blockIdx.x / A.g;
+        it.kvh = blockIdx.x % A.g;
+        it.s = seq_rows(A.r, it.b);
+        if (!it.s.n) return;
+        it.c = it.t = 0;
+        left = it.n = tiles_of(it.s, A.m, 0);
+    }
     Columns<1> C;
     u32x4 q[2][2];
     const int r = A.a / A.g;
@@ -439,10 +450,10 @@ __global__ __launch_bounds__(64, 2) void attention_few_kernel(AttnArgs A) {
     };
     const float one[1] = {1.f};
     bool whole = it.t == 0;        // the share has the item from its first tile on
-    uint32_t x = sp.start(w);      // the list's tile
+    uint32_t x = LIST ? sp.start(w) : 0;      // the list's tile
     auto begin = [&](const Item& i) {
         C.begin(i.s, i.c * A.m, A.m, r);
-        if (whole && lane == 0) A.cut[i.b * A.g + i.kvh] = make_int2(w, sp.wave_of(x + i.n - 1) - w + 1);
+        if (LIST && whole && lane == 0) A.cut[i.b * A.g + i.kvh] = make_int2(w, sp.wave_of(x + i.n - 1) - w + 1);
     };
     C.load_q(A, it, it.c * A.m, A.m, 0, q);
     begin(it);
@@ -457,7 +468,7 @@ __global__ __launch_bounds__(64, 2) void attention_few_kernel(AttnArgs A) {
         bool more = left > 1;
         Item nx = it;
         if (more) {
-            if (ends)
+            if (LIST && ends)
                 more = next_item(A, nx);
             else
                 ++nx.t;
@@ -878,6 +889,11 @@ int many_shares(int simds) { return std::max(1, 3 * simds / 4); }
 
 }  // namespace
 
+// Up to this many positions an item of few columns runs on one wave: five tiles in a row take less time than a second
+// launch and its join.  One wave an item against shares, 32 heads on 8, in us: 16 sequences of up to 120 positions 5.2
+// against 8.5, 310 7.9 against 9.8, 440 11.1 against 10.6; 64 sequences of 120 6.9 against 12.3, 310 10.5 against 16.7.
+constexpr int kShort = 320;
+
 // Pieces, then what the join reads.
 size_t attention_fp8_bytes(int B, int g, int simds) {
     const size_t pieces = (size_t)2 * PSTRIDE * sizeof(float) * std::max(16 * few_shares(simds), 128 * many_shares(simds));
@@ -888,14 +904,20 @@ hipError_t attention_fp8(const NewRows& r, int a, int g, const uint16_t* q, cons
                          const float* sc, uint16_t* out, void* ws, int simds, hipStream_t st) {
     if (r.B < 1 || r.rows < 1 || r.n_pages < 1 || r.stride < 1 || a % g || a / g > 16) return hipErrorInvalidValue;
     const int heads = a / g;
+    // The list counts tiles in 31 bits; where it might not, items run one by one.
+    auto listed = [&](int64_t items) { return items * (r.max_pos / TILE + 1) <= INT32_MAX; };
     AttnArgs A{r, q, kc, vc, sc, out, (float*)ws, a, g, 0, 0, 0, nullptr, nullptr, (float)(1.4426950408889634 / sqrt((double)D))};
     hipError_t e;
     if (r.max_new * heads <= 16) {
         A.m = r.max_new;
         A.cols = A.m * heads;
+        if (r.max_pos < kShort || !listed((int64_t)r.B * g)) {
+            hipLaunchKernelGGL(attention_few_kernel<false>, dim3(r.B * g), dim3(64), 0, st, A);
+            return hipGetLastError();
+        }
         const int shares = few_shares(simds);
         A.cut = (int2*)(A.part + (size_t)2 * shares * A.cols * PSTRIDE);
-        hipLaunchKernelGGL(attention_few_kernel, dim3(shares), dim3(64), 0, st, A);
+        hipLaunchKernelGGL(attention_few_kernel<true>, dim3(shares), dim3(64), 0, st, A);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         hipLaunchKernelGGL(join_few_kernel, dim3(r.B * g * A.cols), dim3(kJoinThreads), 0, st, A);
         return hipGetLastError();
@@ -908,7 +930,8 @@ hipError_t attention_fp8(const NewRows& r, int a, int g, const uint16_t* q, cons
     // has as many for every sequence as the longest may have).
     const int shares = many_shares(simds);
     const int64_t items = (int64_t)g * (r.rows / A.m + r.B), grid = (int64_t)g * r.B * ((r.max_new + A.m - 1) / A.m);
-    if (items >= 2 * shares && grid <= 4 * items) {
+    if ((items >= 2 * shares && grid <= 4 * items) || !listed(items)) {
+        if (grid >= 1 << 24) return hipErrorInvalidValue;       // 2^32 threads
         hipLaunchKernelGGL(attention_many_kernel<false>, dim3((unsigned)grid), dim3(256), 0, st, A);
         return hipGetLastError();
     }

@@ -149,8 +149,10 @@ def check_append(before, after, table, lens, new, kv, exact_rows=None):
 
 def attention(q, kv, n, a):
     """q [T][a][128] at positions n, n + 1, ... over kv [2][n + T][g][128]: output [T][a][128] and a bound on the device's
-    difference: the softmax weights and the output are rounded to bf16, half a step of each (2^-8), and 1e-4 for the 32-bit
-    sums (of 128 products of a score, 128 * 2^-24 of their magnitudes, which the exponential turns into a share of a weight)."""
+    difference.  Its weights are w_i = p_i (1 + e_i), |e_i| <= 2^-8 (half a step of bf16), in the sum above and below the line:
+    sum w v / sum w - out = sum p_i e_i (v_i - out) / (1 + sum p_i e_i), at most 2^-8 / (1 - 2^-8) of sum p_i |v_i - out|; the
+    output's rounding is 2^-8 of it; and 1e-4 for the 32-bit sums (of 128 products of a score, 128 * 2^-24 of their magnitudes,
+    which the exponential turns into a share of a weight)."""
     T, g = q.shape[0], kv.shape[2]
     out, tol = np.zeros((T, a, D)), np.zeros((T, a, D))
     for t in range(T):
@@ -159,8 +161,9 @@ def attention(q, kv, n, a):
             s = k[:, h * g // a] @ q[t, h] / np.sqrt(D)
             p = np.exp(s - s.max())
             p /= p.sum()
-            out[t, h] = p @ v[:, h * g // a]
-            tol[t, h] = (2.0**-8 + 1e-4) * (p @ np.abs(v[:, h * g // a])) + 2.0**-8 * np.abs(out[t, h])
+            vh = v[:, h * g // a]
+            out[t, h] = p @ vh
+            tol[t, h] = p @ np.abs(vh - out[t, h]) / 255 + 1e-4 * (p @ np.abs(vh)) + 2.0**-8 * np.abs(out[t, h])
     return out, tol
 
 

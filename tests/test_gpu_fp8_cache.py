@@ -235,14 +235,14 @@ def test_append_queries_of_a_consumer_and_in_place():
 
 # ---- attention -----------------------------------------------------------------------------------
 
-def _attention(c, cu=True, pages=None, **kw):
+def _attention(c, cu=True, max_seq=1, **kw):
     """Runs kvp_attention_fp8 on rotated queries over a cache that holds the new rows too; output and the reference."""
     rng = np.random.default_rng(99)
     for b, (n, T) in enumerate(zip(c.lens, c.new)):
         if n >= 0 and T:
             c.cache.write(c.table, b, rng.standard_normal((2, n + T, c.g, D)) * (1 + np.arange(n + T) % 5)[None, :, None, None])
     dev = c.cache.to_device()
-    m = lr.model8(c.a, c.g, dev, c.cache.n_pages, len(c.lens), max(max(c.new), c.rows, 1))
+    m = lr.model8(c.a, c.g, dev, c.cache.n_pages, len(c.lens), max(max(c.new), c.rows, max_seq))
     r, keep = lr.rows_of(c.lens, c.new, c.table, cu=cu, rows=c.rows, **kw)
     q = _dev(c.x[:, : c.a].reshape(c.x.shape[0], -1))
     out = torch.full_like(q, 55.0)
@@ -284,6 +284,59 @@ def test_attention(a, g, lens, new):
     say(f"[attention] a={a} g={g} lens={lens} new={new}")
     c = Case(a, g, lens, new, seed=sum(new) + 3 * len(lens))
     _check_attention(c, _attention(c))
+
+
+@pytest.mark.parametrize("a,g,lens,new", ATTN)
+@pytest.mark.parametrize("max_pos,max_new", [(1500, 1), (0, 200), (1500, 999)])
+def test_attention_loose_bounds(a, g, lens, new, max_pos, max_new):
+    """The host's bounds (as of a captured call) may be far above what the device's lengths and rows turn out to be."""
+    say(f"[attention] a={a} g={g} lens={lens} new={new} max_pos={max_pos} max_new={max_new}")
+    c = Case(a, g, lens, new, seed=sum(new) + 3 * len(lens), stride=24)
+    _check_attention(c, _attention(c, max_pos=max_pos or None, max_new=max(max_new, *new), max_seq=max_new))
+
+
+@pytest.mark.parametrize("last", [318, 319, 320, 321])
+def test_attention_around_the_lengths_of_one_wave(last):
+    c = Case(8, 2, [last, 0, 319 - 64], [1] * 3, seed=last)
+    _check_attention(c, _attention(c))
+
+
+def _attention_64(c, b, q):
+    """Output and bound of sequence b's rows, as lr.attention, on the device in 64 bits."""
+    n, T, r = c.lens[b], c.new[b], c.a // c.g
+    kv = torch.from_numpy(c.cache.values(c.table, b, n + T)).cuda().double()
+    qd = torch.from_numpy(q.astype(np.float64)).cuda()
+    hide = torch.arange(n + T, device="cuda")[None] > n + torch.arange(T, device="cuda")[:, None]
+    out, tol = torch.empty_like(qd), torch.empty_like(qd)
+    for h in range(c.a):
+        k, v = kv[:, :, h // r]
+        p = (qd[:, h] @ k.T / np.sqrt(D)).masked_fill(hide, -np.inf).softmax(-1)
+        out[:, h] = p @ v
+        for d in range(0, D, 16):
+            tol[:, h, d: d + 16] = torch.einsum("tk,tkd->td", p, (v[None, :, d: d + 16] - out[:, h, None, d: d + 16]).abs()) / 255
+        tol[:, h] += 1e-4 * (p @ v.abs()) + 2.0**-8 * out[:, h].abs()
+    return out.cpu().numpy(), tol.cpu().numpy()
+
+
+@pytest.mark.parametrize("a,g,lens,new", [
+    (128, 8, [100, 0], [903, 731]),                      # more blocks of rows than two a workgroup: one by one
+    (64, 16, [0, 63, -1, 17], [700, 1, 40, 801]),
+    (2, 1, [20001], [1]), (4, 1, [18000, 5], [4, 2]),    # more than 256 pieces to join
+    (2, 1, [21000], [40]),
+])
+def test_attention_many_blocks_and_many_pieces(a, g, lens, new):
+    say(f"[attention] a={a} g={g} lens={lens} new={new}")
+    c = Case(a, g, lens, new, seed=31)
+    got = _attention(c)
+    for b, (n, T) in enumerate(zip(lens, new)):
+        rows = slice(int(c.cu[b]), int(c.cu[b]) + T)
+        if n < 0:
+            assert (got[rows] == 0).all()
+            continue
+        want, tol = _attention_64(c, b, c.x[rows, :a])
+        say(f"[attention] sequence {b}: {np.abs((got[rows] - want) / tol).max():.3f} of the bound")
+        assert np.isfinite(got[rows]).all() and (np.abs(got[rows] - want) <= tol).all(), \
+            (b, np.abs((got[rows] - want) / tol).max())
 
 
 def test_attention_one_row_each_without_cu():
