@@ -23,7 +23,8 @@
 // (sequence, K/V head, block, tile), which the waves (workgroups) share evenly: an item that begins
 // and ends with one of them is written by it, the others leave their pieces (running maximum, sum,
 // unnormalised O) to a second kernel.  Where there are many more items than workgroups they run one by
-// one instead, the longest first.
+// one instead, the longest first; so do items of few columns over short contexts, a workgroup of 1, 2 or
+// 8 waves each, which join in LDS.
 #include <math.h>
 
 #include <algorithm>
@@ -410,10 +411,12 @@ struct Columns {
     }
 };
 
-// LIST: a share of the list; else one item.
-template <bool LIST>
-__global__ __launch_bounds__(64, 2) void attention_few_kernel(AttnArgs A) {
-    const int lane = threadIdx.x, col = lane & 15, grp = lane >> 4;
+// NW 0: a share of the list, one wave.  Else one item, whose tiles NW waves take in turn and join in LDS.
+template <int NW>
+__global__ __launch_bounds__(NW ? 64 * NW : 64, 2) void attention_few_kernel(AttnArgs A) {
+    constexpr bool LIST = NW == 0;
+    constexpr int STEP = LIST ? 1 : NW;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
     Item it;
     Split sp;
     uint32_t w = 0, left;
@@ -424,8 +427,10 @@ __global__ __launch_bounds__(64, 2) void attention_few_kernel(AttnArgs A) {
         it.kvh = blockIdx.x % A.g;
         it.s = seq_rows(A.r, it.b);
         if (!it.s.n) return;
-        it.c = it.t = 0;
-        left = it.n = tiles_of(it.s, A.m, 0);
+        it.c = 0;
+        it.t = wave;
+        it.n = tiles_of(it.s, A.m, 0);
+        left = max(it.n - wave + NW - 1, 0) / NW;
     }
     Columns<1> C;
     u32x4 q[2][2];
@@ -449,7 +454,7 @@ __global__ __launch_bounds__(64, 2) void attention_few_kernel(AttnArgs A) {
         for (int db = 0; db < 8; ++db) v[db] = *(const u32x4*)(p + 16 * db * kBlk + voff);
     };
     const float one[1] = {1.f};
-    bool whole = it.t == 0;        // the share has the item from its first tile on
+    bool whole = !LIST || it.t == 0;        // the share has the item from its first tile on
     uint32_t x = LIST ? sp.start(w) : 0;      // the list's tile
     auto begin = [&](const Item& i) {
         C.begin(i.s, i.c * A.m, A.m, r);
@@ -457,21 +462,21 @@ __global__ __launch_bounds__(64, 2) void attention_few_kernel(AttnArgs A) {
     };
     C.load_q(A, it, it.c * A.m, A.m, 0, q);
     begin(it);
-    {
+    if (NW < 2 || left) {
         const size_t at = tab.page(A, it);
         load_k(at);
         load_v(at);
     }
-    for (;;) {
+    while (NW < 2 || left) {
         // The next tile of the share, perhaps in the next item.
-        const bool ends = it.t + 1 == it.n;
+        const bool ends = it.t + STEP >= it.n;
         bool more = left > 1;
         Item nx = it;
         if (more) {
             if (LIST && ends)
                 more = next_item(A, nx);
             else
-                ++nx.t;
+                nx.t += STEP;
         }
         const size_t at = more ? tab.page(A, nx) : 0;
         const int p0 = TILE * it.t + 16 * grp;
@@ -510,6 +515,7 @@ __global__ __launch_bounds__(64, 2) void attention_few_kernel(AttnArgs A) {
                 C.o[0][db] = mfma16x16x32(widen(v[db][2 * h], v[db][2 * h + 1]), pb[0][h], C.o[0][db]);
         __builtin_amdgcn_sched_barrier(0);
         if (more) load_v(at);
+        if (NW > 1 && !more) break;
         if (ends || !more) {
             C.finish(A, it, it.c * A.m, A.m, whole && ends, A.part + (2 * (size_t)w + (whole ? 1 : 0)) * A.cols * PSTRIDE);
             if (!more) break;
@@ -521,6 +527,26 @@ __global__ __launch_bounds__(64, 2) void attention_few_kernel(AttnArgs A) {
         it = nx;
         ++x;
         --left;
+    }
+    if constexpr (NW > 1) {
+        __shared__ float parts[NW][16][PSTRIDE];
+        C.finish(A, it, 0, A.m, false, &parts[wave][0][0]);
+        __syncthreads();
+        const int cols = min(A.cols, it.s.n * r);
+        for (int c = wave; c < cols; c += NW) {
+            float M = kNoScore, den = 0.f;
+            f32x2 num = {0.f, 0.f};
+#pragma unroll
+            for (int v = 0; v < NW; ++v) M = fmaxf(M, parts[v][c][D]);
+#pragma unroll
+            for (int v = 0; v < NW; ++v) {
+                const float f = __builtin_amdgcn_exp2f(parts[v][c][D] - M);
+                den += f * parts[v][c][D + 1];
+                num += f * *(const f32x2*)&parts[v][c][2 * lane];
+            }
+            const uint32_t o = c / r < it.s.act ? pack2bf(num[0] / den, num[1] / den) : 0u;
+            *(uint32_t*)(A.out + ((size_t)(it.s.row0 + c / r) * A.a + it.kvh * r + c % r) * D + 2 * lane) = o;
+        }
     }
 }
 
@@ -887,12 +913,20 @@ __global__ __launch_bounds__(kJoinThreads) void join_many_kernel(AttnArgs A) {
 int few_shares(int simds) { return std::min(simds, kMaxDecodeSplits); }
 int many_shares(int simds) { return std::max(1, 3 * simds / 4); }
 
-}  // namespace
+// Waves that take an item of few columns where a launch without a list and a join is the faster one, else 0.  One
+// workgroup an item against the list, 32 heads on 8, in us: 1 sequence of 500 positions 6.5 against 8.4, 1000 8.7
+// against 8.7, 2000 13.1 against 9.2; 8 sequences of 1000 9.6 against 11.2, 2000 14.7 against 14.4; 16 of 2000 15.1
+// against 19.0, 4000 34 against 33; 64 of 500 14.8 against 19.5, 2000 53 against 59; 100 of 1000 41 against 54.  (Past
+// 2048 positions one long sequence among short ones would cost more than there is to gain.)  8, 2 and 1 waves: 32
+// sequences of 500 positions 9.5, 9.8 and 12.9; 64 of 1000 31, 29 and 36; 100 of 1000 51, 46 and 41; 16 of 60 4.7,
+// 4.6 and 4.1.
+int few_waves(int64_t items, int max_pos, int simds) {
+    if (max_pos < 2 * TILE) return 1;
+    if (max_pos >= std::min<int64_t>(2048, 900 + 17 * items)) return 0;
+    return items <= simds / 4 ? 8 : items <= simds / 2 ? 2 : 1;
+}
 
-// Up to this many positions an item of few columns runs on one wave: five tiles in a row take less time than a second
-// launch and its join.  One wave an item against shares, 32 heads on 8, in us: 16 sequences of up to 120 positions 5.2
-// against 8.5, 310 7.9 against 9.8, 440 11.1 against 10.6; 64 sequences of 120 6.9 against 12.3, 310 10.5 against 16.7.
-constexpr int kShort = 320;
+}  // namespace
 
 // Pieces, then what the join reads.
 size_t attention_fp8_bytes(int B, int g, int simds) {
@@ -911,13 +945,19 @@ hipError_t attention_fp8(const NewRows& r, int a, int g, const uint16_t* q, cons
     if (r.max_new * heads <= 16) {
         A.m = r.max_new;
         A.cols = A.m * heads;
-        if (r.max_pos < kShort || !listed((int64_t)r.B * g)) {
-            hipLaunchKernelGGL(attention_few_kernel<false>, dim3(r.B * g), dim3(64), 0, st, A);
+        const int items = r.B * g, nw = listed(items) ? few_waves(items, r.max_pos, simds) : 1;
+        if (nw) {
+            if (nw == 8)
+                hipLaunchKernelGGL(attention_few_kernel<8>, dim3(items), dim3(512), 0, st, A);
+            else if (nw == 2)
+                hipLaunchKernelGGL(attention_few_kernel<2>, dim3(items), dim3(128), 0, st, A);
+            else
+                hipLaunchKernelGGL(attention_few_kernel<1>, dim3(items), dim3(64), 0, st, A);
             return hipGetLastError();
         }
         const int shares = few_shares(simds);
         A.cut = (int2*)(A.part + (size_t)2 * shares * A.cols * PSTRIDE);
-        hipLaunchKernelGGL(attention_few_kernel<true>, dim3(shares), dim3(64), 0, st, A);
+        hipLaunchKernelGGL(attention_few_kernel<0>, dim3(shares), dim3(64), 0, st, A);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         hipLaunchKernelGGL(join_few_kernel, dim3(r.B * g * A.cols), dim3(kJoinThreads), 0, st, A);
         return hipGetLastError();

@@ -295,9 +295,18 @@ def test_attention_loose_bounds(a, g, lens, new, max_pos, max_new):
     _check_attention(c, _attention(c, max_pos=max_pos or None, max_new=max(max_new, *new), max_seq=max_new))
 
 
-@pytest.mark.parametrize("last", [318, 319, 320, 321])
-def test_attention_around_the_lengths_of_one_wave(last):
-    c = Case(8, 2, [last, 0, 319 - 64], [1] * 3, seed=last)
+@pytest.mark.parametrize("last", [126, 127, 128, 129, 1000, 1001, 1002, 1003])
+def test_attention_around_the_lengths_that_change_the_launch(last):
+    c = Case(8, 2, [last, 0, last - 64], [1] * 3, seed=last)
+    _check_attention(c, _attention(c))
+
+
+@pytest.mark.parametrize("a,g", [(2, 1), (4, 2), (4, 4)])
+@pytest.mark.parametrize("new", [1, 3])
+def test_attention_workgroups_of_8_2_and_1_waves(a, g, new):
+    """150 sequences of up to ten tiles, some without a row, with one tile, inactive."""
+    lens = [(173 * i) % 640 - (650 if i % 19 == 0 else 0) for i in range(150)]
+    c = Case(a, g, lens, [new - (new > 1) * (i % (new + 1)) for i in range(150)], seed=33)
     _check_attention(c, _attention(c))
 
 
