@@ -10,8 +10,11 @@
 // A code becomes a bf16 number by placing it in the top four bits of the mantissa of 1.0: 1 + c / 16,
 // one shift and one and-or for two codes.  (c - 8) / 16 is 1.5 less, so a second product with the
 // constant -1.5 in place of the weights takes 1.5 sum_k x[m][k] off again.  Both run on the matrix
-// cores with fp32 sums, which the weights' stream leaves idle; the group's scale multiplies the fp32
-// sum of its inputs.
+// cores with fp32 sums; the group's scale multiplies the fp32 sum of its inputs.
+//
+// Bound: few rows by reading the weights, in the time that a launch with cold weights allows (1 row, 6144 x 4096,
+// 13 MB: 5.3 us, a bare read of as much 3.2; 14000 x 11008, 80 MB: 15.4 us, a bare read 12.5); more rows also by what
+// every CU reads of x (16 rows, 8192 x 8192: 9.3 us, 36 MB of weights 6.6; 64 rows: 19.0 us, 1 MB of x a CU through LDS).
 #include "common.h"
 #include "kernels.h"
 
@@ -31,17 +34,31 @@ __device__ __forceinline__ bf16x8 widen4(uint32_t w, uint32_t mask, uint32_t one
 
 __device__ __forceinline__ float bf(uint32_t u) { return __uint_as_float(u << 16); }
 
+constexpr int NW = 8;      // waves a workgroup
+
 typedef __attribute__((address_space(1))) void gvoid_t;
 typedef __attribute__((address_space(3))) void lvoid_t;
 
-// Workgroup: 16 NT outputs and 16 NMB rows, of them at most ROWS of x; its waves take every NW-th 128 inputs, U of
-// them at a time, all of their loads ahead of the products.  A wave's x goes through a part of LDS of its own, in
-// whole lines of memory: fragments read from memory would touch 16 half lines each, which bounded everything from 4
-// rows on (64 rows, 6144 x 4096: 19 us).  GS: groups of scales in 128 inputs.
-template <int NMB, int ROWS, int NT, int U, int NW, int GS>
+// 16-byte LDS reads at a[0..3] + OFF and their wait: written by hand, since the compiler would first wait for the
+// loads that go into the other stage.
+template <int OFF>
+__device__ __forceinline__ void lds_four(const uint32_t (&a)[4], u32x4 (&f)[4]) {
+    asm volatile("ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%8\n\tds_read_b128 %2, %6 offset:%8\n\t"
+                 "ds_read_b128 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "i"(OFF)
+                 : "memory");
+}
+
+// Workgroup: 16 NT outputs and 16 NMB rows, of them at most ROWS of x; its NW waves take every NW-th 128 inputs.  A
+// wave's x goes through a part of LDS of its own, in whole lines of memory: fragments read from memory would touch
+// 16 half lines each, which bounded everything from 4 rows on (64 rows, 6144 x 4096: 19 us).  ST 2: the next 128
+// inputs are under way during the products (8192 x 8192, 16 rows, 10.0 to 9.4 us); of 64 rows LDS holds one stage.
+// GS: groups of scales in 128 inputs.
+template <int NMB, int ROWS, int NT, int ST, int GS>
 __global__ __launch_bounds__(64 * NW, NW / 4) void linear_kernel(const uint16_t* __restrict__ X, W4Rows W, int M, int N,
                                                                  int K, LinearOut out) {
-    constexpr int XS = U * ROWS * 16, RS = NT * NMB * 64;          // 16-byte words of a wave: x, partial sums
+    constexpr int XS = ST * ROWS * 16, RS = NT * NMB * 64;          // 16-byte words of a wave: x, partial sums
     __shared__ u32x4 lds[NW * (XS > RS ? XS : RS)];
     f32x4* red = (f32x4*)lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, kg = lane >> 4;
@@ -68,63 +85,71 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void linear_kernel(const uint16_t*
     const uint16_t* xb = X + (size_t)m0 * K;
     const int rows = min(ROWS, M - m0);
     const int xr = ROWS == 4 ? col & 3 : col;          // the lane's row of a block
+    uint32_t xa[4];                                    // addresses of its four chunks
+#pragma unroll
+    for (int w = 0; w < 4; ++w) xa[w] = (uint32_t)(uintptr_t)(xl + xr * 16 + ((4 * w + kg) ^ xr));
     uint32_t mask = 0x00780078u, one = 0x3F803F80u;
     asm("" : "+s"(mask), "+v"(one));
     const bf16x8 off = as_bf16x8(u32x4{0xBFC0BFC0u, 0xBFC0BFC0u, 0xBFC0BFC0u, 0xBFC0BFC0u});   // -1.5
-    for (int kb0 = wave; kb0 < KB; kb0 += U * NW) {
-        u32x4 c[U][NT];
-        u32x2 sw[U][NT][GS];
+    struct Codes {
+        u32x4 c[NT];
+        u32x2 s[NT][GS];
+    };
+    auto request = [&](Codes& S, int kb, int stg) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int kb = min(kb0 + u * NW, KB - 1);       // past the last: weighs nothing
+        for (int j = 0; j < ROWS / 4; ++j) {
+            if (j && 4 * j >= rows) break;
+            const int r = 4 * j + (lane >> 4);
+            __builtin_amdgcn_global_load_lds(
+                (gvoid_t*)(xb + (size_t)kb * 128 + (uint32_t)(min(r, rows - 1) * K + 8 * ((lane & 15) ^ (r & 15)))),
+                (lvoid_t*)(xl + (stg * ROWS + 4 * j) * 16), 16, 0, 0);
+        }
 #pragma unroll
-            for (int j = 0; j < ROWS / 4; ++j) {
-                if (j && 4 * j >= rows) break;
-                const int r = 4 * j + (lane >> 4);
-                __builtin_amdgcn_global_load_lds(
-                    (gvoid_t*)(xb + (size_t)kb * 128 + (uint32_t)(min(r, rows - 1) * K + 8 * ((lane & 15) ^ (r & 15)))),
-                    (lvoid_t*)(xl + (u * ROWS + 4 * j) * 16), 16, 0, 0);
-            }
+        for (int i = 0; i < NT; ++i) {
+            S.c[i] = *(const u32x4*)(codes[i] + (size_t)kb * 1024 + (uint32_t)(16 * lane));
+#pragma unroll
+            for (int g = 0; g < GS; ++g)
+                S.s[i][g] = *(const u32x2*)(scales[i] + (size_t)(kb * GS + g) * 16 + (uint32_t)(4 * kg));
+        }
+    };
+    Codes now, next;
+    if (ST == 2 && wave < KB) request(next, wave, 0);
+    for (int kb = wave, stg = 0; kb < KB; kb += NW, stg ^= ST - 1) {
+        if (ST == 1) request(next, kb, 0);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // x is in LDS
+        now = next;
+        if (ST == 2 && kb + NW < KB) request(next, kb + NW, stg ^ 1);
+        __builtin_amdgcn_sched_barrier(0);
+        uint32_t at[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) at[w] = xa[w] + stg * (ROWS * 256);
+        u32x4 x[NMB][4];
+        lds_four<0>(at, x[0]);
+        if constexpr (NMB > 1) lds_four<16 * 256>(at, x[1]);
+        if constexpr (NMB > 2) lds_four<32 * 256>(at, x[2]);
+        if constexpr (NMB > 3) lds_four<48 * 256>(at, x[3]);
+#pragma unroll
+        for (int g = 0; g < GS; ++g) {
+            f32x4 none[NMB];          // -1.5 sum_k x, for all outputs
+#pragma unroll
+            for (int w = g * (4 / GS); w < (g + 1) * (4 / GS); ++w)
+#pragma unroll
+                for (int mb = 0; mb < NMB; ++mb)
+                    none[mb] = mfma16x16x32(off, as_bf16x8(x[mb][w]), w % (4 / GS) ? none[mb] : f32x4{});
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-                c[u][i] = *(const u32x4*)(codes[i] + (size_t)kb * 1024 + (uint32_t)(16 * lane));
+                f32x4 part[NMB];
 #pragma unroll
-                for (int g = 0; g < GS; ++g)
-                    sw[u][i][g] = *(const u32x2*)(scales[i] + (size_t)(kb * GS + g) * 16 + (uint32_t)(4 * kg));
-            }
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // x is in LDS
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t live = U == 1 || kb0 + u * NW < KB ? 0xFFFFFFFFu : 0u;
-            u32x4 x[NMB][4];
-#pragma unroll
-            for (int mb = 0; mb < NMB; ++mb)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) x[mb][w] = xl[(u * ROWS + 16 * mb + xr) * 16 + ((4 * w + kg) ^ xr)];
-#pragma unroll
-            for (int g = 0; g < GS; ++g) {
-                f32x4 none[NMB];          // -1.5 sum_k x, for all outputs
-#pragma unroll
-                for (int w = g * (4 / GS); w < (g + 1) * (4 / GS); ++w)
+                for (int w = g * (4 / GS); w < (g + 1) * (4 / GS); ++w) {
+                    const bf16x8 wf = widen4(now.c[i][w], mask, one);
 #pragma unroll
                     for (int mb = 0; mb < NMB; ++mb)
-                        none[mb] = mfma16x16x32(off, as_bf16x8(x[mb][w]), w % (4 / GS) ? none[mb] : f32x4{});
-#pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    f32x4 part[NMB];
-#pragma unroll
-                    for (int w = g * (4 / GS); w < (g + 1) * (4 / GS); ++w) {
-                        const bf16x8 wf = widen4(c[u][i][w], mask, one);
-#pragma unroll
-                        for (int mb = 0; mb < NMB; ++mb)
-                            part[mb] = mfma16x16x32(wf, as_bf16x8(x[mb][w]), w % (4 / GS) ? part[mb] : none[mb]);
-                    }
-                    const u32x2 s = U == 1 ? sw[u][i][g] : sw[u][i][g] & live;
-                    const f32x4 sf = {bf(s[0]), __uint_as_float(s[0] & 0xFFFF0000u), bf(s[1]), __uint_as_float(s[1] & 0xFFFF0000u)};
-#pragma unroll
-                    for (int mb = 0; mb < NMB; ++mb) acc[i][mb] += sf * part[mb];
+                        part[mb] = mfma16x16x32(wf, as_bf16x8(x[mb][w]), w % (4 / GS) ? part[mb] : none[mb]);
                 }
+                const u32x2 s = now.s[i][g];
+                const f32x4 sf = {bf(s[0]), __uint_as_float(s[0] & 0xFFFF0000u), bf(s[1]), __uint_as_float(s[1] & 0xFFFF0000u)};
+#pragma unroll
+                for (int mb = 0; mb < NMB; ++mb) acc[i][mb] += sf * part[mb];
             }
         }
     }
@@ -215,21 +240,31 @@ __global__ __launch_bounds__(64) void pack_kernel(const uint16_t* __restrict__ W
     *(u32x4*)(out + ((size_t)nb * KB + kb) * 1024 + 16 * lane) = c;
 }
 
-template <int NMB, int ROWS, int NT, int U, int NW, int GS>
+template <int NMB, int ROWS, int NT, int ST, int GS>
 hipError_t launch(const uint16_t* x, const W4Rows& w, int M, int N, int K, const LinearOut& o, hipStream_t st) {
     const dim3 grid(((N + 15) / 16 + NT - 1) / NT, (M + 16 * NMB - 1) / (16 * NMB)), block(64 * NW);
-    hipLaunchKernelGGL((linear_kernel<NMB, ROWS, NT, U, NW, GS>), grid, block, 0, st, x, w, M, N, K, o);
+    hipLaunchKernelGGL((linear_kernel<NMB, ROWS, NT, ST, GS>), grid, block, 0, st, x, w, M, N, K, o);
     return hipGetLastError();
+}
+// Blocks of 16 outputs a workgroup: as few as one workgroup on each of the 256 CUs allows, up to 4.  Every
+// workgroup reads all of x, and a second one on some of the CUs costs as much as on all.  8192 inputs, us: 64 rows,
+// 2048 outputs 13.9 with 1 block (16.2 with 2), 10240 21.8 with 3 (31.2 with 2), 14000 27.0 with 4 (33.0 with 2); 16
+// rows, 4096 outputs 7.0 with 1 (8.3 with 2), 10240 11.1 with 3 (13.9 with 2).  11008 inputs, 1 row: 8192 outputs
+// 9.8 with 2 (10.3 with 1), 14000 15.4 with 4 (16.5 with 1).
+template <int NMB, int ROWS, int ST, int GS>
+hipError_t launch_some(const uint16_t* x, const W4Rows& w, int M, int N, int K, const LinearOut& o, hipStream_t st) {
+    const int64_t blocks = (int64_t)((N + 15) / 16) * ((M + 16 * NMB - 1) / (16 * NMB)), nt = (blocks + 255) / 256;
+    if (nt <= 1) return launch<NMB, ROWS, 1, ST, GS>(x, w, M, N, K, o, st);
+    if (nt == 2) return launch<NMB, ROWS, 2, ST, GS>(x, w, M, N, K, o, st);
+    if (nt == 3) return launch<NMB, ROWS, 3, ST, GS>(x, w, M, N, K, o, st);
+    return launch<NMB, ROWS, 4, ST, GS>(x, w, M, N, K, o, st);
 }
 template <int GS>
 hipError_t launch(const uint16_t* x, const W4Rows& w, int M, int N, int K, const LinearOut& o, hipStream_t st) {
-    // 16 outputs a workgroup while x is short, then 32, which share what is read of x: 1 row, 4096 x 4096, 3.9
-    // us (32 outputs: 5.3; 16 waves: 4.1); 16 rows, 8192 x 8192, 10.9 us (16 outputs: 14.2), 64 rows, 6144 x
-    // 4096, 11.0 us (16 outputs: 16.8).
-    if (M <= 4) return launch<1, 4, 1, 2, 8, GS>(x, w, M, N, K, o, st);
-    if (M <= 16) return launch<1, 16, 2, 2, 8, GS>(x, w, M, N, K, o, st);
-    if (M <= 32) return launch<2, 32, 2, 1, 8, GS>(x, w, M, N, K, o, st);
-    return launch<4, 64, 2, 1, 8, GS>(x, w, M, N, K, o, st);
+    if (M <= 4) return launch_some<1, 4, 2, GS>(x, w, M, N, K, o, st);
+    if (M <= 16) return launch_some<1, 16, 2, GS>(x, w, M, N, K, o, st);
+    if (M <= 32) return launch_some<2, 32, 2, GS>(x, w, M, N, K, o, st);
+    return launch_some<4, 64, 1, GS>(x, w, M, N, K, o, st);
 }
 
 }  // namespace

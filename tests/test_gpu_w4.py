@@ -113,6 +113,20 @@ def test_linear(M, N, K, group):
     assert (np.abs(got - y) <= tol).all(), np.abs((got - y) / tol).max()
 
 
+@pytest.mark.parametrize("M", [3, 16, 32, 64, 200])
+@pytest.mark.parametrize("N,K,group", [(4100, 256, 32), (8195, 128, 64), (12288, 1280, 128), (17000, 256, 128)])
+def test_linear_many_outputs(M, N, K, group):
+    """One to four blocks of 16 outputs a workgroup, with blocks left over."""
+    say(f"[linear w4] M={M} N={N} K={K} group={group}")
+    rng = np.random.default_rng(M + N)
+    codes, s = lr.w4_codes(lr.bf16(_normal(rng, N, K) * np.float32(0.1)), group)
+    buf = torch.from_numpy(lr.w4_pack(codes, s)).cuda()
+    x = _normal(rng, M, K)
+    y = x.astype(np.float64) @ lr.w4_weights(codes, s, group).T
+    got = _linear(x, buf, N, group)
+    assert (np.abs(got - y) <= lr.linear_bound(x.astype(np.float64), y, s, group)).all()
+
+
 @pytest.mark.parametrize("inplace", [False, True])
 def test_linear_residual(inplace):
     rng = np.random.default_rng(3)
