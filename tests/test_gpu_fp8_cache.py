@@ -301,8 +301,8 @@ def test_attention_around_the_lengths_that_change_the_launch(last):
     _check_attention(c, _attention(c))
 
 
-@pytest.mark.parametrize("a,g", [(2, 1), (4, 2), (4, 4)])
-@pytest.mark.parametrize("new", [1, 3])
+@pytest.mark.parametrize("a,g", [(2, 1), (4, 2), (8, 4)])
+@pytest.mark.parametrize("new", [1, 3, 12])
 def test_attention_workgroups_of_8_2_and_1_waves(a, g, new):
     """150 sequences of up to ten tiles, some without a row, with one tile, inactive."""
     lens = [(173 * i) % 640 - (650 if i % 19 == 0 else 0) for i in range(150)]
@@ -328,10 +328,12 @@ def _attention_64(c, b, q):
 
 
 @pytest.mark.parametrize("a,g,lens,new", [
-    (128, 8, [100, 0], [903, 731]),                      # more blocks of rows than two a workgroup: one by one
+    (128, 8, [100, 0], [903, 731]),                      # more blocks of rows than workgroups: one by one
     (64, 16, [0, 63, -1, 17], [700, 1, 40, 801]),
     (2, 1, [20001], [1]), (4, 1, [18000, 5], [4, 2]),    # more than 256 pieces to join
-    (2, 1, [21000], [40]),
+    (2, 1, [21000], [40]), (8, 2, [9000, 300], [9, 12]), (8, 2, [9000, 300], [5, 8]),
+    (16, 4, [(41 * i) % 3001 for i in range(70)], [5 + i % 8 for i in range(70)]),      # few pieces an item
+    (64, 16, [2500, 2990], [300, 280]),
 ])
 def test_attention_many_blocks_and_many_pieces(a, g, lens, new):
     say(f"[attention] a={a} g={g} lens={lens} new={new}")
