@@ -17,8 +17,8 @@
 // attention_few_kernel: sequences with at most 32 columns (single tokens, a few proposed ones); K and V go straight
 // to registers.  Bound by reading the cache: 64 x 32768 positions (32 heads on 8, 4.3 GB) 707 us, 6.1 TB/s; 8 x
 // 64K-128K 276 us, 5.8 TB/s.  attention_many_kernel: more columns; four waves share each tile through LDS.  Bound by
-// the vector instructions (widening, softmax) beside the matrix ones: prompts of 4 x 4096 rows (16 heads on 8) 271 us,
-// 1010 TFLOP/s.
+// the vector instructions (widening, softmax) beside the matrix ones: prompts of 4 x 4096 rows (16 heads on 8) 270 us,
+// 1018 TFLOP/s.
 //
 // Work: the tiles of all items (a sequence's block of rows and a K/V head) in one list, in the order
 // (sequence, K/V head, block, tile), which the waves (workgroups) share evenly: an item that begins
@@ -640,10 +640,10 @@ __device__ __forceinline__ void lds_run(uint32_t a, u32x4 (&f)[4]) {
                  : "memory");
 }
 
-// Workgroup: an item of 4 mw rows, wave v's 32 columns are its rows v mw .. (v + 1) mw - 1.  The tiles
+// Workgroup: an item of 4 mw rows, wave v's 16 NB columns are its rows v mw .. (v + 1) mw - 1.  The tiles
 // go from memory to LDS directly, two stages of 16 KB, one barrier a tile: it ends the loads of the
-// tile that comes and the reads of the one before it, whose stage is then loaded again.  Three
-// workgroups a CU run in each other's waits.
+// tile that comes and the reads of the one before it, whose stage is then loaded again.  Three (NB 1:
+// four) workgroups a CU run in each other's waits.
 // LIST: a share of the list; else one item, counted from a sequence's last.
 template <bool LIST, int NB>
 __global__ __launch_bounds__(256, NB == 1 ? 4 : 3) void attention_many_kernel(AttnArgs A) {
@@ -975,8 +975,9 @@ __global__ __launch_bounds__(kJoinThreads) void join_long_kernel(AttnArgs A) {
 
 // Shares of the list.  Few: one wave a SIMD (of 1, 1.5, 2 and 3 a SIMD, us: 64 x 32768 positions 738, 743,
 // 746, 761; 8 x 64K-128K 287, 290, 292, 299; 16 x 4 rows over 1500-8000 positions 44, 46, 47, 52; 3/4 of a wave
-// 739, 289, 45; half a wave 930, 359, 50; requesting two tiles ahead changes none of them).  Many: three
-// workgroups a CU (two, without a limit on the registers: prompts of 4 x 4096 rows 6 % slower).
+// 739, 289, 45; half a wave 930, 359, 50; requesting two tiles ahead changes none of them).  Many: as many
+// workgroups as a CU holds, three with 32 columns a wave (two, without a limit on the registers: prompts of 4 x
+// 4096 rows 6 % slower), four with 16.
 int few_shares(int simds) { return std::min(simds, kMaxDecodeSplits); }
 int many_shares(int simds, int nb) { return std::max(1, (nb == 1 ? 4 : 3) * simds / 4); }
 
@@ -1058,8 +1059,9 @@ hipError_t attention_fp8(const NewRows& r, int a, int g, const uint16_t* q, cons
     const double n = r.max_pos / TILE + 1, T = 0.6 * items * n;
     const double one = 6 + 1.65 * n + T / 512 + grid / 2000.,
                  list = 12 + T / 256 + (std::min<double>(T, shares) + items) * A.cols * (PSTRIDE * sizeof(float)) / 2.3e6;
-    if (one < list || !listed(items)) {
-        if (grid >= 1 << 24) return hipErrorInvalidValue;       // 2^32 threads
+    const bool fits = grid < 1 << 24;       // 2^32 threads
+    if ((one < list && fits) || !listed(items)) {
+        if (!fits) return hipErrorInvalidValue;
         nb == 1 ? launch_many<1>(false, grid, A, st) : launch_many<2>(false, grid, A, st);
         return hipGetLastError();
     }
