@@ -17,8 +17,8 @@
 // attention_few_kernel: sequences with at most 32 columns (single tokens, a few proposed ones); K and V go straight
 // to registers.  Bound by reading the cache: 64 x 32768 positions (32 heads on 8, 4.3 GB) 707 us, 6.1 TB/s; 8 x
 // 64K-128K 276 us, 5.8 TB/s.  attention_many_kernel: more columns; four waves share each tile through LDS.  Bound by
-// the vector instructions (widening, softmax) beside the matrix ones: prompts of 4 x 4096 rows (16 heads on 8) 270 us,
-// 1018 TFLOP/s.
+// the vector instructions (widening, softmax) beside the matrix ones: prompts of 4 x 4096 rows (16 heads on 8) 265-270 us,
+// 1018-1037 TFLOP/s.
 //
 // Work: the tiles of all items (a sequence's block of rows and a K/V head) in one list, in the order
 // (sequence, K/V head, block, tile), which the waves (workgroups) share evenly: an item that begins
@@ -807,6 +807,53 @@ __device__ __forceinline__ size_t slot_of(int w0, int i) { return 2 * (size_t)(w
 
 constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
 
+// Joins np pieces of NC columns, half a wave a piece, 8 requested at a time: lane holds dimensions 4 (lane % 32) .. + 3 of
+// num.  piece(i, j): piece i of column j.
+template <int NC, class Piece>
+__device__ __forceinline__ void join_halves(int np, Piece piece, f32x4 (&num)[NC], float (&den)[NC]) {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    float M[NC], wt[NC];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+        M[j] = -INFINITY;
+        den[j] = 0.f;
+        num[j] = f32x4{};
+    }
+    for (int s0 = 0; s0 < np; s0 += 64) {
+        const int k = min(np - s0, 64);
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            float m = -INFINITY, l = 0.f;
+            if (lane < k) {
+                const float* p = piece(s0 + lane, j);
+                m = p[D];
+                l = p[D + 1];
+            }
+            const float Mn = fmaxf(M[j], wave_max(m)), f = exp2f(M[j] - Mn);
+            wt[j] = exp2f(m - Mn);
+            den[j] = den[j] * f + wave_sum(wt[j] * l);
+            num[j] *= f;
+            M[j] = Mn;
+        }
+        for (int i = 0; i < k; i += 8) {
+            f32x4 v[NC][4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int j = 0; j < NC; ++j)       // a piece past the last weighs nothing
+                    v[j][u] = *(const f32x4*)(piece(s0 + min(i + 2 * u + half, k - 1), j) + 4 * (lane & 31));
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int j = 0; j < NC; ++j) num[j] += __shfl(wt[j], i + 2 * u + half) * v[j][u];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) num[j][e] += __shfl_xor(num[j][e], 32);
+}
+
 // One new row a sequence or a few (an item is a sequence and K/V head): a workgroup a column.  Wave
 // v takes pieces v, v + 4, ...: lane i holds the maximum and sum of its i-th, every lane two of the
 // 128 dimensions; the waves meet in LDS.
@@ -874,6 +921,27 @@ __global__ __launch_bounds__(kJoinThreads) void join_few_kernel(AttnArgs A) {
     A.out[((size_t)(s.row0 + t) * A.a + kvh * r + c % r) * D + tid] = t < s.act ? f2bf(ns / ds) : (uint16_t)0;
 }
 
+// The same where items have few pieces: a wave a column.
+__global__ __launch_bounds__(kJoinThreads) void join_short_kernel(AttnArgs A) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = A.a / A.g;
+    const int y = blockIdx.x * kJoinWaves + wave;
+    if (y >= A.r.B * A.g * A.cols) return;
+    const int x = y / A.cols, c = y % A.cols, b = x / A.g, kvh = x % A.g;
+    const SeqRows s = seq_rows(A.r, b);
+    const int t = c / r;
+    if (t >= s.n) return;
+    const int w0 = A.cut[x].x, np = A.cut[x].y;
+    if (np == 1) return;                       // written by its wave
+    const size_t step = (size_t)A.cols * PSTRIDE;
+    const float* part = A.part + (size_t)c * PSTRIDE;
+    f32x4 num[1];
+    float den[1];
+    join_halves<1>(np, [&](int i, int) { return part + slot_of(w0, i) * step; }, num, den);
+    u32x2 o = {pack2bf(num[0][0] / den[0], num[0][1] / den[0]), pack2bf(num[0][2] / den[0], num[0][3] / den[0])};
+    if (t >= s.act) o = u32x2{0, 0};
+    if (lane < 32) *(u32x2*)(A.out + ((size_t)(s.row0 + t) * A.a + kvh * r + c % r) * D + 4 * lane) = o;
+}
+
 // Many rows: workgroups for each share, which join the item that it begins and does not end; a wave a pair
 // of columns, with the pieces of both requested together.
 constexpr int kJoinCols = 2 * kJoinWaves;
@@ -919,57 +987,27 @@ __global__ __launch_bounds__(kJoinThreads) void join_many_kernel(AttnArgs A) {
     }
 }
 
-// The same where items have many pieces: half a wave a piece, 8 pieces of both columns requested at a time.
+// The same where items have many pieces.
 __global__ __launch_bounds__(kJoinThreads) void join_long_kernel(AttnArgs A) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, r = A.a / A.g, w0 = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = A.a / A.g, w0 = blockIdx.x;
     const CutItem it = A.cut_many[w0];
     if (it.np == 0) return;
     const int c0 = kJoinCols * blockIdx.y + 2 * wave;
     const int cols = min(A.cols, it.n * r);
     if (c0 >= cols) return;
-    // A column past the item's repeats the last one.
     const size_t step = (size_t)A.cols * PSTRIDE;
-    auto piece = [&](int i, int j) { return A.part + slot_of(w0, i) * step + (size_t)min(c0 + j, cols - 1) * PSTRIDE; };
-    float M[2] = {-INFINITY, -INFINITY}, den[2] = {0.f, 0.f}, wt[2];
-    f32x4 num[2] = {};
-    for (int s0 = 0; s0 < it.np; s0 += 64) {
-        const int k = min(it.np - s0, 64);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            float m = -INFINITY, l = 0.f;
-            if (lane < k) {
-                const float* p = piece(s0 + lane, j);
-                m = p[D];
-                l = p[D + 1];
-            }
-            const float Mn = fmaxf(M[j], wave_max(m)), f = exp2f(M[j] - Mn);
-            wt[j] = exp2f(m - Mn);
-            den[j] = den[j] * f + wave_sum(wt[j] * l);
-            num[j] *= f;
-            M[j] = Mn;
-        }
-        for (int i = 0; i < k; i += 8) {
-            f32x4 v[2][4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)       // a piece past the last weighs nothing
-                    v[j][u] = *(const f32x4*)(piece(s0 + min(i + 2 * u + half, k - 1), j) + 4 * (lane & 31));
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) num[j] += __shfl(wt[j], i + 2 * u + half) * v[j][u];
-        }
-    }
+    f32x4 num[2];
+    float den[2];
+    // A column past the item's repeats the last one.
+    join_halves<2>(it.np, [&](int i, int j) { return A.part + slot_of(w0, i) * step + (size_t)min(c0 + j, cols - 1) * PSTRIDE; }, num,
+                   den);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int c = c0 + j, t = c / r;
         if (c >= cols) break;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) num[j][e] += __shfl_xor(num[j][e], 32);
         u32x2 o = {pack2bf(num[j][0] / den[j], num[j][1] / den[j]), pack2bf(num[j][2] / den[j], num[j][3] / den[j])};
         if (t >= it.act) o = u32x2{0, 0};
-        if (!half) *(u32x2*)(A.out + ((size_t)(it.row + t) * A.a + it.head + c % r) * D + 4 * (lane & 31)) = o;
+        if (lane < 32) *(u32x2*)(A.out + ((size_t)(it.row + t) * A.a + it.head + c % r) * D + 4 * lane) = o;
     }
 }
 
@@ -1040,7 +1078,13 @@ hipError_t attention_fp8(const NewRows& r, int a, int g, const uint16_t* q, cons
         if (A.cols <= 16) launch_few<1>(0, shares, A, st);
         else launch_few<2>(0, shares, A, st);
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        hipLaunchKernelGGL(join_few_kernel, dim3(r.B * g * A.cols), dim3(kJoinThreads), 0, st, A);
+        // Few pieces an item, a wave a column: 14 x 4630 positions, 4 rows, 64 heads on 8, 41 us (four waves a column
+        // 45).  Many, four waves: 30000 positions, 5 heads on 1 (469 pieces) 17 us (one wave 38); 2 x 5000, 32 on 8
+        // (64) 13.3 (15.7).
+        if (shares <= 32 * items)
+            hipLaunchKernelGGL(join_short_kernel, dim3((items * A.cols + kJoinWaves - 1) / kJoinWaves), dim3(kJoinThreads), 0, st, A);
+        else
+            hipLaunchKernelGGL(join_few_kernel, dim3(items * A.cols), dim3(kJoinThreads), 0, st, A);
         return hipGetLastError();
     }
     // Rows of a wave: what its 16 (where they hold a quarter of the longest sequence's rows: 14 sequences of 4630
