@@ -698,3 +698,33 @@ def test_calls_on_another_stream():
         m.kvp_attention_fp8(0, q.data_ptr(), r, out.data_ptr(), ws.data_ptr(), n, st.cuda_stream)
     st.synchronize()
     assert np.array_equal(out.float().cpu().numpy().reshape(-1, 8, D), want)
+
+
+def test_two_streams_at_once():
+    """Calls of one model on two streams with a workspace each, by list and item by item, equal the same calls alone."""
+    c = Case(8, 2, [2500, 64], [3, 40], seed=41)
+    want = _attention(c)
+    dev = c.cache.to_device()
+    m = lr.model8(8, 2, dev, c.cache.n_pages, 2, 200)
+    q = _dev(c.x[:, :8].reshape(c.rows, -1))
+    n = m.kvp_workspace_size(kb.KVP_PHASE_STEP_FP8, 2, c.rows)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    rows = [lr.rows_of(c.lens, c.new, c.table), lr.rows_of(c.lens, c.new, c.table, max_new=200)]
+    ws = [torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda") for _ in streams]
+    out = [[torch.zeros_like(q) for _ in range(8)] for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for k, st in enumerate(streams):
+            m.kvp_attention_fp8(0, q.data_ptr(), rows[k][0], out[k][i].data_ptr(), ws[k].data_ptr(), n, st.cuda_stream)
+    torch.cuda.synchronize()
+    assert np.array_equal(out[0][0].float().cpu().numpy().reshape(-1, 8, D), want)
+    for o in out:
+        _check_attention(c, o[0].float().cpu().numpy().reshape(-1, 8, D))
+        assert all(torch.equal(o[0], x) for x in o)
+
+
+def test_attention_shared_pages():
+    """A prefix's pages in the table rows of two sequences."""
+    c = Case(6, 2, [128, 128, 70], [1, 30, 2], seed=42)
+    c.table[1, :2] = c.table[0, :2]
+    _check_attention(c, _attention(c))
