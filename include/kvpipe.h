@@ -515,9 +515,12 @@ int kvp_append_fp8(kvp_ctx* ctx, int l, const void* q, const void* k, const void
  * pools of tau(l), into out (same shape, bf16): the row at position p sees positions [0, p], which
  * must have been appended, its own among them.  One row a sequence is a decode step, more are
  * proposed tokens or a (part of a) prompt.  Rows of inactive sequences become 0; rows of no
- * sequence are left as they are.  Products on bf16 matrix cores, e4m3 widened exactly, softmax
- * statistics and sums in fp32, its weights rounded to bf16.  Workspace: KVP_PHASE_STEP_FP8 with
- * B and rows.  Errors: as kvp_append_fp8, KVP_E_WORKSPACE.
+ * sequence are left as they are.  Codes are multiplied as they are or widened to bf16, exactly both
+ * ways; the queries in bf16 or, where a sequence and KV head have more than 32 rows x heads, as the
+ * sum of two e4m3 numbers under a power of two for each row and head (off by 2^-19 of its largest
+ * value at most); softmax statistics and sums in fp32, its weights rounded to bf16.  max_new and
+ * max_pos choose between kernels: close bounds are faster.  Workspace: KVP_PHASE_STEP_FP8 with B and
+ * rows.  Errors: as kvp_append_fp8, KVP_E_WORKSPACE.
  */
 int kvp_attention_fp8(kvp_ctx* ctx, int l, const void* q, const kvp_rows* r, void* out, void* ws,
                       size_t ws_bytes, void* stream);
