@@ -517,8 +517,9 @@ int kvp_append_fp8(kvp_ctx* ctx, int l, const void* q, const void* k, const void
  * proposed tokens or a (part of a) prompt.  Rows of inactive sequences become 0; rows of no
  * sequence are left as they are.  Codes are multiplied as they are or widened to bf16, exactly both
  * ways; the queries in bf16 or, where a sequence and KV head have more than 32 rows x heads, as the
- * sum of two e4m3 numbers under a power of two for each row and head (off by 2^-19 of its largest
- * value at most); softmax statistics and sums in fp32, its weights rounded to bf16.  max_new and
+ * sum of two 8-bit numbers under a power of two for each row and head: exactly but for values below
+ * 2^-13 of the row's largest, which are off by 2^-21 of it at most (by 2^-114 where that is more).
+ * Softmax statistics and sums in fp32, its weights rounded to bf16.  max_new and
  * max_pos choose between kernels: close bounds are faster.  Workspace: KVP_PHASE_STEP_FP8 with B and
  * rows.  Errors: as kvp_append_fp8, KVP_E_WORKSPACE.
  */

@@ -574,10 +574,14 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, int b
     return __builtin_amdgcn_make_buffer_rsrc((void*)u, 0, bytes, 0x00020000);
 }
 
-// The queries of a wave's columns as sums of two e4m3 numbers, times a power of two s for each column: 8
-// significant bits in two times 4, exact but for what lies below 2^-19 of the column's largest value.  Scores
-// are then products of 8-bit numbers as they are in memory, K with both halves, at twice the rate of bf16
-// and without widening K.
+// The queries of a wave's columns as sums of an e4m3 and an e5m2 number, times a power of two s for each column: the
+// 8 significant bits of bf16 in 4 and what 4 bits leave.  Scores are then products of 8-bit numbers as they are in
+// memory, K with both halves, at twice the rate of bf16 and without widening K.
+//
+// In units of s the column's largest value lies in (224, 448].  From 2^-6 on hi takes 4 of a value's 8 bits and leaves
+// j units of the last of them, |j| <= 8: 3 bits, a number of e5m2, so that the sum is exact.  Below, hi is a multiple of
+// 2^-9 and leaves 2^-10 at most, of which lo, with 3 bits, misses 2^-14 at most: 2^-21.8 of the column's largest value, or 2^-114
+// where s is 2^-100, its least.  (lo in e4m3 would miss up to 2^-10 there, 2^-17.8 of the largest value.)
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 template <int NB>
 struct Queries8 {
@@ -612,13 +616,16 @@ struct Queries8 {
                         const uint32_t c = e4m3_pack(x0, x1, x2, x3);
                         const f32x2 y0 = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), y1 = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
                         hi[cb][4 * j + 2 * h + i] = (int)c;
-                        lo[cb][4 * j + 2 * h + i] = (int)e4m3_pack(x0 - y0[0], x1 - y0[1], x2 - y1[0], x3 - y1[1]);
+                        const int r = __builtin_amdgcn_cvt_pk_bf8_f32(x0 - y0[0], x1 - y0[1], 0, false);
+                        lo[cb][4 * j + 2 * h + i] = __builtin_amdgcn_cvt_pk_bf8_f32(x2 - y1[0], x3 - y1[1], r, true);
                     }
         }
     }
 };
-__device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+// a in e4m3, b in e4m3 or (B 1) e5m2.
+template <int B>
+__device__ __forceinline__ f32x4 mfma_8bit(i32x8 a, i32x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, B, 0, 0, 0, 0);
 }
 
 // N 16-byte LDS reads at addr (or a0, a1 in turn) + OFF, STEP apart, and their wait: written by hand, since
@@ -749,9 +756,9 @@ __global__ __launch_bounds__(256, NB == 1 ? 4 : 3) void attention_many_kernel(At
                     const u32x4 x = kv[2 * i], y = kv[2 * i + 1];
                     const i32x8 f = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
 #pragma unroll
-                    for (int cb = 0; cb < NB; ++cb) sc[cb][tb0 + i] = mfma_e4m3(f, Q.hi[cb], f32x4{});
+                    for (int cb = 0; cb < NB; ++cb) sc[cb][tb0 + i] = mfma_8bit<0>(f, Q.hi[cb], f32x4{});
 #pragma unroll
-                    for (int cb = 0; cb < NB; ++cb) sc[cb][tb0 + i] = mfma_e4m3(f, Q.lo[cb], sc[cb][tb0 + i]);
+                    for (int cb = 0; cb < NB; ++cb) sc[cb][tb0 + i] = mfma_8bit<1>(f, Q.lo[cb], sc[cb][tb0 + i]);
                 }
             };
             __builtin_amdgcn_s_setprio(1);
