@@ -212,12 +212,21 @@ __device__ __forceinline__ Item find_tile(const AttnArgs& A, Lanes<FEW>& L, uint
     return it;
 }
 
+// Whether the sequences have no more rows together than the call has, as the launch's rule takes it for the bound of the
+// list's 2^31 tiles (of few columns it holds whatever the offsets are).  Exact: rows < 2^23, 384 or more values each.
+__device__ __forceinline__ bool rows_bounded(const NewRows& r) {
+    float n = 0.f;
+    for (int b = threadIdx.x & 63; b < r.B; b += 64) n += (float)seq_rows(r, b).n;
+    return wave_sum(n) <= (float)r.rows;
+}
+
 // A share of the list: where it begins and ends.
 template <bool FEW>
 __device__ __forceinline__ bool take_share(const AttnArgs& A, Split* sp, uint32_t* w, uint32_t* left, Item* it) {
     Lanes<FEW> L;
+    const bool bounded = FEW || rows_bounded(A.r);
     *sp = Split(list_tiles(A, L), gridDim.x);
-    if (blockIdx.x >= sp->W) return false;
+    if (!bounded || blockIdx.x >= sp->W) return false;
     // Shares in one block on one XCD: neighbours read the same K/V head.
     *w = xcd_remap(blockIdx.x, sp->W);
     const uint32_t x = sp->start(*w);

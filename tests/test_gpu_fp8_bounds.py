@@ -1,4 +1,5 @@
-"""The 8-bit attention at the ends of what include/kvpipe.h promises: queries in two 8-bit parts."""
+"""The 8-bit attention at the ends of what include/kvpipe.h promises: queries in two 8-bit parts, row offsets that
+are none."""
 import numpy as np
 import pytest
 import torch
@@ -19,9 +20,9 @@ def _gpu():
     kb.lib()
 
 
-def _attend(q, kv, lens, new, max_new=None):
+def _attend(q, kv, lens, new, pad=0):
     """kvp_attention_fp8 of q [rows][a][128] (bf16 numbers), the rows of sequence b behind lens[b] positions, over the cached
-    kv[b] [2][lens[b] + new[b]][g][128]; the output and the cache's values."""
+    kv[b] [2][lens[b] + new[b]][g][128]; pad: further sequences, with 0 in their row offsets.  The output and the cache's values."""
     a, g = q.shape[1], kv[0].shape[2]
     need = lr.pages_for(lens, new)
     table, n_pages = lr.scattered(need, max(need), 2, 1)
@@ -29,11 +30,13 @@ def _attend(q, kv, lens, new, max_new=None):
     for b, x in enumerate(kv):
         cache.write(table, b, x)
     dev = cache.to_device()
-    m = lr.model8(a, g, dev, n_pages, len(lens), max(q.shape[0], max_new or 1))
-    r, keep = lr.rows_of(lens, new, table, max_new=max_new)
+    m = lr.model8(a, g, dev, n_pages, len(lens) + pad, q.shape[0])
+    r, keep = lr.rows_of(lens + [70] * pad, new + [0] * pad, np.concatenate([table, table[:1].repeat(pad, 0)]))
+    if pad:
+        keep["cu"][-pad:] = 0
     qd = torch.from_numpy(np.ascontiguousarray(q, dtype=np.float32)).to(torch.bfloat16).cuda()
     out = torch.full_like(qd, float("nan"))
-    n = m.kvp_workspace_size(kb.KVP_PHASE_STEP_FP8, len(lens), q.shape[0])
+    n = m.kvp_workspace_size(kb.KVP_PHASE_STEP_FP8, r.B, q.shape[0])
     ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
     m.kvp_attention_fp8(0, qd.data_ptr(), r, out.data_ptr(), ws.data_ptr(), n, torch.cuda.current_stream().cuda_stream)
     torch.cuda.synchronize()
@@ -74,3 +77,38 @@ def test_queries_of_two_parts(T, exact, unit):
     e = np.abs(got - want).max()
     say(f"[two parts] T={T} exact={exact} unit={unit}: off {e:.2e}, allowed {tol.max() + shift:.2e}")
     assert (np.abs(got - want) <= tol + shift).all()
+
+
+def test_decreasing_row_offsets_do_not_overflow_the_list():
+    """Offsets that alternate between 0 and all rows give them to 250 sequences, with more tiles than 32 bits count (a
+    count that wraps let the join read pieces behind the workspace).  The call is the caller's mistake, but it reaches nothing
+    outside its buffers: here it writes nothing."""
+    a, B, rows, stride = 16, 500, 5000, 27527
+    last = 64 * stride - 1
+    k, v, s = lr.Cache(1, 1, garbage=False).to_device()
+    m = lr.model8(a, 1, (k, v, s), 1, B, rows)
+    t = dict(cu=torch.tensor([rows * (b % 2) for b in range(B + 1)], dtype=torch.int32, device="cuda"),
+             len=torch.full((B,), last + 1 - rows, dtype=torch.int32, device="cuda"),
+             pages=torch.zeros(B, stride, dtype=torch.int32, device="cuda"))
+    tiles = (B // 2) * sum((last + 1 - rows + 8 * c + 7) // 64 + 1 for c in range(rows // 8))     # blocks of 8 rows
+    assert 0 < tiles - 2**32 < 10**6
+    r = kb.kvp_rows(t["cu"].data_ptr(), t["len"].data_ptr(), t["pages"].data_ptr(), stride, B, rows, rows, last)
+    q = torch.ones(rows, a * D, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 55.0)
+    n = m.kvp_workspace_size(kb.KVP_PHASE_STEP_FP8, B, rows)
+    ws = torch.full((n + 4096,), 0xEE, dtype=torch.uint8, device="cuda")
+    m.kvp_attention_fp8(0, q.data_ptr(), r, out.data_ptr(), ws.data_ptr(), n, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert (out == 55.0).all() and (ws[n:] == 0xEE).all()
+
+
+def test_offsets_that_end_in_zeros():
+    """Offsets of a padded batch whose unused ends were left 0: those sequences have no rows, in the list too."""
+    rng = np.random.default_rng(3)
+    lens, new = [2500, 64], [3, 40]
+    q = lr.bf16(rng.standard_normal((43, 8, D)).astype(np.float32))
+    kv = [rng.standard_normal((2, n + T, 2, D)) for n, T in zip(lens, new)]
+    got, held = _attend(q, kv, lens, new, pad=4)
+    for b, rows in enumerate((slice(0, 3), slice(3, 43))):
+        want, tol = lr.attention(q[rows].astype(np.float64), held[b], lens[b], 8)
+        assert (np.abs(got[rows] - want) <= tol).all()
