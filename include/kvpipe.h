@@ -519,7 +519,9 @@ int kvp_append_fp8(kvp_ctx* ctx, int l, const void* q, const void* k, const void
  * ways; the queries in bf16 or, where a sequence and KV head have more than 32 rows x heads, as the
  * sum of two 8-bit numbers under a power of two for each row and head: exactly but for values below
  * 2^-13 of the row's largest, which are off by 2^-21 of it at most (by 2^-114 where that is more).
- * Softmax statistics and sums in fp32, its weights rounded to bf16.  max_new and
+ * Softmax statistics and sums in fp32, its weights rounded to bf16.  Range: queries up to 2^112,
+ * largest magnitudes of a query and a key that multiply to at most 2^21 (scores of some 2^24, of
+ * which fp32 keeps units), values up to 2^80; a row past that may be infinite or NaN.  max_new and
  * max_pos choose between kernels: close bounds are faster.  Workspace: KVP_PHASE_STEP_FP8 with B and
  * rows.  Errors: as kvp_append_fp8, KVP_E_WORKSPACE.
  */

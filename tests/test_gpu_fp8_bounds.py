@@ -1,5 +1,5 @@
 """The 8-bit attention at the ends of what include/kvpipe.h promises: queries in two 8-bit parts, row offsets that
-are none."""
+are none, large queries, keys and values."""
 import numpy as np
 import pytest
 import torch
@@ -112,3 +112,47 @@ def test_offsets_that_end_in_zeros():
     for b, rows in enumerate((slice(0, 3), slice(3, 43))):
         want, tol = lr.attention(q[rows].astype(np.float64), held[b], lens[b], 8)
         assert (np.abs(got[rows] - want) <= tol).all()
+
+
+@pytest.mark.parametrize("lens,new", [([150, 0], [3, 5]), ([2100], [4]), ([60, 1], [30, 20]), ([2500], [20])])
+@pytest.mark.parametrize("qexp,kexp", [(112, -91), (10, 11), (-80, 101)])
+def test_largest_queries_keys_and_values(lens, new, qexp, kexp):
+    """Queries, keys and values at the ends of the stated range (few and many columns, one by one and listed): scores so large
+    that one key takes everything, so the output is that key's value, bit for bit."""
+    rng = np.random.default_rng(5)
+    rows = sum(new)
+    q = lr.bf16((rng.uniform(0.5, 0.99, (rows, 4, D)) * rng.choice([-1, 1], (rows, 4, D))).astype(np.float32)) * 2.0**qexp
+    kv = []
+    for n, T in zip(lens, new):
+        x = rng.uniform(-1, 1, (2, n + T, 1, D))
+        x[:, ::7, :, ::5] = 1.0
+        kv.append(x * np.array([2.0**kexp, 2.0**80])[:, None, None, None])
+    got, held = _attend(q, kv, lens, new)
+    r0 = checked = 0
+    for x, n, T in zip(held, lens, new):
+        for t in range(T):
+            s = q[r0 + t] @ x[0, : n + t + 1, 0].T / np.sqrt(D)
+            top = np.argsort(-s, 1)[:, :2]
+            mag = (np.abs(q[r0 + t]) @ np.abs(x[0, : n + t + 1, 0]).T).max() / np.sqrt(D)
+            for h in range(4):
+                # The 32-bit sums of two scores are off by 2 (D + 8) 2^-24 of their magnitudes at most; a weight of e^-60 is
+                # below half a step of every value it is added to.
+                if n + t and s[h, top[h, 0]] - s[h, top[h, 1]] < 2 * (D + 8) * 2.0**-24 * mag + 60:
+                    continue
+                checked += 1
+                assert np.array_equal(got[r0 + t, h].astype(np.float64), x[1, top[h, 0], 0]), (r0 + t, h)
+        r0 += T
+    assert np.isfinite(got).all() and checked >= 2 * rows
+
+
+@pytest.mark.parametrize("lens,new", [([977], [1]), ([3000], [1]), ([70, 300], [12, 40]), ([3000, 5], [12, 3])])
+def test_large_values_under_ordinary_weights(lens, new):
+    rng = np.random.default_rng(6)
+    q = lr.bf16(rng.standard_normal((sum(new), 8, D)).astype(np.float32))
+    kv = [rng.uniform(-1, 1, (2, n + T, 2, D)) * np.array([1.0, 2.0**80])[:, None, None, None] for n, T in zip(lens, new)]
+    got, held = _attend(q, kv, lens, new)
+    cu = np.cumsum([0] + new)
+    for b, n in enumerate(lens):
+        rows = slice(cu[b], cu[b + 1])
+        want, tol = lr.attention(q[rows].astype(np.float64), held[b], n, 8)
+        assert (np.abs(got[rows] - want) <= tol).all(), b
