@@ -1,4 +1,5 @@
-"""Calls on 8-bit pages beside each other: different launches at once on streams of one model."""
+"""Calls on 8-bit pages beside each other: different launches at once on streams of one model, and what a prompt at once and
+in chunks leaves in the cache."""
 import numpy as np
 import pytest
 import torch
@@ -6,7 +7,7 @@ import torch
 import lowbit_ref as lr
 from gpu_util import say
 from paper_2608_15943_amd import binding as kb
-from test_gpu_fp8_cache import Case, _dev
+from test_gpu_fp8_cache import Case, Stack, _dev, _normal
 
 pytestmark = pytest.mark.gpu
 D = lr.D
@@ -64,3 +65,52 @@ def test_every_launch_at_once_on_streams_of_one_model():
     torch.cuda.synchronize()
     for a, o in zip(alone, outs):
         assert all(torch.equal(a, x) for x in o)
+
+
+def _held(s, l, n):
+    """[2][n][g][128] values and [2][n][g] scales of sequence 0 in layer l's pools."""
+    c = lr.Cache(s.g, 1).from_device(s.dev[l])
+    pos = np.arange(n)
+    page, blk = s.table[0][pos // lr.PAGE], pos % lr.PAGE // lr.BLK
+    return c.values(s.table, 0, n), np.stack([c.s[:, page, z, blk].T for z in range(2)]).astype(np.float64)
+
+
+@pytest.mark.parametrize("rows,chunks", [(64, (0, 16, 48, 64)), (61, (0, 13, 40, 61)), (70, (0, 16, 48, 70))])
+def test_prompt_at_once_and_in_chunks_fill_the_cache_alike(rows, chunks):
+    """Up to 64 rows the projections stay in 32 bits until a value is rounded to its code, so layer 0's caches differ where
+    another order of sums (or, of chunks that begin inside a block, a scale that grew on the way) tips a rounding; past 64 rows
+    the prompt's are rounded to bf16 in between.  Layer 1 gets what differs in layer 0's outputs, which stacks of that layer
+    alone show."""
+    rng = np.random.default_rng(45)
+    x = _normal(rng, rows, 512)
+
+    def runs(tau):
+        one, two = Stack(4, 2, tau, 1, 4, seed=46), Stack(4, 2, tau, 1, 4, seed=46)
+        y1 = one.step(x, [0], [rows])
+        y2 = np.concatenate([two.step(x[lo:hi], [lo], [hi - lo]) for lo, hi in zip(chunks, chunks[1:])])
+        return one, two, y1, y2
+
+    one, two, _, _ = runs((0, 1))
+    alone, _, y1, y2 = runs((0,))
+    assert all(np.array_equal(alone.w[0][k], one.w[0][k]) for k in "qkvo") and np.array_equal(alone.table, one.table)
+    for l, (inp, diff) in enumerate(((x, np.zeros_like(x)), (y1, np.abs(y1 - y2)))):
+        (v1, s1), (v2, s2) = _held(one, l, rows), _held(two, l, rows)
+        assert np.isfinite(v1).all() and np.isfinite(v2).all()
+        assert (np.maximum(s1, s2) / np.minimum(s1, s2) <= 2).all()
+        # The values before their codes, [2][rows][g][128]: the inputs' differences times the weights, another order of 512
+        # products (2 x 512 x 2^-24 of their magnitudes), 2^-8 of them where they are rounded to bf16; a rotation adds a pair's.
+        delta = np.zeros((2, rows, 2, D))
+        for z, k in enumerate("kv"):
+            w = one.w[l][k].T
+            moved, mag = diff @ np.abs(w), np.abs(inp) @ np.abs(w)
+            rounded = 2.0**-8 * (np.abs(inp @ w) + moved + 2.0**-14 * mag) if rows > 64 else 0
+            delta[z] = (moved + 2.0**-14 * mag + rounded).reshape(rows, 2, D)
+        delta[0] += np.roll(delta[0], D // 2, -1)
+        # Codes: half a step each, 2^-4 of the value or 2^-10 of the scale; a scale that grows rounds the earlier ones again.
+        top, s = np.maximum(np.abs(v1), np.abs(v2)), np.maximum(s1, s2)[..., None]
+        tol = delta + 3 * np.maximum(2.0**-4 * 1.1 * top, 2.0**-10 * s)
+        e = np.abs(v1 - v2)
+        say(f"[chunks] rows={rows} layer {l}: {(e > 0).mean():.4f} of the values differ, {(e / tol).max():.3f} of what may be")
+        assert (e <= tol).all(), l
+        if l == 0 and rows == 64:      # chunks end at block ends: another order of sums alone
+            assert (e > 0).mean() <= 0.01
