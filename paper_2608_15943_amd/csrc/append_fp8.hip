@@ -32,7 +32,8 @@ __device__ __forceinline__ uint32_t wave_maxu(uint32_t v) {
     return step(q[0], q[1]);
 }
 
-// Turns of a position at frequency i, to some 2^-100.
+// Turns of a position at frequency i, to some 2^-61 of them: the host's factors have 64 bits, the products here keep
+// them.  At the farthest position, 2^30, that is 2^-33 of a turn, below half a step of the cosine in fp32.
 struct Turns {
     double hi, lo;
     __device__ __forceinline__ Turns(const RopeFreqs& th, int i) : hi(th.hi[0]), lo(th.lo[0]) {

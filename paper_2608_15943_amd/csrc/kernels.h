@@ -193,8 +193,8 @@ struct NewRows {
     const int32_t* pt;
     int stride, n_pages, B, rows, max_new, max_pos;
 };
-// Turns of a position, base^(-2i / 128) / (2 pi) for i = 0 .. 63, as factors: hi + lo of index 0 is 1 / (2 pi), of
-// index 1 + j base^(-2^(j + 1) / 128), which i has where its bit j is set.
+// Turns of a position, base^(-2i / 128) / (2 pi) for i = 0 .. 63, as factors of 64 bits in two doubles: hi + lo of index 0
+// is 1 / (2 pi), of index 1 + j base^(-2^(j + 1) / 128), which i has where its bit j is set.
 struct RopeFreqs {
     double hi[7], lo[7];
 };

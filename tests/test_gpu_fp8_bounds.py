@@ -1,5 +1,7 @@
 """The 8-bit attention at the ends of what include/kvpipe.h promises: queries in two 8-bit parts, row offsets that
-are none, large queries, keys and values."""
+are none, large queries, keys and values, far positions."""
+import decimal
+
 import numpy as np
 import pytest
 import torch
@@ -156,3 +158,47 @@ def test_large_values_under_ordinary_weights(lens, new):
         rows = slice(cu[b], cu[b + 1])
         want, tol = lr.attention(q[rows].astype(np.float64), held[b], n, 8)
         assert (np.abs(got[rows] - want) <= tol).all(), b
+
+
+def _exact_rotation(pos, base):
+    """Cosines and sines of pos base^(-2i / 128), i = 0 .. 63, the whole turns taken off with 60 digits."""
+    decimal.getcontext().prec = 60
+    two_pi = 2 * decimal.Decimal("3.14159265358979323846264338327950288419716939937510582097494")
+    ln = decimal.Decimal(repr(base)).ln()
+    t = [decimal.Decimal(pos) * (-ln * i / 64).exp() / two_pi for i in range(D // 2)]
+    ang = np.array([float((x - x.to_integral_value()) * two_pi) for x in t])
+    return np.cos(ang), np.sin(ang)
+
+
+@pytest.mark.parametrize("base", [10000.0, 500000.0, 17.5])
+def test_rotation_at_the_farthest_positions(base):
+    """Angles of the last positions that a page table may reach are right to the rounding of what is rotated."""
+    stride = (1 << 24) - 1
+    n = 64 * stride - 5
+    table = torch.full((1, stride), -1, dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    before = lr.Cache(1, 2, 7, garbage=False)
+    dev = before.to_device()
+    m = lr.model8(1, 1, dev, 2, 1, 5, base=base)
+    t = dict(cu=torch.tensor([0, 5], dtype=torch.int32, device="cuda"), len=torch.tensor([n], dtype=torch.int32, device="cuda"))
+    r = kb.kvp_rows(t["cu"].data_ptr(), t["len"].data_ptr(), table.data_ptr(), stride, 1, 5, 5, n + 4)
+    x = lr.bf16(np.random.default_rng(8).standard_normal((5, 3, D)).astype(np.float32))
+    x[0, 0, : D // 2], x[0, 0, D // 2:] = 1, 0          # the cosines and sines themselves
+    xd = torch.from_numpy(x).to(torch.bfloat16).cuda()
+    q = torch.empty(5, D, dtype=torch.bfloat16, device="cuda")
+    p = xd.data_ptr()
+    m.kvp_append_fp8(0, p, p + 2 * D, p + 4 * D, 3 * D, r, q.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    want = np.zeros((2, 5, D))
+    for j in range(5):
+        c, s = _exact_rotation(n + j, base)
+        a, b = x[j, :2, : D // 2].astype(np.float64), x[j, :2, D // 2:].astype(np.float64)
+        want[:, j] = np.concatenate([a * c - b * s, b * c + a * s], -1)
+    got = q.float().cpu().numpy()
+    # Half a step of bf16, and 2^-22 of the pair for cosine, sine and products in 32 bits.
+    assert (np.abs(got - want[0]) <= 2.0**-8 * np.abs(want[0]) + 2.0**-22 * 2 * np.abs(x[:, 0]).max()).all()
+    after = before.from_device(dev)
+    s = float(after.s[0, 1, 0, 3])
+    assert s == max(1.0, lr.scale_of(np.abs(want[1]).max()))
+    k = lr.E4M3[after.k[0, 1, 59:64]] * s
+    assert (np.abs(k - want[1]) <= np.maximum(2.0**-4 * np.abs(want[1]), 2.0**-10 * s) + 2.0**-22 * 2 * np.abs(x[:, 1]).max()).all()
