@@ -9,8 +9,8 @@
 // one wave ever touches a block and head, so nothing is shared between waves and the result does
 // not depend on the order in which they run.
 //
-// Bound by memory: prompts of 4 x 4096 rows (16 query heads, 8 K/V heads, 235 MB) 56 us, 4.2 TB/s; 2560 rows in
-// 7 chunks (64, 8; 100 MB) 26.8 us; one row of each of 64 sequences 3.8 us, the latency of three loads that
+// Bound by memory: prompts of 4 x 4096 rows (16 query heads, 8 K/V heads, 235 MB) 57 us, 4.1 TB/s; 2568 rows in
+// 7 chunks (64, 8; 100 MB) 26.9 us; one row of each of 64 sequences 4.2 us, the latency of three loads that
 // depend on each other (length, page, scale).
 #include "fp8_cache.h"
 

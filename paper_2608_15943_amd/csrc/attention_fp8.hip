@@ -11,14 +11,16 @@
 //                the run that the second product sums over.  The K scale multiplies a lane's
 //                scores, one factor for all of them.
 //   O^T += V^T P^T  The V scale, a power of two, goes into the exponent of P before P is rounded to
-//                bf16 (8 bits); the sum of the weights is taken from the rounded P, so that its
-//                rounding cancels where it is common.
+//                bf16 (8 bits), the type of the product beside V's codes; the sum of the weights is
+//                taken from the rounded P, so that its rounding cancels where it is common.  It
+//                leaves 0.0021-0.0024 of the output's scale as the error against 64 bits, where the
+//                output's own rounding is 0.0016-0.0017.
 //
 // attention_few_kernel: sequences with at most 32 columns (single tokens, a few proposed ones); K and V go straight
 // to registers.  Bound by reading the cache: 64 x 32768 positions (32 heads on 8, 4.3 GB) 707 us, 6.1 TB/s; 8 x
-// 64K-128K 276 us, 5.8 TB/s.  attention_many_kernel: more columns; four waves share each tile through LDS.  Bound by
-// the vector instructions (widening, softmax) beside the matrix ones: prompts of 4 x 4096 rows (16 heads on 8) 265-270 us,
-// 1018-1037 TFLOP/s.
+// 64K-128K 276 us, 5.9 TB/s.  attention_many_kernel: more columns; four waves share each tile through LDS.  Bound by
+// the vector instructions (widening, softmax) beside the matrix ones: prompts of 4 x 4096 rows (16 heads on 8) 263 us,
+// 1045 TFLOP/s, once the clock has risen (330 us in the first 20 calls).
 //
 // Work: the tiles of all items (a sequence's block of rows and a K/V head) in one list, in the order
 // (sequence, K/V head, block, tile), which the waves (workgroups) share evenly: an item that begins

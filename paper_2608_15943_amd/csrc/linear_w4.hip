@@ -13,8 +13,10 @@
 // cores with fp32 sums; the group's scale multiplies the fp32 sum of its inputs.
 //
 // Bound: few rows by reading the weights, in the time that a launch with cold weights allows (1 row, 6144 x 4096,
-// 13 MB: 5.3 us, a bare read of as much 3.2; 14000 x 11008, 80 MB: 15.4 us, a bare read 12.5); more rows also by what
-// every CU reads of x (16 rows, 8192 x 8192: 9.3 us, 36 MB of weights 6.6; 64 rows: 19.0 us, 1 MB of x a CU through LDS).
+// 13 MB: 5.5 us, a bare read of as much 3.2; 14000 x 11008, 80 MB: 15.4 us, a bare read 12.5); more rows also by what
+// every CU reads of x (16 rows, 8192 x 8192: 9.4 us, 36 MB of weights 6.6), and 33 to 64 by waiting for it: LDS holds
+// one stage, so that the products stand still while the next comes (64 rows 19.6 us).  Each further 64 rows read and
+// widen the weights again (128 rows 29 us, 4096 795).
 #include "common.h"
 #include "kernels.h"
 
