@@ -202,3 +202,23 @@ def test_rotation_at_the_farthest_positions(base):
     assert s == max(1.0, lr.scale_of(np.abs(want[1]).max()))
     k = lr.E4M3[after.k[0, 1, 59:64]] * s
     assert (np.abs(k - want[1]) <= np.maximum(2.0**-4 * np.abs(want[1]), 2.0**-10 * s) + 2.0**-22 * 2 * np.abs(x[:, 1]).max()).all()
+
+
+@pytest.mark.parametrize("lens,new", [([300, 5], [1, 1]), ([3000, 70], [3, 2]), ([60, 1], [30, 20]), ([2500], [20])])
+def test_queries_that_are_not_finite_stay_apart(lens, new):
+    """A row and head whose query is NaN or infinite comes out NaN; every other is right."""
+    rng = np.random.default_rng(9)
+    rows = sum(new)
+    q = lr.bf16(rng.standard_normal((rows, 8, D)).astype(np.float32))
+    kv = [rng.standard_normal((2, n + T, 2, D)) for n, T in zip(lens, new)]
+    bad = np.zeros((rows, 8), bool)
+    for t, h, x in ((0, 3, np.nan), (rows - 1, 0, np.inf), (rows - 1, 6, -np.inf)):
+        bad[t, h], q[t, h, 17] = True, x
+    got, held = _attend(q, kv, lens, new)
+    assert np.isnan(got[bad]).all()
+    cu = np.cumsum([0] + new)
+    for b, n in enumerate(lens):
+        r = slice(cu[b], cu[b + 1])
+        ok = ~bad[r]
+        want, tol = lr.attention(np.where(bad[r][..., None], 0, q[r]).astype(np.float64), held[b], n, 8)
+        assert (np.abs(got[r] - want) <= tol)[ok].all(), b

@@ -1,5 +1,5 @@
-"""Calls on 8-bit pages beside each other: different launches at once on streams of one model, and what a prompt at once and
-in chunks leaves in the cache."""
+"""Calls on 8-bit pages beside each other: different launches at once on streams of one model, graphs that share a workspace,
+and what a prompt at once and in chunks leaves in the cache."""
 import numpy as np
 import pytest
 import torch
@@ -114,3 +114,48 @@ def test_prompt_at_once_and_in_chunks_fill_the_cache_alike(rows, chunks):
         assert (e <= tol).all(), l
         if l == 0 and rows == 64:      # chunks end at block ends: another order of sums alone
             assert (e > 0).mean() <= 0.01
+
+
+def test_two_graphs_share_a_workspace():
+    """Two captured steps on one workspace, one of single tokens and one of chunks, replayed in turn and between eager calls:
+    each leaves the outputs and caches of the same eager call."""
+    s = Stack(4, 2, (0, 0), 3, 8, seed=47)
+    rng = np.random.default_rng(48)
+    s.step(_normal(rng, 140, s.h), [0, 0, 0], [30, 100, 10])
+    start = {l: [t.clone() for t in d] for l, d in s.dev.items()}
+    calls = [([30, 100, 10], [1, 1, 1]), ([30, 100, 10], [40, 3, 29])]
+    n = max(s.m.kvp_workspace_size(kb.KVP_PHASE_STEP_FP8, 3, sum(t)) for _, t in calls)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    state = []
+    for lens, new in calls:
+        r, keep = lr.rows_of(lens, new, s.table)
+        x = _dev(_normal(rng, sum(new), s.h))
+        state.append((r, keep, x, torch.empty_like(x)))
+
+    def run(i):
+        r, _, x, y = state[i]
+        s.m.kvp_step_fp8(x.data_ptr(), r, y.data_ptr(), ws.data_ptr(), n, torch.cuda.current_stream().cuda_stream)
+
+    def result(f, i):
+        for l, d in s.dev.items():
+            for t, u in zip(d, start[l]):
+                t.copy_(u)
+        state[i][3].fill_(float("nan"))
+        f()
+        torch.cuda.synchronize()
+        return state[i][3].clone(), [t.clone() for d in s.dev.values() for t in d]
+
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        run(0), run(1)
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in calls]
+    for i, g in enumerate(graphs):
+        with torch.cuda.graph(g):
+            run(i)
+    for rep in range(3):
+        for i, g in enumerate(graphs):
+            state[i][2].copy_(_dev(_normal(rng, sum(calls[i][1]), s.h)))
+            want, got = result(lambda: run(i), i), result(g.replay, i)
+            assert torch.isfinite(want[0]).all() and torch.equal(want[0], got[0]), (rep, i)
+            assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(want[1], got[1])), (rep, i)
