@@ -89,6 +89,7 @@ extern "C" {
 #define KVP_PHASE_DECODE    1
 #define KVP_PHASE_BACKWARD  2  /* workspace of kvp_backward (kvp_workspace_size only) */
 #define KVP_PHASE_STEP_FP8  3  /* workspace of kvp_step_fp8, kvp_attention_fp8 (likewise) */
+#define KVP_PHASE_STEP      4  /* workspace of kvp_step, kvp_attention (likewise)        */
 
 #define KVP_STOP_FIR_MET        0  /* FIR <= 1 + eps                                    */
 #define KVP_STOP_BUDGET         1  /* m conversions made                                */
@@ -290,7 +291,7 @@ int kvp_set_kv_slot(kvp_ctx* ctx, int l, void* K, void* V);
 /*
  * kvp_workspace_size -- bytes of device scratch that a call with this phase,
  * batch B and length S (prefill, backward; ignored for decode) needs.  For
- * KVP_PHASE_STEP_FP8 S is the number of rows of the whole call (kvp_rows.rows, at most
+ * KVP_PHASE_STEP and KVP_PHASE_STEP_FP8 S is the number of rows of the whole call (kvp_rows.rows, at most
  * max_batch * max_seq).  The
  * workspace holds Q, the attention output, the fp32 residual stream and its
  * bf16 copy, the RoPE table (prefill) and split-K partial results (decode);
@@ -301,7 +302,7 @@ int kvp_set_kv_slot(kvp_ctx* ctx, int l, void* K, void* V);
  * shrinks as B or S grows: a workspace sized for max_batch and max_seq serves
  * every call of its phase.
  * Errors: KVP_E_INVALID_ARG, KVP_E_CAPACITY (B > max_batch, S > max_seq), KVP_E_SHAPE
- * (KVP_PHASE_STEP_FP8 of an fp32 model).
+ * (KVP_PHASE_STEP and KVP_PHASE_STEP_FP8 of an fp32 model).
  */
 int kvp_workspace_size(const kvp_ctx* ctx, int phase, int B, int S, size_t* bytes);
 
@@ -428,6 +429,32 @@ int kvp_decode_step_paged(kvp_ctx* ctx, const void* x, const int32_t* len_dev, i
  *   kvp_pager_release  -- return all of seq's pages.
  *   kvp_pager_rows     -- copy the rows of seqs[0..B) to out [B][max_pages_per_seq]
  *                         (host memory; the caller copies it to the device).
+ *
+ * Several sequences may hold one page; it is free when the last of them lets go of it.
+ *   kvp_pager_fork     -- sequence `to`, which holds none, gets the pages of `from` that hold
+ *                         positions [0, n_tokens): the same pages, nothing is copied.
+ *                         KVP_E_STATE where `to` holds pages, KVP_E_CAPACITY where `from` has
+ *                         no pages for so many tokens.
+ *   kvp_pager_own      -- before rows are appended at positions [from, to) of seq: every page
+ *                         there that another sequence holds too is replaced, in seq's row, by a
+ *                         free one.  src[i], dst[i], i < *n: the page it was and the page it
+ *                         is now; the caller copies them (kvp_copy_pages, kvp_copy_pages_fp8) before
+ *                         the append.  Positions without a page are left out (reserve them first).
+ *                         All or nothing: KVP_E_CAPACITY when the pool has too few free pages or
+ *                         more than max_pairs would have to be copied (*n = 0, nothing changes).
+ *   kvp_pager_trim     -- lets go of the pages of seq that lie wholly in positions [from, to):
+ *                         their entries become -1, the row's end stays where it is; to <= from
+ *                         does nothing.  With an attention window, rows from position p on
+ *                         see nothing in [sinks, p - window + 1).
+ *   kvp_pager_compact  -- moves pages that are held so that they come to lie in front of all
+ *                         free ones, at most max_pairs in this call: rows then hold the new
+ *                         pages, and the caller copies src[i] to dst[i], i < *n, before it
+ *                         uses them (no page is both a source and a target, so one call of
+ *                         kvp_copy_pages does).  *n < max_pairs: done, all held pages are below
+ *                         n_pages - (free pages); free ones are handed out lowest first.
+ * Copies and appends that the caller enqueues on one stream, in the order of these calls, see
+ * each page as it should be.  Errors otherwise: KVP_E_INVALID_ARG; kvp_pager_create also
+ * KVP_E_CAPACITY (out of host memory).
  * Host memory only; not thread-safe (one pager per thread).
  */
 typedef struct kvp_pager kvp_pager;
@@ -437,41 +464,22 @@ int kvp_pager_reserve(kvp_pager* p, int seq, int n_tokens);
 int kvp_pager_release(kvp_pager* p, int seq);
 int kvp_pager_free_pages(const kvp_pager* p, int* n);
 int kvp_pager_rows(const kvp_pager* p, const int32_t* seqs, int B, int32_t* out);
+int kvp_pager_fork(kvp_pager* p, int from, int to, int n_tokens);
+int kvp_pager_own(kvp_pager* p, int seq, int from, int to, int32_t* src, int32_t* dst, int max_pairs, int* n);
+int kvp_pager_trim(kvp_pager* p, int seq, int from, int to);
+int kvp_pager_compact(kvp_pager* p, int32_t* src, int32_t* dst, int max_pairs, int* n);
 
-/* ======================================================================== */
-/* 8-bit paged K/V storage                                                    */
-/* ======================================================================== */
 /*
- * Decode over a long context takes the time of reading the cache (Sec. 4); sharing saves
- * capacity, not those bytes, since every layer still reads its producer's K/V.  Held in 8 bits,
- * a pool takes half the bytes of kvp_set_kv_pool's, in capacity and in every read.
- *
- * A value is code * scale.  Codes are e4m3 numbers (OCP: 1 sign, 4 exponent, 3 mantissa bits,
- * largest 448), scales fp32 powers of two, one for each block of 16 positions (16 j ..
- * 16 j + 15 of a sequence) and KV head, for K and for V.  Page layout, producer l's head-major
- * pools (bytes), n_pages pages of 64 positions:
- *     K      [g][n_pages][64][128]         post-RoPE keys
- *     V      [g][n_pages][4][128][16]      16 positions of one dimension side by side
- *     scales [g][n_pages][2][4] fp32       K's then V's, one for each 16 positions
- * The page table and the host page allocator are those of kvp_set_kv_pool's pools.
- *
- * Scale of a block: with f(m) = the least power of two s with m <= 448 s, at least 2^-100, and m
- * the largest magnitude among the values that a call appends to the block, the scale becomes f(m)
- * where the call fills the block from its first position on, and else the larger of f(m) and the
- * scale it had; the codes that the block held before the call are then rounded to the larger
- * scale.  New codes are the nearest to value / scale, ties to even.  If a value is infinite or
- * NaN, the block's scale becomes NaN and its codes 0 (all 16 positions read as NaN) until the
- * block is filled again from its first position.
+ * kvp_copy_pages, kvp_copy_pages_fp8 -- copies page src[i] to page dst[i], i < n, in the pools of
+ * every producer that has any: those of kvp_set_kv_pool, or of kvp_set_kv_pool_fp8 (codes and
+ * scales).  src, dst: device int32 [n], not read on the host; a pair with an index outside a
+ * producer's pool (-1, say, in a list that is filled up) is left out there.  A page may be the
+ * source of several pairs; one that is the target of several, or of one and the source of
+ * another, ends up with undefined contents.  n 0 does nothing.
+ * Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE (fp32 model), KVP_E_STATE (no such pools set), KVP_E_HIP.
  */
-
-/* kvp_set_kv_pool_fp8 -- producer l's pools and scales (device, caller-owned, 16-byte
- * aligned), n_pages pages each.  Independent of the pools of kvp_set_kv_pool.
- * Errors: KVP_E_INVALID_ARG (NULL, n_pages < 1, l not a producer), KVP_E_SHAPE (fp32 model). */
-int kvp_set_kv_pool_fp8(kvp_ctx* ctx, int l, void* K, void* V, void* scales, int n_pages);
-
-/* kvp_page_bytes_fp8 -- bytes of one page (K, V and scales) in one producer's pools:
- * g (2 * 64 * d_h + 32).  Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE. */
-int kvp_page_bytes_fp8(const kvp_ctx* ctx, size_t* bytes);
+int kvp_copy_pages(kvp_ctx* ctx, const int32_t* src, const int32_t* dst, int n, void* stream);
+int kvp_copy_pages_fp8(kvp_ctx* ctx, const int32_t* src, const int32_t* dst, int n, void* stream);
 
 /*
  * New rows of a call, for B sequences.  Sequence b owns rows cu[b] .. cu[b + 1] - 1 of the call's
@@ -494,6 +502,97 @@ typedef struct kvp_rows {
     int32_t max_new;        /* most rows of a sequence, <= max_seq (cu NULL: 1)              */
     int32_t max_pos;        /* last position of any row, < 64 * pages_stride                 */
 } kvp_rows;
+
+/*
+ * kvp_append -- appends rows of keys and values to producer l's pools (kvp_set_kv_pool), rotated
+ * to their positions on the way, and rotates the call's queries beside them.  q, k, v are bf16
+ * before RoPE: rows of a * d_h, g * d_h, g * d_h values, ld values apart (the parts of one fused
+ * projection, say; ld % 8 == 0, 16-byte aligned).  q_out [rows][a * d_h] receives the rotated
+ * queries in bf16 (q_out == q with ld == a * d_h rotates in place).  Angles are evaluated in double, the rotation in
+ * fp32, rounded once.  q with q_out, or k with v, may be NULL together; a consumer's k and v must
+ * be (it rotates queries only).  Rows of no sequence and of inactive ones are left as they are in
+ * q_out, positions that are not appended as they are in the pools.
+ * Errors: KVP_E_INVALID_ARG, KVP_E_CAPACITY, KVP_E_SHAPE, KVP_E_STATE (pools never set), KVP_E_HIP.
+ */
+int kvp_append(kvp_ctx* ctx, int l, const void* q, const void* k, const void* v, int ld,
+               const kvp_rows* r, void* q_out, void* stream);
+
+/*
+ * kvp_set_layer_window -- layer l's rows see, of the positions [0, p] up to their own, the last
+ * `window` (those above p - window, their own among them) and those below `sinks`: the first
+ * tokens, which stay visible.  window >= 1, sinks >= 0; both 0 take the window off again (the
+ * state of a new context).  A consumer's window is its own, not its producer's.  kvp_attention and
+ * kvp_step apply it; pages that no row of a call sees are not read and need not be mapped
+ * (kvp_pager_trim).  The calls that attend to everything (prefill, layer forward and decode steps on
+ * slots or pages, training, the 8-bit attention and step) refuse a layer with a window: KVP_E_STATE.
+ * Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE (fp32 model).
+ */
+int kvp_set_layer_window(kvp_ctx* ctx, int l, int window, int sinks);
+
+/*
+ * kvp_attention -- attention of the rows of q [rows][a * d_h] (bf16, rotated) over the pools of
+ * tau(l), into out (same shape, bf16): the row at position p sees positions [0, p], or those of
+ * them in the layer's window, which must have been appended, its own among them.  One row a
+ * sequence is a decode step, more are proposed tokens or a (part of a) prompt.  Rows of inactive
+ * sequences become 0; rows of no sequence are left as they are.  Products of bf16 numbers, softmax
+ * statistics and sums in fp32, the weights rounded to bf16 (their sum is that of the rounded
+ * ones).  What a position holds that a row does not see, infinities and NaN too, does not reach the
+ * row; a value that is not finite makes that dimension NaN or infinite in the rows that see it, a key
+ * that is not finite their whole row NaN where its score is +infinity or NaN.  max_new and max_pos choose between
+ * kernels: close bounds are faster.  Workspace: KVP_PHASE_STEP with B and rows.
+ * Errors: as kvp_append, KVP_E_WORKSPACE.
+ */
+int kvp_attention(kvp_ctx* ctx, int l, const void* q, const kvp_rows* r, void* out, void* ws,
+                  size_t ws_bytes, void* stream);
+
+/*
+ * kvp_step -- rows of new tokens through all L layers on the pools: x [rows][h] to
+ * y [rows][h], for each layer projection, kvp_append, kvp_attention and output projection
+ * with the residual, as kvp_decode_step_paged (cu NULL) or kvp_prefill_paged (len 0) do, and
+ * whatever lies between: chunks of prompts beside single tokens, proposed tokens, layers with
+ * windows.  Layers with 4-bit weights (kvp_set_layer_w4) run on those.  Up to 64 rows the
+ * projections stay in fp32 up to the rotation; more are rounded to bf16 before it.  Rows of no
+ * sequence and of inactive ones pass through (y = x).  Workspace: KVP_PHASE_STEP.  Errors: as
+ * kvp_attention.
+ */
+int kvp_step(kvp_ctx* ctx, const void* x, const kvp_rows* r, void* y, void* ws, size_t ws_bytes,
+             void* stream);
+
+/* ======================================================================== */
+/* 8-bit paged K/V storage                                                    */
+/* ======================================================================== */
+/*
+ * Decode over a long context takes the time of reading the cache (Sec. 4); sharing saves
+ * capacity, not those bytes, since every layer still reads its producer's K/V.  Held in 8 bits,
+ * a pool takes half the bytes of kvp_set_kv_pool's, in capacity and in every read.
+ *
+ * A value is code * scale.  Codes are e4m3 numbers (OCP: 1 sign, 4 exponent, 3 mantissa bits,
+ * largest 448), scales fp32 powers of two, one for each block of 16 positions (16 j ..
+ * 16 j + 15 of a sequence) and KV head, for K and for V.  Page layout, producer l's head-major
+ * pools (bytes), n_pages pages of 64 positions:
+ *     K      [g][n_pages][64][128]         post-RoPE keys
+ *     V      [g][n_pages][4][128][16]      16 positions of one dimension side by side
+ *     scales [g][n_pages][2][4] fp32       K's then V's, one for each 16 positions
+ * The page table, the host page allocator and the rows of a call (kvp_rows) are those of
+ * kvp_set_kv_pool's pools.
+ *
+ * Scale of a block: with f(m) = the least power of two s with m <= 448 s, at least 2^-100, and m
+ * the largest magnitude among the values that a call appends to the block, the scale becomes f(m)
+ * where the call fills the block from its first position on, and else the larger of f(m) and the
+ * scale it had; the codes that the block held before the call are then rounded to the larger
+ * scale.  New codes are the nearest to value / scale, ties to even.  If a value is infinite or
+ * NaN, the block's scale becomes NaN and its codes 0 (all 16 positions read as NaN) until the
+ * block is filled again from its first position.
+ */
+
+/* kvp_set_kv_pool_fp8 -- producer l's pools and scales (device, caller-owned, 16-byte
+ * aligned), n_pages pages each.  Independent of the pools of kvp_set_kv_pool.
+ * Errors: KVP_E_INVALID_ARG (NULL, n_pages < 1, l not a producer), KVP_E_SHAPE (fp32 model). */
+int kvp_set_kv_pool_fp8(kvp_ctx* ctx, int l, void* K, void* V, void* scales, int n_pages);
+
+/* kvp_page_bytes_fp8 -- bytes of one page (K, V and scales) in one producer's pools:
+ * g (2 * 64 * d_h + 32).  Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE. */
+int kvp_page_bytes_fp8(const kvp_ctx* ctx, size_t* bytes);
 
 /*
  * kvp_append_fp8 -- appends rows of keys and values to producer l's 8-bit pools, rotated to
@@ -574,7 +673,7 @@ int kvp_linear_w4(const void* x, const void* packed, const void* res, void* y, i
 
 /*
  * kvp_set_layer_w4 -- packed weights of layer l, shapes as kvp_set_layer's: the decode steps
- * (kvp_decode_step and its _noalloc and _paged forms, kvp_step_fp8) take them in place of the bf16
+ * (kvp_decode_step and its _noalloc and _paged forms, kvp_step, kvp_step_fp8) take them in place of the bf16
  * ones, which prefill and training go on using and which need not be set for the steps.  Wk and
  * Wv are NULL for a consumer.  All NULL with group 0 takes them off again.  The pointers are kept, not
  * copied.  Errors: KVP_E_INVALID_ARG, KVP_E_SHAPE.
@@ -667,7 +766,8 @@ int kvp_backward(kvp_ctx* ctx, const void* x, const void* dy, void* dx, int B, i
 #define KVP_K_BWD_ATTN_KV    12  /* backward: attention dK, dV                      */
 #define KVP_K_BWD_ATTN_Q     13  /* backward: attention dQ                          */
 #define KVP_K_BWD_AUX        14  /* backward: D, transposes, split-K sums, casts    */
-#define KVP_NUM_KERNEL_KINDS 15
+#define KVP_K_PAGE_COPY      15  /* kvp_copy_pages, kvp_copy_pages_fp8                */
+#define KVP_NUM_KERNEL_KINDS 16
 
 /*
  * kvp_profile_enable -- enable (1) or disable (0) kernel timing on ctx and

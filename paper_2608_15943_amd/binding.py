@@ -32,6 +32,7 @@ KVP_PHASE_PREFILL = 0
 KVP_PHASE_DECODE = 1
 KVP_PHASE_BACKWARD = 2
 KVP_PHASE_STEP_FP8 = 3
+KVP_PHASE_STEP = 4
 KVP_STOP_FIR_MET = 0
 KVP_STOP_BUDGET = 1
 KVP_STOP_NO_CONVERTIBLE = 2
@@ -49,6 +50,8 @@ EXPORTS = [
     "kvp_pager_create", "kvp_pager_destroy", "kvp_pager_reserve", "kvp_pager_release",
     "kvp_pager_free_pages", "kvp_pager_rows", "kvp_decode_step_noalloc",
     "kvp_set_kv_pool_fp8", "kvp_page_bytes_fp8", "kvp_append_fp8", "kvp_attention_fp8", "kvp_step_fp8",
+    "kvp_append", "kvp_attention", "kvp_step", "kvp_set_layer_window", "kvp_copy_pages", "kvp_copy_pages_fp8",
+    "kvp_pager_fork", "kvp_pager_own", "kvp_pager_trim", "kvp_pager_compact",
     "kvp_w4_bytes", "kvp_pack_w4", "kvp_linear_w4", "kvp_set_layer_w4",
     # include/kvp_calib.h: achievable-peak calibration (measurement support)
     "kvp_calib_mfma_bf16", "kvp_calib_stream_read",
@@ -56,7 +59,7 @@ EXPORTS = [
 
 KERNEL_KINDS = ["rope_table", "qkv_gemm", "flash_attn", "oproj_gemm", "dec_gemm", "dec_rope",
                 "dec_attn", "dec_combine", "dec_oproj", "f32_rope", "f32_attn", "bwd_gemm",
-                "bwd_attn_kv", "bwd_attn_q", "bwd_aux"]
+                "bwd_attn_kv", "bwd_attn_q", "bwd_aux", "page_copy"]
 
 
 class kvp_shape(C.Structure):
@@ -84,7 +87,7 @@ class kvp_model_desc(C.Structure):
 
 
 class kvp_rows(C.Structure):
-    """New rows of a call on 8-bit pages; cu, len and pages are device addresses (cu 0: one row a
+    """New rows of a call on pages; cu, len and pages are device addresses (cu 0: one row a
     sequence)."""
     _fields_ = [("cu", C.c_void_p), ("len", C.c_void_p), ("pages", C.c_void_p),
                 ("pages_stride", C.c_int32), ("B", C.c_int32), ("rows", C.c_int32),
@@ -142,6 +145,12 @@ def lib() -> C.CDLL:
         "kvp_append_fp8": ([vp, i32, vp, vp, vp, i32, C.POINTER(kvp_rows), vp, vp], i32),
         "kvp_attention_fp8": ([vp, i32, vp, C.POINTER(kvp_rows), vp, vp, C.c_size_t, vp], i32),
         "kvp_step_fp8": ([vp, vp, C.POINTER(kvp_rows), vp, vp, C.c_size_t, vp], i32),
+        "kvp_append": ([vp, i32, vp, vp, vp, i32, C.POINTER(kvp_rows), vp, vp], i32),
+        "kvp_attention": ([vp, i32, vp, C.POINTER(kvp_rows), vp, vp, C.c_size_t, vp], i32),
+        "kvp_step": ([vp, vp, C.POINTER(kvp_rows), vp, vp, C.c_size_t, vp], i32),
+        "kvp_set_layer_window": ([vp, i32, i32, i32], i32),
+        "kvp_copy_pages": ([vp, vp, vp, i32, vp], i32),
+        "kvp_copy_pages_fp8": ([vp, vp, vp, i32, vp], i32),
         "kvp_w4_bytes": ([i32, i32, i32, C.POINTER(C.c_size_t)], i32),
         "kvp_pack_w4": ([vp, i32, i32, i32, vp, vp], i32),
         "kvp_linear_w4": ([vp, vp, vp, vp, i32, i32, i32, i32, vp], i32),
@@ -152,6 +161,10 @@ def lib() -> C.CDLL:
         "kvp_pager_release": ([vp, i32], i32),
         "kvp_pager_free_pages": ([vp, C.POINTER(i32)], i32),
         "kvp_pager_rows": ([vp, C.POINTER(C.c_int32), i32, C.POINTER(C.c_int32)], i32),
+        "kvp_pager_fork": ([vp, i32, i32, i32], i32),
+        "kvp_pager_own": ([vp, i32, i32, i32, C.POINTER(C.c_int32), C.POINTER(C.c_int32), i32, C.POINTER(i32)], i32),
+        "kvp_pager_trim": ([vp, i32, i32, i32], i32),
+        "kvp_pager_compact": ([vp, C.POINTER(C.c_int32), C.POINTER(C.c_int32), i32, C.POINTER(i32)], i32),
         "kvp_status_string": ([i32], C.c_char_p),
         "kvp_last_error": ([], C.c_char_p),
         "kvp_profile_enable": ([vp, i32], i32),
@@ -343,6 +356,25 @@ class Model:
         _check(lib().kvp_decode_step_paged(self.ctx, x, len_dev, max_len, pages_dev, pages_stride, y, B,
                                            ws, ws_bytes, stream or None), "kvp_decode_step_paged")
 
+    def kvp_append(self, l, q, k, v, ld, rows, q_out, stream=0):
+        _check(lib().kvp_append(self.ctx, l, q or None, k or None, v or None, ld, C.byref(rows), q_out or None,
+                                stream or None), "kvp_append")
+
+    def kvp_set_layer_window(self, l, window, sinks=0):
+        _check(lib().kvp_set_layer_window(self.ctx, l, window, sinks), "kvp_set_layer_window")
+
+    def kvp_attention(self, l, q, rows, out, ws, ws_bytes, stream=0):
+        _check(lib().kvp_attention(self.ctx, l, q, C.byref(rows), out, ws, ws_bytes, stream or None), "kvp_attention")
+
+    def kvp_step(self, x, rows, y, ws, ws_bytes, stream=0):
+        _check(lib().kvp_step(self.ctx, x, C.byref(rows), y, ws, ws_bytes, stream or None), "kvp_step")
+
+    def kvp_copy_pages(self, src, dst, n, stream=0):
+        _check(lib().kvp_copy_pages(self.ctx, src or None, dst or None, n, stream or None), "kvp_copy_pages")
+
+    def kvp_copy_pages_fp8(self, src, dst, n, stream=0):
+        _check(lib().kvp_copy_pages_fp8(self.ctx, src or None, dst or None, n, stream or None), "kvp_copy_pages_fp8")
+
     def kvp_set_kv_pool_fp8(self, l, k, v, scales, n_pages):
         _check(lib().kvp_set_kv_pool_fp8(self.ctx, l, k, v, scales, n_pages), "kvp_set_kv_pool_fp8")
 
@@ -449,6 +481,29 @@ class Pager:
 
     def release(self, seq):
         _check(lib().kvp_pager_release(self.p, seq), "kvp_pager_release")
+
+    def fork(self, src, dst, n_tokens):
+        _check(lib().kvp_pager_fork(self.p, src, dst, n_tokens), "kvp_pager_fork")
+
+    def own(self, seq, start, end, max_pairs=None):
+        """Pages (src, dst), numpy int32, that the caller copies before it appends at [start, end)."""
+        if max_pairs is None:
+            max_pairs = max((end + 63) // 64 - start // 64, 0)
+        return self._pairs("kvp_pager_own", max_pairs, lambda *a: lib().kvp_pager_own(self.p, seq, start, end, *a))
+
+    def trim(self, seq, start, end):
+        _check(lib().kvp_pager_trim(self.p, seq, start, end), "kvp_pager_trim")
+
+    def compact(self, max_pairs):
+        """Pages (src, dst), numpy int32, that the caller copies before it uses the rows again."""
+        return self._pairs("kvp_pager_compact", max_pairs, lambda *a: lib().kvp_pager_compact(self.p, *a))
+
+    def _pairs(self, where, max_pairs, call):
+        src, dst = np.empty(max_pairs, np.int32), np.empty(max_pairs, np.int32)
+        n = C.c_int()
+        _check(call(src.ctypes.data_as(C.POINTER(C.c_int32)), dst.ctypes.data_as(C.POINTER(C.c_int32)), max_pairs,
+                    C.byref(n)), where)
+        return src[: n.value], dst[: n.value]
 
     def free_pages(self) -> int:
         n = C.c_int()

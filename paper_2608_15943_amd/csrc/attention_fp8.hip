@@ -33,14 +33,10 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "fp8_cache.h"
+#include "attn_rows.h"
 
 namespace kvp {
 namespace {
-
-constexpr int D = kHead, TILE = kPage;
-constexpr int PSTRIDE = D + 4;    // O[128], m, l, pad
-constexpr float kLazy = 8.0f;     // the running maximum follows once it is 2^8 behind
 
 // 8 codes (two words) as bf16.
 __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
@@ -51,232 +47,13 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-struct CutItem {
-    int np, row, n, act, head, pad[3];     // pieces; first row in the tensors, rows (of them act see something), first head
-};
-
-struct AttnArgs {
-    NewRows r;
+struct AttnArgs : ListArgs {
     const uint16_t* q;
     const uint8_t* kc;
     const uint8_t* vc;
     const float* sc;
-    uint16_t* out;
-    float* part;       // [2 W][cols][PSTRIDE]: slot 2 w: share w's piece of an item that began before it,
-                       // 2 w + 1: of one that begins with it and goes on
-    int a, g;
-    int m, cols;       // rows of an item, columns that they make
-    int mw;            // rows of a wave of attention_many_kernel: m / 4
-    // What the join reads: of attention_few_kernel, for each sequence and K/V head the share that
-    // begins it and how many shares have a part; of attention_many_kernel, for each share the item that it
-    // begins and does not end (np 0: none).
-    int2* cut;
-    struct CutItem* cut_many;
     float scale_log2;
 };
-
-// sum of floor((A i + B) / M) over 0 <= i < N, by Euclid's steps.
-__device__ __forceinline__ uint32_t floor_sum(uint32_t N, uint32_t M, uint32_t A, uint32_t B) {
-    uint32_t s = 0;
-    while (N) {
-        s += (uint32_t)((uint64_t)N * (N - 1) / 2) * (A / M) + N * (B / M);
-        A %= M;
-        B %= M;
-        const uint32_t y = A * N + B;
-        N = y / M;
-        B = y % M;
-        const uint32_t t = M;
-        M = A;
-        A = t;
-    }
-    return s;
-}
-
-// Tiles of block c of a sequence, and of its first c blocks; a block without a row that sees anything
-// counts one (it writes zeros).
-__device__ __forceinline__ int tiles_of(const SeqRows& s, int m, int c) {
-    const int last = min((c + 1) * m, s.act) - 1;
-    return last < c * m ? 1 : (s.len + last) / TILE + 1;
-}
-__device__ __forceinline__ uint32_t tiles_before(const SeqRows& s, int m, int c) {
-    const int full = min(c, s.act / m);            // blocks whose m rows all see something
-    uint32_t n = full + floor_sum(full, TILE, m, s.len + m - 1);
-    if (c > full) n += tiles_of(s, m, full) + (c - full - 1);
-    return n;
-}
-__device__ __forceinline__ int blocks_of(const SeqRows& s, int m) { return (s.n + m - 1) / m; }
-// FEW: every sequence has one block at most.
-template <bool FEW>
-__device__ __forceinline__ uint32_t seq_tiles(const SeqRows& s, int m) {
-    if (FEW) return s.n ? tiles_of(s, m, 0) : 0;
-    return tiles_before(s, m, blocks_of(s, m));
-}
-
-// The list shared by W waves: wave w starts at tile floor(w T / W).  T < 2^31, W <= 4096.
-struct Split {
-    uint32_t T, W, q, rem;
-    Split() = default;
-    __device__ __forceinline__ Split(uint32_t T_, uint32_t waves) : T(T_), W(min(T_, waves)), q(T_ / max(W, 1u)), rem(T_ % max(W, 1u)) {}
-    __device__ __forceinline__ uint32_t start(uint32_t w) const { return w * q + w * rem / W; }
-    // The wave that holds tile x: ceil((x + 1) W / T) - 1; exact in double.
-    __device__ __forceinline__ uint32_t wave_of(uint32_t x) const {
-        return (uint32_t)(((double)(x + 1) * (double)W - 1.0) / (double)T);
-    }
-};
-
-// 64 sequences at a time, one a lane: their rows, tiles for one K/V head, and the tiles of the list
-// before each.
-template <bool FEW>
-struct Lanes {
-    int b0;
-    SeqRows s;
-    uint32_t n, pre;     // pre: before this lane's sequence
-    uint32_t total;      // tiles of the 64
-    __device__ __forceinline__ void load(const AttnArgs& A, int b0_, uint32_t base) {
-        const int lane = threadIdx.x & 63;
-        b0 = b0_;
-        s = SeqRows{0, 0, 0, 0};
-        n = 0;
-        if (b0 + lane < A.r.B) {
-            s = seq_rows(A.r, b0 + lane);
-            n = seq_tiles<FEW>(s, A.m);
-        }
-        uint32_t p = n * A.g;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const uint32_t v = __shfl_up(p, off);
-            if (lane >= off) p += v;
-        }
-        total = __builtin_amdgcn_readlane(p, 63);
-        pre = base + p - n * A.g;
-    }
-    __device__ __forceinline__ SeqRows rows(int w) const {
-        return {__builtin_amdgcn_readlane(s.row0, w), __builtin_amdgcn_readlane(s.n, w),
-                __builtin_amdgcn_readlane(s.len, w), __builtin_amdgcn_readlane(s.act, w)};
-    }
-};
-template <bool FEW>
-__device__ __forceinline__ uint32_t list_tiles(const AttnArgs& A, Lanes<FEW>& L) {
-    uint32_t T = 0;
-    for (int b0 = 0; b0 < A.r.B; b0 += 64) {
-        L.load(A, b0, T);
-        T += L.total;
-    }
-    return T;
-}
-
-// An item and a place in it.
-struct Item {
-    int b, kvh, c;       // sequence, K/V head, block of rows
-    SeqRows s;
-    int t, n;            // tile, tiles
-};
-// The item that holds tile x of the list (x < T).
-template <bool FEW>
-__device__ __forceinline__ Item find_tile(const AttnArgs& A, Lanes<FEW>& L, uint32_t x) {
-    if (A.r.B > 64) {
-        uint32_t base = 0;
-        for (int b0 = 0;; b0 += 64) {
-            L.load(A, b0, base);
-            if (x < base + L.total) break;
-            base += L.total;
-        }
-    }
-    Item it;
-    // The last lane that begins at or before x and has tiles: those behind it begin later.
-    const int w = 63 - __builtin_clzll(__ballot(L.n > 0 && L.pre <= x));
-    it.b = L.b0 + w;
-    it.s = L.rows(w);
-    const uint32_t n = __builtin_amdgcn_readlane(L.n, w);
-    uint32_t rem = x - __builtin_amdgcn_readlane(L.pre, w);
-    it.kvh = rem / n;
-    rem %= n;
-    it.c = 0;
-    it.t = rem;
-    if (!FEW) {
-        // The last block with tiles_before <= rem.  About c (1 + (len + m / 2) / 64) + c^2 m / 128 tiles lie
-        // before block c: its root, then exactly.
-        const float al = A.m / 128.f, be = 1.f + (max(it.s.len, 0) + 0.5f * A.m) / 64.f;
-        const int cmax = blocks_of(it.s, A.m) - 1;
-        int c = (int)((sqrtf(be * be + 4.f * al * rem) - be) / (2.f * al));
-        c = __builtin_amdgcn_readfirstlane(min(max(c, 0), cmax));
-        uint32_t n0 = tiles_before(it.s, A.m, c);
-        while (c > 0 && n0 > rem) n0 -= tiles_of(it.s, A.m, --c);
-        for (; c < cmax; ++c) {
-            const uint32_t k = tiles_of(it.s, A.m, c);
-            if (n0 + k > rem) break;
-            n0 += k;
-        }
-        it.c = c;
-        it.t = rem - n0;
-    }
-    it.n = tiles_of(it.s, A.m, it.c);
-    return it;
-}
-
-// Whether the sequences have no more rows together than the call has, as the launch's rule takes it for the bound of the
-// list's 2^31 tiles (of few columns it holds whatever the offsets are).  Exact: rows < 2^23, 384 or more values each.
-__device__ __forceinline__ bool rows_bounded(const NewRows& r) {
-    float n = 0.f;
-    for (int b = threadIdx.x & 63; b < r.B; b += 64) n += (float)seq_rows(r, b).n;
-    return wave_sum(n) <= (float)r.rows;
-}
-
-// A share of the list: where it begins and ends.
-template <bool FEW>
-__device__ __forceinline__ bool take_share(const AttnArgs& A, Split* sp, uint32_t* w, uint32_t* left, Item* it) {
-    Lanes<FEW> L;
-    const bool bounded = FEW || rows_bounded(A.r);
-    *sp = Split(list_tiles(A, L), gridDim.x);
-    if (!bounded || blockIdx.x >= sp->W) return false;
-    // Shares in one block on one XCD: neighbours read the same K/V head.
-    *w = xcd_remap(blockIdx.x, sp->W);
-    const uint32_t x = sp->start(*w);
-    *left = sp->start(*w + 1) - x;
-    *it = find_tile(A, L, x);
-    return true;
-}
-// The item behind `it` in the list; false past the end.
-__device__ __forceinline__ bool next_item(const AttnArgs& A, Item& it) {
-    it.t = 0;
-    if (++it.c == blocks_of(it.s, A.m)) {
-        it.c = 0;
-        if (++it.kvh == A.g) {
-            it.kvh = 0;
-            for (++it.b; it.b < A.r.B; ++it.b) {       // sequences without rows have no tiles
-                it.s = seq_rows(A.r, it.b);
-                if (it.s.n) break;
-            }
-            if (it.b >= A.r.B) return false;
-        }
-    }
-    it.n = tiles_of(it.s, A.m, it.c);
-    return true;
-}
-
-// Index of the page of tile it.t, for it.kvh.  A wave keeps 64 entries of a table row, so that one
-// dependent load serves 64 tiles.
-struct Table {
-    int b = -1, c = -1, v = 0;
-    __device__ __forceinline__ size_t page(const AttnArgs& A, const Item& i) {
-        if (i.b != b || (i.t >> 6) != c) {
-            b = i.b;
-            c = i.t >> 6;
-            const int e = 64 * c + (threadIdx.x & 63);
-            v = e < A.r.stride ? A.r.pt[(size_t)i.b * A.r.stride + e] : 0;
-        }
-        const int pg = min(max(__builtin_amdgcn_readlane(v, i.t & 63), 0), A.r.n_pages - 1);
-        return (size_t)i.kvh * A.r.n_pages + pg;
-    }
-};
-
-// The thread's index, unknown to the compiler: what is computed from it where an item begins or ends is not
-// held in registers (or spilled) through the loop over its tiles.
-__device__ __forceinline__ int thread_now() {
-    int t = threadIdx.x;
-    asm volatile("" : "+v"(t));
-    return t;
-}
 
 // 16 NB columns of an item, from row t0 of the sequence on: a lane's column of block cb is head tj of
 // row t0 + tc.
@@ -434,7 +211,7 @@ __global__ __launch_bounds__(NW ? 64 * NW : 64, 2) void attention_few_kernel(Att
     Split sp;
     uint32_t w = 0, left;
     if constexpr (LIST) {
-        if (!take_share<true>(A, &sp, &w, &left, &it)) return;
+        if (!take_share<true, false>(A, &sp, &w, &left, &it)) return;
     } else {
         it.b = blockIdx.x / A.g;
         it.kvh = blockIdx.x % A.g;
@@ -442,13 +219,13 @@ __global__ __launch_bounds__(NW ? 64 * NW : 64, 2) void attention_few_kernel(Att
         if (!it.s.n) return;
         it.c = 0;
         it.t = wave;
-        it.n = tiles_of(it.s, A.m, 0);
+        it.begin<false>(A);
         left = max(it.n - wave + NW - 1, 0) / NW;
     }
     Columns<NB> C;
     u32x4 q[NB][2][2];
     const int r = A.a / A.g;
-    Table tab;
+    Table<false> tab;
     u32x4 k[4][2], v[8];         // [score block][64-dimension half], [16-dimension block]
     float ks, vs;                // scales of the lane group's 16 positions
     const uint32_t koff = (16 * (col >> 2) + (col & 3)) * D + 16 * grp, voff = grp * kBlkBytes + col * kBlk;
@@ -493,7 +270,7 @@ __global__ __launch_bounds__(NW ? 64 * NW : 64, 2) void attention_few_kernel(Att
         Item nx = it;
         if (more) {
             if (LIST && ends)
-                more = next_item(A, nx);
+                more = next_item<false>(A, nx);
             else
                 nx.t += STEP;
         }
@@ -675,7 +452,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 4 : 3) void attention_many_kernel(At
     uint32_t w = 0, left;
     if constexpr (LIST) {
         Split sp;
-        if (!take_share<false>(A, &sp, &w, &left, &it)) {
+        if (!take_share<false, false>(A, &sp, &w, &left, &it)) {
             if (tid == 0) A.cut_many[blockIdx.x].np = 0;
             return;
         }
@@ -684,9 +461,9 @@ __global__ __launch_bounds__(256, NB == 1 ? 4 : 3) void attention_many_kernel(At
             CutItem cut{};
             if (w + 1 < sp.W) {
                 const uint32_t xe = sp.start(w + 1) - 1;
-                Lanes<false> L;
-                list_tiles(A, L);
-                const Item e = find_tile(A, L, xe);
+                Lanes<false, false> L;
+                list_tiles<false, false>(A, L);
+                const Item e = find_tile<false, false>(A, L, xe);
                 if (e.t + 1 < e.n && xe - e.t >= sp.start(w)) {
                     cut.np = sp.wave_of(xe - e.t + e.n - 1) - w + 1;
                     cut.row = e.s.row0 + e.c * A.m;
@@ -707,13 +484,13 @@ __global__ __launch_bounds__(256, NB == 1 ? 4 : 3) void attention_many_kernel(At
         it.s = seq_rows(A.r, it.b);
         if (it.c >= blocks_of(it.s, A.m)) return;
         it.t = 0;
-        it.n = tiles_of(it.s, A.m, it.c);
+        it.begin<false>(A);
         left = it.n;
     }
     const int r = A.a / A.g, wcols = A.mw * r;
     Columns<NB> C;
     Queries8<NB> Q;
-    Table tab;
+    Table<false> tab;
     float kn, vn;          // scales of the tile that comes
     auto issue = [&](const Item& i, int stg) {
         const size_t at = tab.page(A, i);
@@ -743,7 +520,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 4 : 3) void attention_many_kernel(At
         Item nx = it;
         if (more) {
             if (LIST && ends)
-                more = next_item(A, nx);
+                more = next_item<false>(A, nx);
             else
                 ++nx.t;
         }
@@ -820,215 +597,6 @@ __global__ __launch_bounds__(256, NB == 1 ? 4 : 3) void attention_many_kernel(At
     }
 }
 
-// Slot of piece i of an item that share w0 begins.
-__device__ __forceinline__ size_t slot_of(int w0, int i) { return 2 * (size_t)(w0 + i) + (i == 0 ? 1 : 0); }
-
-constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
-
-// Joins np pieces of NC columns, half a wave a piece, 8 requested at a time: lane holds dimensions 4 (lane % 32) .. + 3 of
-// num.  piece(i, j): piece i of column j.
-template <int NC, class Piece>
-__device__ __forceinline__ void join_halves(int np, Piece piece, f32x4 (&num)[NC], float (&den)[NC]) {
-    const int lane = threadIdx.x & 63, half = lane >> 5;
-    float M[NC], wt[NC];
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-        M[j] = -INFINITY;
-        den[j] = 0.f;
-        num[j] = f32x4{};
-    }
-    for (int s0 = 0; s0 < np; s0 += 64) {
-        const int k = min(np - s0, 64);
-#pragma unroll
-        for (int j = 0; j < NC; ++j) {
-            float m = -INFINITY, l = 0.f;
-            if (lane < k) {
-                const float* p = piece(s0 + lane, j);
-                m = p[D];
-                l = p[D + 1];
-            }
-            const float Mn = fmaxf(M[j], wave_max(m)), f = exp2f(M[j] - Mn);
-            wt[j] = exp2f(m - Mn);
-            den[j] = den[j] * f + wave_sum(wt[j] * l);
-            num[j] *= f;
-            M[j] = Mn;
-        }
-        for (int i = 0; i < k; i += 8) {
-            f32x4 v[NC][4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int j = 0; j < NC; ++j)       // a piece past the last weighs nothing
-                    v[j][u] = *(const f32x4*)(piece(s0 + min(i + 2 * u + half, k - 1), j) + 4 * (lane & 31));
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int j = 0; j < NC; ++j) num[j] += __shfl(wt[j], i + 2 * u + half) * v[j][u];
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < NC; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) num[j][e] += __shfl_xor(num[j][e], 32);
-}
-
-// One new row a sequence or a few (an item is a sequence and K/V head): a workgroup a column.  Wave
-// v takes pieces v, v + 4, ...: lane i holds the maximum and sum of its i-th, every lane two of the
-// 128 dimensions; the waves meet in LDS.
-__global__ __launch_bounds__(kJoinThreads) void join_few_kernel(AttnArgs A) {
-    __shared__ float num_s[kJoinWaves][D], m_s[kJoinWaves], den_s[kJoinWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int x = blockIdx.x / A.cols, c = blockIdx.x % A.cols, b = x / A.g, kvh = x % A.g, r = A.a / A.g;
-    const SeqRows s = seq_rows(A.r, b);
-    const int t = c / r;
-    if (t >= s.n) return;
-    const int w0 = A.cut[x].x, np = A.cut[x].y;
-    if (np == 1) return;                       // written by its wave
-    const size_t step = (size_t)A.cols * PSTRIDE;
-    const float* part = A.part + (size_t)c * PSTRIDE;
-    const int mine = (np - wave + kJoinWaves - 1) / kJoinWaves;
-    float M = -INFINITY, den = 0.f;
-    f32x2 num = {0.f, 0.f};
-    for (int s0 = 0; s0 < mine; s0 += 64) {
-        const int k = min(mine - s0, 64);
-        auto piece = [&](int i) { return part + slot_of(w0, wave + kJoinWaves * (s0 + i)) * step; };
-        float m = -INFINITY, l = 0.f;
-        if (lane < k) {
-            const float* p = piece(lane);
-            m = p[D];
-            l = p[D + 1];
-        }
-        const float Mn = fmaxf(M, wave_max(m)), f = exp2f(M - Mn), wt = exp2f(m - Mn);
-        den = den * f + wave_sum(lane < k ? wt * l : 0.f);
-        num *= f;
-        M = Mn;
-        auto add = [&](auto n_t, int i0) __attribute__((always_inline)) {
-            constexpr int N = decltype(n_t)::value;
-            f32x2 v[N];
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = *(const f32x2*)(piece(i0 + i) + 2 * lane);
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wt), i0 + i));
-                num[0] += w * v[i][0];
-                num[1] += w * v[i][1];
-            }
-        };
-        int i = 0;
-        for (; i + 8 <= k; i += 8) add(std::integral_constant<int, 8>{}, i);
-        for (; i + 4 <= k; i += 4) add(std::integral_constant<int, 4>{}, i);
-        for (; i < k; ++i) add(std::integral_constant<int, 1>{}, i);
-    }
-    *(f32x2*)&num_s[wave][2 * lane] = num;
-    if (lane == 0) {
-        m_s[wave] = M;
-        den_s[wave] = den;
-    }
-    __syncthreads();
-    if (tid >= D) return;
-    float Mx = m_s[0];
-#pragma unroll
-    for (int v = 1; v < kJoinWaves; ++v) Mx = fmaxf(Mx, m_s[v]);
-    float ns = 0.f, ds = 0.f;
-#pragma unroll
-    for (int v = 0; v < kJoinWaves; ++v) {
-        const float f = exp2f(m_s[v] - Mx);
-        ns += f * num_s[v][tid];
-        ds += f * den_s[v];
-    }
-    A.out[((size_t)(s.row0 + t) * A.a + kvh * r + c % r) * D + tid] = t < s.act ? f2bf(ns / ds) : (uint16_t)0;
-}
-
-// The same where items have few pieces: a wave a column.
-__global__ __launch_bounds__(kJoinThreads) void join_short_kernel(AttnArgs A) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = A.a / A.g;
-    const int y = blockIdx.x * kJoinWaves + wave;
-    if (y >= A.r.B * A.g * A.cols) return;
-    const int x = y / A.cols, c = y % A.cols, b = x / A.g, kvh = x % A.g;
-    const SeqRows s = seq_rows(A.r, b);
-    const int t = c / r;
-    if (t >= s.n) return;
-    const int w0 = A.cut[x].x, np = A.cut[x].y;
-    if (np == 1) return;                       // written by its wave
-    const size_t step = (size_t)A.cols * PSTRIDE;
-    const float* part = A.part + (size_t)c * PSTRIDE;
-    f32x4 num[1];
-    float den[1];
-    join_halves<1>(np, [&](int i, int) { return part + slot_of(w0, i) * step; }, num, den);
-    u32x2 o = {pack2bf(num[0][0] / den[0], num[0][1] / den[0]), pack2bf(num[0][2] / den[0], num[0][3] / den[0])};
-    if (t >= s.act) o = u32x2{0, 0};
-    if (lane < 32) *(u32x2*)(A.out + ((size_t)(s.row0 + t) * A.a + kvh * r + c % r) * D + 4 * lane) = o;
-}
-
-// Many rows: workgroups for each share, which join the item that it begins and does not end; a wave a pair
-// of columns, with the pieces of both requested together.
-constexpr int kJoinCols = 2 * kJoinWaves;
-__global__ __launch_bounds__(kJoinThreads) void join_many_kernel(AttnArgs A) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = A.a / A.g, w0 = blockIdx.x;
-    const CutItem it = A.cut_many[w0];
-    if (it.np == 0) return;
-    const size_t step = (size_t)A.cols * PSTRIDE;
-    const int c0 = kJoinCols * blockIdx.y + 2 * wave;
-    const int cols = min(A.cols, it.n * r);
-    if (c0 >= cols) return;
-    float M[2] = {-INFINITY, -INFINITY}, den[2] = {0.f, 0.f};
-    f32x2 num[2] = {{0.f, 0.f}, {0.f, 0.f}};
-    for (int i0 = 0; i0 < it.np; i0 += 2) {
-        f32x2 v[2][2], ml[2][2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                // A piece past the last and a column past the item's repeat the last one.
-                const float* p = A.part + slot_of(w0, min(i0 + i, it.np - 1)) * step + (size_t)min(c0 + j, cols - 1) * PSTRIDE;
-                v[i][j] = *(const f32x2*)(p + 2 * lane);
-                ml[i][j] = *(const f32x2*)(p + D);
-            }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (i0 + i >= it.np) continue;
-                const float Mn = fmaxf(M[j], ml[i][j][0]), f = exp2f(M[j] - Mn), wt = exp2f(ml[i][j][0] - Mn);
-                den[j] = den[j] * f + wt * ml[i][j][1];
-                num[j][0] = num[j][0] * f + wt * v[i][j][0];
-                num[j][1] = num[j][1] * f + wt * v[i][j][1];
-                M[j] = Mn;
-            }
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int c = c0 + j, t = c / r;
-        if (c >= cols) break;
-        const uint32_t o = t < it.act ? pack2bf(num[j][0] / den[j], num[j][1] / den[j]) : 0u;
-        *(uint32_t*)(A.out + ((size_t)(it.row + t) * A.a + it.head + c % r) * D + 2 * lane) = o;
-    }
-}
-
-// The same where items have many pieces.
-__global__ __launch_bounds__(kJoinThreads) void join_long_kernel(AttnArgs A) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = A.a / A.g, w0 = blockIdx.x;
-    const CutItem it = A.cut_many[w0];
-    if (it.np == 0) return;
-    const int c0 = kJoinCols * blockIdx.y + 2 * wave;
-    const int cols = min(A.cols, it.n * r);
-    if (c0 >= cols) return;
-    const size_t step = (size_t)A.cols * PSTRIDE;
-    f32x4 num[2];
-    float den[2];
-    // A column past the item's repeats the last one.
-    join_halves<2>(it.np, [&](int i, int j) { return A.part + slot_of(w0, i) * step + (size_t)min(c0 + j, cols - 1) * PSTRIDE; }, num,
-                   den);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int c = c0 + j, t = c / r;
-        if (c >= cols) break;
-        u32x2 o = {pack2bf(num[j][0] / den[j], num[j][1] / den[j]), pack2bf(num[j][2] / den[j], num[j][3] / den[j])};
-        if (t >= it.act) o = u32x2{0, 0};
-        if (lane < 32) *(u32x2*)(A.out + ((size_t)(it.row + t) * A.a + it.head + c % r) * D + 4 * lane) = o;
-    }
-}
-
 // Shares of the list.  Few: one wave a SIMD (of 1, 1.5, 2 and 3 a SIMD, us: 64 x 32768 positions 738, 743,
 // 746, 761; 8 x 64K-128K 287, 290, 292, 299; 16 x 4 rows over 1500-8000 positions 44, 46, 47, 52; 3/4 of a wave
 // 739, 289, 45; half a wave 930, 359, 50; requesting two tiles ahead changes none of them).  Many: as many
@@ -1080,7 +648,7 @@ hipError_t attention_fp8(const NewRows& r, int a, int g, const uint16_t* q, cons
     const int heads = a / g;
     // The list counts tiles in 31 bits; where it might not, items run one by one.
     auto listed = [&](int64_t items) { return items * (r.max_pos / TILE + 1) <= INT32_MAX; };
-    AttnArgs A{r, q, kc, vc, sc, out, (float*)ws, a, g, 0, 0, 0, nullptr, nullptr, (float)(1.4426950408889634 / sqrt((double)D))};
+    AttnArgs A{{r, out, (float*)ws, a, g}, q, kc, vc, sc, (float)(1.4426950408889634 / sqrt((double)D))};
     hipError_t e;
     if (r.max_new * heads <= kFewCols) {
         A.m = r.max_new;

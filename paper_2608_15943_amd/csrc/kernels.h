@@ -215,6 +215,34 @@ size_t attention_fp8_bytes(int B, int g, int simds);
 hipError_t attention_fp8(const NewRows& r, int a, int g, const uint16_t* q, const uint8_t* kc, const uint8_t* vc,
                          const float* sc, uint16_t* out, void* ws, int simds, hipStream_t st);
 
+// ---- new rows on the paged bf16 cache ---------------------------------------------
+
+// As append_fp8 and append_fp8_planes, into pools K [g][n][64][128] and V [g][n][128][64].
+hipError_t append_bf16(const NewRows& r, int a, int g, const uint16_t* q, const uint16_t* k, const uint16_t* v, int ldq,
+                       int ldkv, const RopeFreqs& th, uint16_t* q_out, uint16_t* kc, uint16_t* vc, hipStream_t st);
+hipError_t append_bf16_planes(const NewRows& r, int a, int g, const float* part, int nsplit, int N, bool producer,
+                              const RopeFreqs& th, uint16_t* q_out, uint16_t* kc, uint16_t* vc, hipStream_t st);
+
+// Attention of the rows of q [rows][a * 128] over the pools; window 0: all of [0, p], else above p - window and below
+// sinks.  ws: attention_rows_bytes of scratch (16-byte aligned).  simds: of the device.
+size_t attention_rows_bytes(int B, int g, int simds);
+hipError_t attention_rows(const NewRows& r, int a, int g, int window, int sinks, const uint16_t* q, const uint16_t* kc,
+                          const uint16_t* vc, uint16_t* out, void* ws, int simds, hipStream_t st);
+
+// Page pools of several producers (sc: 8-bit pools only).
+struct PagePools {
+    static constexpr int kMax = 32;
+    struct Pool {
+        void* k;
+        void* v;
+        float* sc;
+        int n_pages;
+    } pool[kMax];
+    int n = 0;
+};
+// Pages src[i] to pages dst[i], i < n (device arrays), in every pool; pairs with an index outside a pool are left out.
+hipError_t copy_pages(const PagePools& pools, bool fp8, const int32_t* src, const int32_t* dst, int n, int g, hipStream_t st);
+
 // ---- 4-bit weights --------------------------------------------------------------
 
 // Up to three packed weights [rows_i][K] stacked along N (layout: linear_w4.hip).

@@ -51,6 +51,8 @@ struct Layer {
     int n_pages8 = 0;
     const void* w4[4] = {}; // 4-bit weights Q, K, V, O (kvp_set_layer_w4)
     int group = 0;          // inputs a scale; 0: none set
+    int window = 0;         // kvp_set_layer_window; 0: none
+    int sinks = 0;
     bool weights = false;
     float* dwq = nullptr;   // weight gradients (training), fp32
     float* dwk = nullptr;
@@ -120,7 +122,9 @@ struct kvp_ctx {
 
 namespace {
 
-// KVP_PHASE_STEP_FP8: S is the number of rows.
+// The steps on rows: S is the number of rows.
+bool step_phase(int phase) { return phase == KVP_PHASE_STEP || phase == KVP_PHASE_STEP_FP8; }
+
 Workspace layout(const kvp_ctx& c, int phase, int B, int S) {
     Workspace w;
     size_t off = 0;
@@ -130,7 +134,7 @@ Workspace layout(const kvp_ctx& c, int phase, int B, int S) {
         return at;
     };
     const size_t e = c.esize();
-    const size_t rows = phase == KVP_PHASE_PREFILL ? (size_t)B * S : phase == KVP_PHASE_STEP_FP8 ? (size_t)S : (size_t)B;
+    const size_t rows = phase == KVP_PHASE_PREFILL ? (size_t)B * S : step_phase(phase) ? (size_t)S : (size_t)B;
     const size_t nproj = (size_t)(c.d.a + 2 * c.d.g) * c.d.d_h;
     w.q = take(rows * c.n_q() * e);
     w.o = take(rows * c.n_q() * e);
@@ -141,12 +145,13 @@ Workspace layout(const kvp_ctx& c, int phase, int B, int S) {
             w.rope = take((size_t)S * (c.d.d_h / 2) * sizeof(float2));
         else
             w.proj = take(rows * nproj * sizeof(float));
-    } else if (phase == KVP_PHASE_STEP_FP8) {
+    } else if (step_phase(phase)) {
         // Few rows: planes of the skinny projection; more: the rows of Q, K and V in bf16.
         const size_t few = std::min<size_t>(rows, kDecodeMaxRows);
         const size_t planes = few * nproj * sizeof(float) * kvp::decode_gemm_splits(c.d.h);
         w.proj = take(rows > few ? std::max(planes, rows * nproj * 2) : planes);
-        w.part = take(kvp::attention_fp8_bytes(B, c.d.g, c.decode_waves));
+        w.part = take(phase == KVP_PHASE_STEP ? kvp::attention_rows_bytes(B, c.d.g, c.decode_waves)
+                                              : kvp::attention_fp8_bytes(B, c.d.g, c.decode_waves));
     } else {
         // bf16: one plane per 512-wide K slice of the projection GEMM (K = h for both GEMMs).
         const size_t planes = c.bf16() ? (size_t)kvp::decode_gemm_splits(c.d.h) : 1;
@@ -201,7 +206,7 @@ const char* kind_name(int kind) {
         "RoPE table", "projection GEMM", "flash attention", "output projection GEMM",
         "decode projection GEMM", "decode RoPE + append", "decode attention", "decode combine",
         "decode output projection", "fp32 RoPE", "fp32 attention", "backward GEMM",
-        "backward attention dK/dV", "backward attention dQ", "backward auxiliary kernel"};
+        "backward attention dK/dV", "backward attention dQ", "backward auxiliary kernel", "page copy"};
     return kind >= 0 && kind < KVP_NUM_KERNEL_KINDS ? names[kind] : "kernel";
 }
 
@@ -238,11 +243,19 @@ int timed(kvp_ctx* c, int kind, hipStream_t st, F&& launch) {
     return debug_check(c, kind, st);
 }
 
+// Of a call that attends to everything: no layer has a window.
+int check_no_window(const kvp_ctx* c, int l) {
+    if (c->layers[l].window)
+        return fail(KVP_E_STATE, "layer %d has an attention window, which this call does not apply", l);
+    return KVP_OK;
+}
+
 // w4: the call runs on a layer's 4-bit weights where it has them.
 int check_layers(const kvp_ctx* c, int lo, int hi, bool paged = false, bool w4 = false) {
     for (int l = lo; l < hi; ++l) {
         if (!c->layers[l].weights && !(w4 && c->layers[l].group))
             return fail(KVP_E_STATE, "weights of layer %d were never set", l);
+        if (const int rc = check_no_window(c, l)) return rc;
         const int p = c->tau[l];
         if (paged ? !c->layers[p].kp || !c->layers[p].vp : !c->layers[p].kc || !c->layers[p].vc)
             return fail(KVP_E_STATE, "KV %s of producer %d (used by layer %d) was never set",
@@ -774,15 +787,14 @@ BwdWs bwd_layout(const kvp_ctx& c, int B, int S) {
 
 extern "C" int kvp_workspace_size(const kvp_ctx* ctx, int phase, int B, int S, size_t* bytes) {
     if (!ctx || !bytes) return fail(KVP_E_INVALID_ARG, "kvp_workspace_size: NULL argument");
-    if (phase != KVP_PHASE_PREFILL && phase != KVP_PHASE_DECODE && phase != KVP_PHASE_BACKWARD &&
-        phase != KVP_PHASE_STEP_FP8)
+    if (phase != KVP_PHASE_PREFILL && phase != KVP_PHASE_DECODE && phase != KVP_PHASE_BACKWARD && !step_phase(phase))
         return fail(KVP_E_INVALID_ARG, "kvp_workspace_size: unknown phase");
     const bool seq = phase != KVP_PHASE_DECODE;
     if (B < 1 || (seq && S < 1))
         return fail(KVP_E_INVALID_ARG, "kvp_workspace_size: B and S must be >= 1");
     if (B > ctx->d.max_batch) return fail(KVP_E_CAPACITY, "kvp_workspace_size: B > max_batch");
-    if (phase == KVP_PHASE_STEP_FP8) {
-        if (!ctx->bf16()) return fail(KVP_E_SHAPE, "kvp_workspace_size: 8-bit K/V storage needs a bf16 model");
+    if (step_phase(phase)) {
+        if (!ctx->bf16()) return fail(KVP_E_SHAPE, "kvp_workspace_size: paged K/V storage needs a bf16 model");
         if (S > (int64_t)ctx->d.max_batch * ctx->d.max_seq)
             return fail(KVP_E_CAPACITY, "kvp_workspace_size: S > max_batch * max_seq rows");
     } else if (seq && S > ctx->d.max_seq)
@@ -968,8 +980,20 @@ extern "C" int kvp_decode_step_paged(kvp_ctx* ctx, const void* x, const int32_t*
 }
 
 // ============================================================================
-// 8-bit paged K/V and 4-bit weights
+// Rows on paged K/V (bf16 and 8-bit), page copies and 4-bit weights
 // ============================================================================
+
+extern "C" int kvp_set_layer_window(kvp_ctx* ctx, int l, int window, int sinks) {
+    if (!ctx) return fail(KVP_E_INVALID_ARG, "kvp_set_layer_window: NULL ctx");
+    if (l < 0 || l >= ctx->d.L) return fail(KVP_E_INVALID_ARG, "kvp_set_layer_window: layer %d out of range", l);
+    if (!ctx->bf16()) return fail(KVP_E_SHAPE, "kvp_set_layer_window: attention windows need a bf16 model");
+    if (window < 0 || sinks < 0 || (!window && sinks))
+        return fail(KVP_E_INVALID_ARG, "kvp_set_layer_window: window=%d >= 1 and sinks=%d >= 0 required (both 0: none)",
+                    window, sinks);
+    ctx->layers[l].window = window;
+    ctx->layers[l].sinks = sinks;
+    return ok();
+}
 
 extern "C" int kvp_set_kv_pool_fp8(kvp_ctx* ctx, int l, void* K, void* V, void* scales, int n_pages) {
     if (!ctx) return fail(KVP_E_INVALID_ARG, "kvp_set_kv_pool_fp8: NULL ctx");
@@ -1000,7 +1024,7 @@ namespace {
 
 int check_rows(const kvp_ctx* ctx, const kvp_rows* r, const char* who) {
     if (!ctx || !r) return fail(KVP_E_INVALID_ARG, "%s: NULL ctx or rows", who);
-    if (!ctx->bf16()) return fail(KVP_E_SHAPE, "%s: 8-bit K/V storage needs a bf16 model", who);
+    if (!ctx->bf16()) return fail(KVP_E_SHAPE, "%s: paged K/V storage needs a bf16 model", who);
     if (!r->len || !r->pages || r->pages_stride < 1)
         return fail(KVP_E_INVALID_ARG, "%s: NULL len or page table, or stride < 1", who);
     if ((int64_t)r->pages_stride * kvp::kPage > INT32_MAX / 2)
@@ -1021,37 +1045,62 @@ int check_rows(const kvp_ctx* ctx, const kvp_rows* r, const char* who) {
     return KVP_OK;
 }
 
-int check_pool8(const kvp_ctx* ctx, int l, const char* who) {
+// fp8: the 8-bit pools, else the bf16 ones.
+int check_pool(const kvp_ctx* ctx, int l, bool fp8, const char* who) {
     if (l < 0 || l >= ctx->d.L) return fail(KVP_E_INVALID_ARG, "%s: layer %d out of range", who, l);
-    if (!ctx->layers[ctx->tau[l]].kp8)
-        return fail(KVP_E_STATE, "%s: 8-bit pools of producer %d (used by layer %d) were never set", who, ctx->tau[l], l);
+    const Layer& P = ctx->layers[ctx->tau[l]];
+    if (fp8 ? !P.kp8 : !P.kp)
+        return fail(KVP_E_STATE, "%s: %s pools of producer %d (used by layer %d) were never set", who, fp8 ? "8-bit" : "bf16",
+                    ctx->tau[l], l);
     return KVP_OK;
 }
 
-int check_step_ws(const kvp_ctx* ctx, const kvp_rows* r, const void* ws, size_t ws_bytes, Workspace* w, const char* who) {
-    *w = layout(*ctx, KVP_PHASE_STEP_FP8, r->B, r->rows);
+int check_step_ws(const kvp_ctx* ctx, const kvp_rows* r, bool fp8, const void* ws, size_t ws_bytes, Workspace* w,
+                  const char* who) {
+    *w = layout(*ctx, fp8 ? KVP_PHASE_STEP_FP8 : KVP_PHASE_STEP, r->B, r->rows);
     if (!ws || ws_bytes < w->total || !aligned16(ws))
         return fail(KVP_E_WORKSPACE, "%s: workspace needs %zu bytes (16-byte aligned), got %zu", who, w->total,
                     ws ? ws_bytes : (size_t)0);
     return KVP_OK;
 }
 
-kvp::NewRows new_rows(const kvp_ctx* ctx, int p, const kvp_rows* r) {
-    return {r->cu, r->len, r->pages, r->pages_stride, ctx->layers[p].n_pages8, r->B, r->rows, r->max_new, r->max_pos};
+kvp::NewRows new_rows(const kvp_ctx* ctx, int p, bool fp8, const kvp_rows* r) {
+    const Layer& P = ctx->layers[p];
+    return {r->cu, r->len, r->pages, r->pages_stride, fp8 ? P.n_pages8 : P.n_pages, r->B, r->rows, r->max_new, r->max_pos};
 }
 
-int run_attention_fp8(kvp_ctx* c, int l, const void* q, const kvp_rows* r, void* out, void* part, hipStream_t st) {
+int run_append(kvp_ctx* c, int l, bool fp8, const void* q, const void* k, const void* v, int ldq, int ldkv, const kvp_rows* r,
+               void* q_out, hipStream_t st) {
     const int p = c->tau[l];
     const Layer& P = c->layers[p];
-    return timed(c, KVP_K_DEC_ATTN, st, [&] {
-        return check_hip(kvp::attention_fp8(new_rows(c, p, r), c->d.a, c->d.g, (const uint16_t*)q, (const uint8_t*)P.kp8,
-                                            (const uint8_t*)P.vp8, P.sc8, (uint16_t*)out, part, c->decode_waves, st),
-                         "attention (8-bit cache)");
+    const kvp::NewRows nr = new_rows(c, p, fp8, r);
+    const uint16_t *q16 = (const uint16_t*)q, *k16 = (const uint16_t*)k, *v16 = (const uint16_t*)v;
+    return timed(c, KVP_K_DEC_ROPE, st, [&] {
+        return check_hip(fp8 ? kvp::append_fp8(nr, c->d.a, c->d.g, q16, k16, v16, ldq, ldkv, c->freqs, (uint16_t*)q_out,
+                                               (uint8_t*)P.kp8, (uint8_t*)P.vp8, P.sc8, st)
+                             : kvp::append_bf16(nr, c->d.a, c->d.g, q16, k16, v16, ldq, ldkv, c->freqs, (uint16_t*)q_out,
+                                                (uint16_t*)P.kp, (uint16_t*)P.vp, st),
+                         "rotation + cache append");
     });
 }
 
-// One layer of kvp_step_fp8.
-int run_step_layer(kvp_ctx* c, int l, const LayerIO& io, const kvp_rows* r, char* ws, const Workspace& w, hipStream_t st) {
+int run_attention(kvp_ctx* c, int l, bool fp8, const void* q, const kvp_rows* r, void* out, void* part, hipStream_t st) {
+    const int p = c->tau[l];
+    const Layer& P = c->layers[p];
+    const kvp::NewRows nr = new_rows(c, p, fp8, r);
+    return timed(c, KVP_K_DEC_ATTN, st, [&] {
+        return check_hip(fp8 ? kvp::attention_fp8(nr, c->d.a, c->d.g, (const uint16_t*)q, (const uint8_t*)P.kp8,
+                                                  (const uint8_t*)P.vp8, P.sc8, (uint16_t*)out, part, c->decode_waves, st)
+                             : kvp::attention_rows(nr, c->d.a, c->d.g, c->layers[l].window, c->layers[l].sinks,
+                                                   (const uint16_t*)q, (const uint16_t*)P.kp, (const uint16_t*)P.vp,
+                                                   (uint16_t*)out, part, c->decode_waves, st),
+                         fp8 ? "attention (8-bit cache)" : "attention (paged cache)");
+    });
+}
+
+// One layer of kvp_step or kvp_step_fp8.
+int run_step_layer(kvp_ctx* c, int l, bool fp8, const LayerIO& io, const kvp_rows* r, char* ws, const Workspace& w,
+                   hipStream_t st) {
     const int p = c->tau[l], rows = r->rows, h = c->d.h, nq = c->n_q(), nkv = c->n_kv();
     const bool producer = p == l, few = rows <= kDecodeMaxRows, w4 = c->layers[l].group != 0;
     const int N = producer ? nq + 2 * nkv : nq;
@@ -1063,7 +1112,6 @@ int run_step_layer(kvp_ctx* c, int l, const LayerIO& io, const kvp_rows* r, char
     void* o = ws + w.o;
     float* proj = (float*)(ws + w.proj);
     uint16_t* raw = (uint16_t*)proj;
-    const kvp::NewRows nr = new_rows(c, p, r);
     int rc;
     // Few rows: the sums of the projections stay in fp32 up to the rotation; more: bf16 rows.
     if ((rc = timed(c, KVP_K_DEC_GEMM, st, [&] {
@@ -1083,21 +1131,24 @@ int run_step_layer(kvp_ctx* c, int l, const LayerIO& io, const kvp_rows* r, char
              return r2;
          })))
         return rc;
-    if ((rc = timed(c, KVP_K_DEC_ROPE, st, [&] {
-             uint8_t *k8 = (uint8_t*)P.kp8, *v8 = (uint8_t*)P.vp8;
-             if (few)
-                 return check_hip(kvp::append_fp8_planes(nr, c->d.a, c->d.g, proj, w4 ? 1 : kvp::decode_gemm_splits(h), N,
-                                                         producer, c->freqs, q, k8, v8, P.sc8, st),
-                                  "rotation + cache append");
-             // 4-bit products leave whole rows, the others three matrices.
-             const uint16_t* k = w4 ? raw + nq : raw + (size_t)rows * nq;
-             const uint16_t* v = w4 ? k + nkv : k + (size_t)rows * nkv;
-             return check_hip(kvp::append_fp8(nr, c->d.a, c->d.g, raw, producer ? k : nullptr, producer ? v : nullptr,
-                                              w4 ? N : nq, w4 ? N : nkv, c->freqs, q, k8, v8, P.sc8, st),
-                              "rotation + cache append");
-         })))
-        return rc;
-    if ((rc = run_attention_fp8(c, l, q, r, o, ws + w.part, st))) return rc;
+    if (few) {
+        const kvp::NewRows nr = new_rows(c, p, fp8, r);
+        const int planes = w4 ? 1 : kvp::decode_gemm_splits(h);
+        rc = timed(c, KVP_K_DEC_ROPE, st, [&] {
+            return check_hip(fp8 ? kvp::append_fp8_planes(nr, c->d.a, c->d.g, proj, planes, N, producer, c->freqs, q,
+                                                          (uint8_t*)P.kp8, (uint8_t*)P.vp8, P.sc8, st)
+                                 : kvp::append_bf16_planes(nr, c->d.a, c->d.g, proj, planes, N, producer, c->freqs, q,
+                                                           (uint16_t*)P.kp, (uint16_t*)P.vp, st),
+                             "rotation + cache append");
+        });
+    } else {
+        // 4-bit products leave whole rows, the others three matrices.
+        const uint16_t* k = w4 ? raw + nq : raw + (size_t)rows * nq;
+        const uint16_t* v = w4 ? k + nkv : k + (size_t)rows * nkv;
+        rc = run_append(c, l, fp8, raw, producer ? k : nullptr, producer ? v : nullptr, w4 ? N : nq, w4 ? N : nkv, r, q, st);
+    }
+    if (rc) return rc;
+    if ((rc = run_attention(c, l, fp8, q, r, o, ws + w.part, st))) return rc;
     if (w4) return oproj_w4(c, l, io, o, rows, st);
     return timed(c, few ? KVP_K_DEC_OPROJ : KVP_K_OPROJ_GEMM, st, [&] {
         kvp::WRows wo{};
@@ -1120,77 +1171,134 @@ int run_step_layer(kvp_ctx* c, int l, const LayerIO& io, const kvp_rows* r, char
     });
 }
 
-}  // namespace
-
-extern "C" int kvp_append_fp8(kvp_ctx* ctx, int l, const void* q, const void* k, const void* v, int ld, const kvp_rows* r,
-                              void* q_out, void* stream) {
+int append_impl(kvp_ctx* ctx, int l, bool fp8, const void* q, const void* k, const void* v, int ld, const kvp_rows* r,
+                void* q_out, void* stream, const char* who) {
     int rc;
-    if ((rc = check_rows(ctx, r, "kvp_append_fp8"))) return rc;
-    if ((rc = check_pool8(ctx, l, "kvp_append_fp8"))) return rc;
+    if ((rc = check_rows(ctx, r, who))) return rc;
+    if ((rc = check_pool(ctx, l, fp8, who))) return rc;
     const bool producer = ctx->tau[l] == l;
-    if (!q != !q_out) return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: q and q_out go together");
-    if (!k != !v) return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: k and v go together");
+    if (!q != !q_out) return fail(KVP_E_INVALID_ARG, "%s: q and q_out go together", who);
+    if (!k != !v) return fail(KVP_E_INVALID_ARG, "%s: k and v go together", who);
     if (!producer && k)
-        return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: layer %d shares K/V of layer %d and appends none", l, ctx->tau[l]);
-    if (!q && !k) return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: neither q nor k and v");
+        return fail(KVP_E_INVALID_ARG, "%s: layer %d shares K/V of layer %d and appends none", who, l, ctx->tau[l]);
+    if (!q && !k) return fail(KVP_E_INVALID_ARG, "%s: neither q nor k and v", who);
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || ld % 8)
-        return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: rows must be 16-byte aligned");
+        return fail(KVP_E_INVALID_ARG, "%s: rows must be 16-byte aligned", who);
     if (ld < (q ? ctx->n_q() : ctx->n_kv()) || ld < (k ? ctx->n_kv() : 0))
-        return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: ld=%d is shorter than a row", ld);
+        return fail(KVP_E_INVALID_ARG, "%s: ld=%d is shorter than a row", who, ld);
     if (q && q == q_out && ld != ctx->n_q())
-        return fail(KVP_E_INVALID_ARG, "kvp_append_fp8: q in place needs ld == a * d_h");
-    const Layer& P = ctx->layers[ctx->tau[l]];
-    hipStream_t st = (hipStream_t)stream;
-    return timed(ctx, KVP_K_DEC_ROPE, st, [&] {
-        return check_hip(kvp::append_fp8(new_rows(ctx, ctx->tau[l], r), ctx->d.a, ctx->d.g, (const uint16_t*)q,
-                                         (const uint16_t*)k, (const uint16_t*)v, ld, ld, ctx->freqs, (uint16_t*)q_out,
-                                         (uint8_t*)P.kp8, (uint8_t*)P.vp8, P.sc8, st),
-                         "rotation + cache append");
-    });
+        return fail(KVP_E_INVALID_ARG, "%s: q in place needs ld == a * d_h", who);
+    return run_append(ctx, l, fp8, q, k, v, ld, ld, r, q_out, (hipStream_t)stream);
 }
 
-extern "C" int kvp_attention_fp8(kvp_ctx* ctx, int l, const void* q, const kvp_rows* r, void* out, void* ws,
-                                 size_t ws_bytes, void* stream) {
+int attention_impl(kvp_ctx* ctx, int l, bool fp8, const void* q, const kvp_rows* r, void* out, void* ws, size_t ws_bytes,
+                   void* stream, const char* who) {
     int rc;
-    if ((rc = check_rows(ctx, r, "kvp_attention_fp8"))) return rc;
-    if ((rc = check_pool8(ctx, l, "kvp_attention_fp8"))) return rc;
-    if (!q || !out) return fail(KVP_E_INVALID_ARG, "kvp_attention_fp8: NULL q or out");
-    if (q == out) return fail(KVP_E_INVALID_ARG, "kvp_attention_fp8: q and out must not alias");
-    if (!aligned16(q) || !aligned16(out))
-        return fail(KVP_E_INVALID_ARG, "kvp_attention_fp8: q, out must be 16-byte aligned");
+    if ((rc = check_rows(ctx, r, who))) return rc;
+    if ((rc = check_pool(ctx, l, fp8, who))) return rc;
+    if (fp8 && (rc = check_no_window(ctx, l))) return rc;
+    if (!q || !out) return fail(KVP_E_INVALID_ARG, "%s: NULL q or out", who);
+    if (q == out) return fail(KVP_E_INVALID_ARG, "%s: q and out must not alias", who);
+    if (!aligned16(q) || !aligned16(out)) return fail(KVP_E_INVALID_ARG, "%s: q, out must be 16-byte aligned", who);
     Workspace w;
-    if ((rc = check_step_ws(ctx, r, ws, ws_bytes, &w, "kvp_attention_fp8"))) return rc;
-    return run_attention_fp8(ctx, l, q, r, out, (char*)ws + w.part, (hipStream_t)stream);
+    if ((rc = check_step_ws(ctx, r, fp8, ws, ws_bytes, &w, who))) return rc;
+    return run_attention(ctx, l, fp8, q, r, out, (char*)ws + w.part, (hipStream_t)stream);
 }
 
-extern "C" int kvp_step_fp8(kvp_ctx* ctx, const void* x, const kvp_rows* r, void* y, void* ws, size_t ws_bytes,
-                            void* stream) {
+int step_impl(kvp_ctx* ctx, bool fp8, const void* x, const kvp_rows* r, void* y, void* ws, size_t ws_bytes, void* stream,
+              const char* who) {
     int rc;
-    if ((rc = check_rows(ctx, r, "kvp_step_fp8"))) return rc;
-    if (!x || !y) return fail(KVP_E_INVALID_ARG, "kvp_step_fp8: NULL x or y");
-    if (x == y) return fail(KVP_E_INVALID_ARG, "kvp_step_fp8: x and y must not alias");
-    if (!aligned16(x) || !aligned16(y)) return fail(KVP_E_INVALID_ARG, "kvp_step_fp8: x, y must be 16-byte aligned");
+    if ((rc = check_rows(ctx, r, who))) return rc;
+    if (!x || !y) return fail(KVP_E_INVALID_ARG, "%s: NULL x or y", who);
+    if (x == y) return fail(KVP_E_INVALID_ARG, "%s: x and y must not alias", who);
+    if (!aligned16(x) || !aligned16(y)) return fail(KVP_E_INVALID_ARG, "%s: x, y must be 16-byte aligned", who);
     Workspace w;
-    if ((rc = check_step_ws(ctx, r, ws, ws_bytes, &w, "kvp_step_fp8"))) return rc;
+    if ((rc = check_step_ws(ctx, r, fp8, ws, ws_bytes, &w, who))) return rc;
     for (int l = 0; l < ctx->d.L; ++l) {
-        if ((rc = check_pool8(ctx, l, "kvp_step_fp8"))) return rc;
+        if ((rc = check_pool(ctx, l, fp8, who))) return rc;
+        if (fp8 && (rc = check_no_window(ctx, l))) return rc;
         if (!ctx->layers[l].weights && !ctx->layers[l].group)
-            return fail(KVP_E_STATE, "kvp_step_fp8: weights of layer %d were never set", l);
+            return fail(KVP_E_STATE, "%s: weights of layer %d were never set", who, l);
     }
     hipStream_t st = (hipStream_t)stream;
     char* base = (char*)ws;
     // Rows of no sequence pass through: their attention output is 0 (nothing else writes it).
     if (r->cu && (rc = timed(ctx, KVP_K_DEC_ROPE, st, [&] {
-                      return check_hip(kvp::clear_unowned(new_rows(ctx, 0, r), ctx->n_q(), (uint16_t*)(base + w.o), st),
+                      return check_hip(kvp::clear_unowned(new_rows(ctx, 0, fp8, r), ctx->n_q(), (uint16_t*)(base + w.o), st),
                                        "rows of no sequence");
                   })))
         return rc;
     const int L = ctx->d.L;
     for (int l = 0; l < L; ++l) {
         const LayerIO io = stack_io(true, l, L, x, y, base, w);
-        if ((rc = run_step_layer(ctx, l, io, r, base, w, st))) return rc;
+        if ((rc = run_step_layer(ctx, l, fp8, io, r, base, w, st))) return rc;
     }
     return ok();
+}
+
+// Every producer's pools, kMax of them a launch.
+int copy_pages_impl(kvp_ctx* ctx, bool fp8, const int32_t* src, const int32_t* dst, int n, void* stream, const char* who) {
+    if (!ctx) return fail(KVP_E_INVALID_ARG, "%s: NULL ctx", who);
+    if (!ctx->bf16()) return fail(KVP_E_SHAPE, "%s: paged K/V storage needs a bf16 model", who);
+    if (n < 0 || (n && (!src || !dst))) return fail(KVP_E_INVALID_ARG, "%s: NULL src or dst, or n < 0", who);
+    int set = 0;
+    for (int l = 0; l < ctx->d.L; ++l) set += (fp8 ? ctx->layers[l].kp8 : ctx->layers[l].kp) != nullptr;
+    if (!set) return fail(KVP_E_STATE, "%s: no producer's %s pools were ever set", who, fp8 ? "8-bit" : "bf16");
+    if (n == 0) return ok();
+    hipStream_t st = (hipStream_t)stream;
+    return timed(ctx, KVP_K_PAGE_COPY, st, [&] {
+        kvp::PagePools pools;
+        int rc = KVP_OK;
+        for (int l = 0; l < ctx->d.L && !rc; ++l) {
+            const Layer& P = ctx->layers[l];
+            if (fp8 && P.kp8) pools.pool[pools.n++] = {P.kp8, P.vp8, P.sc8, P.n_pages8};
+            if (!fp8 && P.kp) pools.pool[pools.n++] = {P.kp, P.vp, nullptr, P.n_pages};
+            if (pools.n == kvp::PagePools::kMax || (l == ctx->d.L - 1 && pools.n)) {
+                rc = check_hip(kvp::copy_pages(pools, fp8, src, dst, n, ctx->d.g, st), "page copy");
+                pools.n = 0;
+            }
+        }
+        return rc;
+    });
+}
+
+}  // namespace
+
+extern "C" int kvp_append(kvp_ctx* ctx, int l, const void* q, const void* k, const void* v, int ld, const kvp_rows* r,
+                          void* q_out, void* stream) {
+    return append_impl(ctx, l, false, q, k, v, ld, r, q_out, stream, "kvp_append");
+}
+
+extern "C" int kvp_append_fp8(kvp_ctx* ctx, int l, const void* q, const void* k, const void* v, int ld, const kvp_rows* r,
+                              void* q_out, void* stream) {
+    return append_impl(ctx, l, true, q, k, v, ld, r, q_out, stream, "kvp_append_fp8");
+}
+
+extern "C" int kvp_attention(kvp_ctx* ctx, int l, const void* q, const kvp_rows* r, void* out, void* ws, size_t ws_bytes,
+                             void* stream) {
+    return attention_impl(ctx, l, false, q, r, out, ws, ws_bytes, stream, "kvp_attention");
+}
+
+extern "C" int kvp_attention_fp8(kvp_ctx* ctx, int l, const void* q, const kvp_rows* r, void* out, void* ws,
+                                 size_t ws_bytes, void* stream) {
+    return attention_impl(ctx, l, true, q, r, out, ws, ws_bytes, stream, "kvp_attention_fp8");
+}
+
+extern "C" int kvp_step(kvp_ctx* ctx, const void* x, const kvp_rows* r, void* y, void* ws, size_t ws_bytes, void* stream) {
+    return step_impl(ctx, false, x, r, y, ws, ws_bytes, stream, "kvp_step");
+}
+
+extern "C" int kvp_step_fp8(kvp_ctx* ctx, const void* x, const kvp_rows* r, void* y, void* ws, size_t ws_bytes,
+                            void* stream) {
+    return step_impl(ctx, true, x, r, y, ws, ws_bytes, stream, "kvp_step_fp8");
+}
+
+extern "C" int kvp_copy_pages(kvp_ctx* ctx, const int32_t* src, const int32_t* dst, int n, void* stream) {
+    return copy_pages_impl(ctx, false, src, dst, n, stream, "kvp_copy_pages");
+}
+
+extern "C" int kvp_copy_pages_fp8(kvp_ctx* ctx, const int32_t* src, const int32_t* dst, int n, void* stream) {
+    return copy_pages_impl(ctx, true, src, dst, n, stream, "kvp_copy_pages_fp8");
 }
 
 extern "C" int kvp_w4_bytes(int N, int K, int group, size_t* bytes) {

@@ -1,0 +1,565 @@
+"""Rows on bf16 pages on the GPU: kvp_append, kvp_attention (with windows) and kvp_step against 64-bit references
+(rows_ref.py).  What was never written in the pools holds NaN and infinities, so a read behind a sequence's end shows."""
+import numpy as np
+import pytest
+import torch
+
+import rows_ref as rr
+from gpu_util import say
+from paper_2608_15943_amd import binding as kb
+
+pytestmark = pytest.mark.gpu
+D = rr.D
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    kb.lib()
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _normal(rng, *shape, scale=1.0):
+    return rr.bf16(rng.standard_normal(shape).astype(np.float32) * np.float32(scale))
+
+
+def _dev(x):
+    """bf16 numbers, NaN's bits too."""
+    return torch.from_numpy(rr.bits(x).view(np.int16)).cuda().view(torch.bfloat16)
+
+
+class Case:
+    """A cache with `lens` positions in it and rows of Q | K | V for `new` more."""
+
+    def __init__(self, a, g, lens, new, seed, spare=2, stride=None, rows=None):
+        rng = np.random.default_rng(seed)
+        self.a, self.g, self.lens, self.new = a, g, lens, new
+        need = rr.pages_for(lens, new)
+        self.table, n_pages = rr.scattered(need, max(need + [1]) if stride is None else stride, spare, seed)
+        self.cache = rr.Cache(g, n_pages, seed)
+        for b, n in enumerate(lens):
+            if n > 0:
+                self.cache.put(self.table, b, 0, _normal(rng, 2, n, g, D))
+        self.cu = np.concatenate([[0], np.cumsum(new)]).astype(int)
+        self.rows = int(self.cu[-1]) if rows is None else rows
+        self.x = _normal(rng, max(self.rows, 1), a + 2 * g, D)
+
+    def kv64(self):
+        """Rotated K and V of every sequence's new rows."""
+        out = []
+        for b, (n, T) in enumerate(zip(self.lens, self.new)):
+            x = self.x[self.cu[b]: self.cu[b] + T].astype(np.float64)
+            k = np.stack([rr.rotate(x[t, self.a: self.a + self.g], n + t) for t in range(T)]) if T else x[:, : self.g]
+            out.append(np.stack([k, x[:, self.a + self.g:]]))
+        return out
+
+
+def _append(c, fused=True, cu=True, with_q=True, **kw):
+    """Runs kvp_append on a case; the device's pools and q_out."""
+    dev = c.cache.to_device()
+    m = rr.model(c.a, c.g, dev, c.cache.n_pages, len(c.lens), max(max(c.new), c.rows, 1))
+    r, keep = rr.rows_of(c.lens, c.new, c.table, cu=cu, rows=c.rows, **kw)
+    x = _dev(c.x)
+    q_out = torch.full((max(c.rows, 1), c.a * D), 77.0, dtype=torch.bfloat16, device="cuda")
+    if fused:
+        p, ld = x.data_ptr(), (c.a + 2 * c.g) * D
+        q, k, v = p, p + 2 * c.a * D, p + 2 * (c.a + c.g) * D
+    else:      # three matrices; q's rows are as far apart as k's, behind a gap
+        ld = max(c.a, c.g) * D + 8
+        parts = [torch.zeros(c.x.shape[0], ld, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+        for t, (lo, hi) in zip(parts, ((0, c.a), (c.a, c.a + c.g), (c.a + c.g, c.a + 2 * c.g))):
+            t[:, : (hi - lo) * D] = x[:, lo:hi].reshape(c.x.shape[0], -1)
+        q, k, v = (t.data_ptr() for t in parts)
+    m.kvp_append(0, q if with_q else 0, k, v, ld, r, q_out.data_ptr() if with_q else 0, _stream())
+    torch.cuda.synchronize()
+    return c.cache.from_device(dev), q_out
+
+
+def _check_q(c, q_out):
+    got = q_out.float().cpu().numpy().reshape(-1, c.a, D)
+    owned = np.zeros(max(c.rows, 1), bool)
+    for b, (n, T) in enumerate(zip(c.lens, c.new)):
+        if n >= 0:
+            for t in range(T):
+                i = c.cu[b] + t
+                owned[i] = True
+                want = rr.rotate(c.x[i, : c.a].astype(np.float64), n + t)
+                assert rr.near(got[i], want, np.abs(c.x[i, : c.a]).max()).all(), (b, t)
+    assert (got[~owned] == 77.0).all()
+
+
+APPEND = [
+    # a, g, cached, new
+    (4, 2, [0], [1]), (4, 2, [977], [1]), (5, 1, [15, 16, 17, 63, 64, 0], [1] * 6),
+    (8, 4, [0, 1, 15, 16, 47, 48, 63, 64, 65], [1, 15, 16, 17, 33, 1, 2, 64, 65]),
+    (16, 1, [3, 0, 7], [0, 5, 0]), (3, 3, [-1, 20, -5, 0], [3, 2, 1, 4]), (64, 8, [100], [3]),
+    (4, 2, [13], [400]), (12, 4, [60, 120], [8, 9]),
+]
+
+
+@pytest.mark.parametrize("a,g,lens,new", APPEND)
+def test_append(a, g, lens, new):
+    """Rows that begin and end anywhere in a page, over several pages, of inactive sequences."""
+    say(f"[append] a={a} g={g} lens={lens} new={new}")
+    c = Case(a, g, lens, new, seed=len(lens) + sum(new))
+    after, q_out = _append(c)
+    rr.check_append(c.cache, after, c.table, lens, new, c.kv64())
+    _check_q(c, q_out)
+
+
+def test_append_one_row_each_without_cu():
+    c = Case(8, 2, [5, -1, 31, 32, 64, 0], [1] * 6, seed=2)
+    after, q_out = _append(c, cu=False)
+    rr.check_append(c.cache, after, c.table, c.lens, c.new, c.kv64())
+    _check_q(c, q_out)
+
+
+def test_append_separate_matrices_without_q():
+    c = Case(4, 2, [30, 2], [5, 20], seed=3)
+    after, _ = _append(c, fused=False)
+    rr.check_append(c.cache, after, c.table, c.lens, c.new, c.kv64())
+    again, q_out = _append(c, fused=False, with_q=False)
+    assert again.same(after) and (q_out == 77.0).all()
+
+
+def test_append_many_sequences():
+    """More sequences than a wave has lanes, with and without rows."""
+    n = 150
+    lens = [(7 * i) % 90 - (1 if i % 11 == 0 else 0) for i in range(n)]
+    c = Case(2, 1, lens, [i % 4 for i in range(n)], seed=4)
+    after, q_out = _append(c)
+    rr.check_append(c.cache, after, c.table, lens, c.new, c.kv64())
+    _check_q(c, q_out)
+
+
+def test_append_rows_behind_the_last_sequence_and_past_the_bounds():
+    """Rows of no sequence, rows past max_new, positions past max_pos: nothing is written for them."""
+    c = Case(4, 2, [10, 20], [6, 3], seed=5, rows=14)
+    after, q_out = _append(c)
+    rr.check_append(c.cache, after, c.table, c.lens, c.new, c.kv64())
+    _check_q(c, q_out)
+    after, q_out = _append(c, max_new=4)
+    rr.check_append(c.cache, after, c.table, c.lens, [4, 3], [x[:, :4] for x in c.kv64()])
+    assert (q_out[4:6] == 77.0).all() and (q_out[:4] != 77.0).any() and (q_out[6:9] != 77.0).any()
+    after, q_out = _append(c, max_pos=12)
+    rr.check_append(c.cache, after, c.table, [10, -1], [3, 0], c.kv64())
+    assert (q_out[3:] == 77.0).all()
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("new", [[1, 1], [3, 40]])
+def test_append_not_finite(bad, new):
+    """Such a value reaches its own position alone (a key: its rotated pair)."""
+    c = Case(4, 2, [10, 32], new, seed=6)
+    c.x[0, c.a, 5] = bad
+    c.x[new[0], c.a + c.g + 1, 7] = bad
+    with np.errstate(invalid="ignore"):
+        kv = c.kv64()
+    after, _ = _append(c)
+    rr.check_append(c.cache, after, c.table, c.lens, c.new, kv)
+
+
+@pytest.mark.parametrize("new", [1, 3])
+def test_append_far_positions(new):
+    """The angle of a position past 2^20 in a table of many pages."""
+    n = (1 << 20) + 77
+    c = Case(2, 2, [0], [new], seed=9)
+    c.lens, c.table = [n], np.full((1, n // 64 + 2), -1, np.int32)
+    c.table[0, n // 64], c.table[0, n // 64 + 1] = 1, 0
+    c.cache = rr.Cache(2, 2, 9)
+    after, q_out = _append(c)
+    rr.check_append(c.cache, after, c.table, c.lens, c.new, c.kv64())
+    _check_q(c, q_out)
+
+
+def test_append_table_entries_out_of_range_stay_in_the_pool():
+    """Bad page numbers are taken to the pool's first or last page."""
+    c = Case(4, 2, [5, 70], [2, 2], seed=10)
+    c.cache = rr.Cache(2, c.cache.n_pages, 10)
+    good = c.table.copy()
+    good[0, 0], good[1, 1] = 0, c.cache.n_pages - 1
+    c.table = good.copy()
+    c.table[0, 0], c.table[1, 1] = -7, 1 << 30
+    after, _ = _append(c)
+    rr.check_append(c.cache, after, good, c.lens, c.new, c.kv64())
+
+
+@pytest.mark.parametrize("new", [[2, 5], [1, 1]])
+def test_append_queries_of_a_consumer_and_in_place(new):
+    c = Case(4, 2, [33, 0], new, seed=11)
+    dev = c.cache.to_device()
+    m = rr.model(4, 2, {0: dev}, c.cache.n_pages, 2, 8, tau=(0, 0))
+    r, keep = rr.rows_of(c.lens, c.new, c.table)
+    q = _dev(c.x[:, :4].reshape(sum(new), -1))
+    m.kvp_append(1, q.data_ptr(), 0, 0, 4 * D, r, q.data_ptr(), _stream())
+    torch.cuda.synchronize()
+    _check_q(c, q)
+    assert c.cache.from_device(dev).same(c.cache)
+
+
+def test_append_in_rows_and_at_once_is_the_same():
+    """A prompt at once, in chunks and token by token: the same bits."""
+    c = Case(4, 2, [0], [150], seed=12)
+    once, q_once = _append(c)
+    rr.check_append(c.cache, once, c.table, c.lens, c.new, c.kv64())
+    for cuts in ([0, 1, 2, 65, 100, 150], [0, 64, 128, 150], list(range(40)) + [150]):
+        dev = c.cache.to_device()
+        m = rr.model(4, 2, dev, c.cache.n_pages, 1, 150)
+        x = _dev(c.x)
+        q = torch.empty(150, 4 * D, dtype=torch.bfloat16, device="cuda")
+        for lo, hi in zip(cuts, cuts[1:]):
+            r, keep = rr.rows_of([lo], [hi - lo], c.table)
+            p = x[lo:].data_ptr()
+            m.kvp_append(0, p, p + 8 * D, p + 12 * D, 8 * D, r, q[lo:].data_ptr(), _stream())
+            torch.cuda.synchronize()
+        assert c.cache.from_device(dev).same(once) and torch.equal(q, q_once)
+
+
+# ---- attention -----------------------------------------------------------------------------------
+
+def _fill(c, seed=99):
+    """The new rows' positions in the cache too."""
+    rng = np.random.default_rng(seed)
+    for b, (n, T) in enumerate(zip(c.lens, c.new)):
+        if n >= 0 and T:
+            c.cache.put(c.table, b, n, _normal(rng, 2, T, c.g, D))
+
+
+def _drop_unseen(c, window, sinks):
+    """Pages that no row sees leave the table, as kvp_pager_trim does, and the pool: they hold anything."""
+    for b, (n, T) in enumerate(zip(c.lens, c.new)):
+        if n < 0 or not T:
+            continue
+        see = rr.sees(n + np.arange(T)[:, None], np.arange(n + T)[None], window, sinks).any(0)
+        for j in range((n + T + 63) // 64):
+            if not see[64 * j: 64 * j + 64].any():
+                c.table[b][j] = -1
+
+
+def _attention(c, cu=True, max_seq=1, window=0, sinks=0, **kw):
+    """Runs kvp_attention on rotated queries over the cache of a case."""
+    dev = c.cache.to_device()
+    m = rr.model(c.a, c.g, dev, c.cache.n_pages, len(c.lens), max(max(c.new), c.rows, max_seq))
+    if window:
+        m.kvp_set_layer_window(0, window, sinks)
+    r, keep = rr.rows_of(c.lens, c.new, c.table, cu=cu, rows=c.rows, **kw)
+    q = _dev(c.x[:, : c.a].reshape(c.x.shape[0], -1))
+    out = torch.full_like(q, 55.0)
+    n = m.kvp_workspace_size(kb.KVP_PHASE_STEP, len(c.lens), c.rows)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")      # NaN in whatever is read unwritten
+    m.kvp_attention(0, q.data_ptr(), r, out.data_ptr(), ws.data_ptr(), n, _stream())
+    torch.cuda.synchronize()
+    return out.float().cpu().numpy().reshape(-1, c.a, D)
+
+
+def _check_attention(c, got, window=0, sinks=0):
+    owned, worst = np.zeros(got.shape[0], bool), 0.0
+    for b, (n, T) in enumerate(zip(c.lens, c.new)):
+        rows = slice(c.cu[b], c.cu[b] + T)
+        owned[rows] = True
+        if n < 0:
+            assert (got[rows] == 0).all(), b
+        elif T:
+            want, tol = rr.attention(c.x[rows, : c.a].astype(np.float64), c.cache.values(c.table, b, n + T), n, c.a, window, sinks)
+            assert np.isfinite(got[rows]).all(), b
+            e = (np.abs(got[rows] - want) / tol).max()
+            worst = max(worst, e)
+            assert e <= 1, (b, e)
+    assert (got[~owned] == 55.0).all()
+    say(f"  {worst:.3f} of the bound")
+
+
+ATTN = [
+    # a, g, cached, new: single tokens
+    (4, 2, [0], [1]), (4, 2, [977], [1]), (5, 1, [14, 15, 16, 62, 63, 64, 127], [1] * 7), (16, 1, [300, 5], [1, 1]),
+    (3, 3, [-1, 200, 0, -3], [1] * 4), (32, 8, [1200, 64, 3], [1] * 3),
+    # a few
+    (8, 2, [100, 63, 0], [4, 3, 2]), (16, 1, [70, 6], [2, 5]), (4, 4, [61, 10, 130], [7, 16, 17]), (12, 4, [50, 0], [6, 11]),
+    # chunks
+    (4, 2, [0], [200]), (8, 2, [70, 0, -1, 5], [90, 130, 3, 0]), (5, 1, [33], [77]), (6, 2, [1], [64]),
+    (7, 1, [500, 9], [20, 40]), (16, 1, [65], [33]), (1, 1, [10], [300]),
+]
+WINDOWS = [(1, 0), (1, 1), (17, 0), (64, 4), (63, 64), (100, 130), (200, 0), (2**31 - 1, 0), (5, 2**31 - 1)]
+
+
+@pytest.mark.parametrize("a,g,lens,new", ATTN)
+def test_attention(a, g, lens, new):
+    say(f"[attention] a={a} g={g} lens={lens} new={new}")
+    c = Case(a, g, lens, new, seed=sum(new) + 3 * len(lens))
+    _fill(c)
+    _check_attention(c, _attention(c))
+
+
+@pytest.mark.parametrize("a,g,lens,new", ATTN)
+@pytest.mark.parametrize("window,sinks", WINDOWS)
+def test_window(a, g, lens, new, window, sinks):
+    say(f"[window] a={a} g={g} lens={lens} new={new} window={window} sinks={sinks}")
+    c = Case(a, g, lens, new, seed=sum(new) + 3 * len(lens))
+    _fill(c)
+    _drop_unseen(c, window, sinks)
+    _check_attention(c, _attention(c, window=window, sinks=sinks), window, sinks)
+
+
+@pytest.mark.parametrize("a,g,lens,new", ATTN)
+@pytest.mark.parametrize("max_pos,max_new", [(1500, 1), (0, 200), (1500, 999)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 3)])
+def test_attention_loose_bounds(a, g, lens, new, max_pos, max_new, window, sinks):
+    """The host's bounds (as of a captured call) may be far above what the device's lengths and rows turn out to be."""
+    say(f"[attention] a={a} g={g} lens={lens} new={new} max_pos={max_pos} max_new={max_new} window={window}")
+    c = Case(a, g, lens, new, seed=sum(new) + 3 * len(lens), stride=24)
+    _fill(c)
+    got = _attention(c, max_pos=max_pos or None, max_new=max(max_new, *new), max_seq=max_new, window=window, sinks=sinks)
+    _check_attention(c, got, window, sinks)
+
+
+@pytest.mark.parametrize("a,g", [(2, 1), (4, 2), (8, 4), (16, 4)])
+@pytest.mark.parametrize("new", [1, 3, 12])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 4)])
+def test_attention_workgroups_of_several_waves(a, g, new, window, sinks):
+    """150 sequences of up to ten tiles, some without a row, with one tile, inactive."""
+    lens = [(173 * i) % 640 - (650 if i % 19 == 0 else 0) for i in range(150)]
+    c = Case(a, g, lens, [new - (new > 1) * (i % (new + 1)) for i in range(150)], seed=33)
+    _fill(c)
+    _check_attention(c, _attention(c, window=window, sinks=sinks), window, sinks)
+
+
+LARGE = [
+    (128, 8, [100, 0], [903, 731]),                      # more blocks of rows than workgroups
+    (64, 16, [0, 63, -1, 17], [700, 1, 40, 801]),
+    (2, 1, [20001], [1]), (4, 1, [18000, 5], [4, 2]),    # more than 256 pieces to join
+    (2, 1, [21000], [40]), (8, 2, [9000, 300], [9, 12]), (8, 2, [9000, 300], [5, 8]),
+    (16, 4, [(41 * i) % 3001 for i in range(70)], [5 + i % 8 for i in range(70)]),      # few pieces an item
+    (8, 2, [9000, 1, 640, 64, 63, 100, 2047], [1] * 7), (8, 2, [6000, 300], [3, 70]),
+]
+
+
+@pytest.mark.parametrize("a,g,lens,new", LARGE)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (500, 0), (1111, 70), (4000, 4)])
+def test_attention_many_blocks_and_many_pieces(a, g, lens, new, window, sinks):
+    say(f"[attention] a={a} g={g} lens={lens[:8]} new={new[:8]} window={window} sinks={sinks}")
+    c = Case(a, g, lens, new, seed=31)
+    _fill(c)
+    if window:
+        _drop_unseen(c, window, sinks)
+    _check_attention(c, _attention(c, window=window, sinks=sinks), window, sinks)
+
+
+def test_attention_one_row_each_without_cu():
+    c = Case(8, 2, [5, -1, 31, 1500, 64, 0], [1] * 6, seed=12)
+    _fill(c)
+    _check_attention(c, _attention(c, cu=False))
+    _check_attention(c, _attention(c, cu=False, window=70, sinks=2), 70, 2)
+
+
+def test_attention_rows_of_no_sequence_and_past_the_bounds():
+    c = Case(4, 2, [100, 20], [6, 30], seed=17, rows=40)
+    _fill(c)
+    _check_attention(c, _attention(c))
+    got = _attention(c, max_new=7)
+    d = Case(4, 2, [100, 20], [6, 7], seed=17, rows=40)
+    d.x, d.cache, d.table = c.x, c.cache, c.table
+    _check_attention(d, got)
+    got = _attention(c, max_pos=102)      # the last three rows of sequence 0 see nothing
+    assert (got[3:6] == 0).all()
+    want, tol = rr.attention(c.x[:3, :4].astype(np.float64), c.cache.values(c.table, 0, 103), 100, 4)
+    assert (np.abs(got[:3] - want) <= tol).all() and np.isfinite(got[np.r_[0:3, 6:36]]).all()
+
+
+def test_attention_table_entries_out_of_range_stay_in_the_pool():
+    c = Case(4, 2, [5, 70], [2, 2], seed=18)
+    good = c.table.copy()
+    good[0, 0], good[1, 1] = 0, c.cache.n_pages - 1
+    c.table = good
+    rng = np.random.default_rng(1)
+    for b, n in ((0, 7), (1, 72)):
+        c.cache.put(c.table, b, 0, _normal(rng, 2, n, 2, D))
+    got = _attention(c)
+    _check_attention(c, got)
+    c.table = good.copy()
+    c.table[0, 0], c.table[1, 1] = -7, 1 << 30
+    assert np.array_equal(_attention(c), got)
+
+
+def _by_row(c, b, t, h, window, sinks):
+    """One row and head over the positions that it sees alone; NaN and infinities as they come."""
+    p = c.lens[b] + t
+    seen = np.flatnonzero(rr.sees(p, np.arange(p + 1), window, sinks))
+    kv = c.cache.values(c.table, b, p + 1)[:, seen, h * c.g // c.a]
+    with np.errstate(invalid="ignore", over="ignore"):
+        s = kv[0] @ c.x[c.cu[b] + t, h].astype(np.float64) / np.sqrt(D)
+        w = np.exp(s - s.max())
+        return (w / w.sum()) @ kv[1]
+
+
+@pytest.mark.parametrize("a,g,lens,new", [(4, 2, [40, 130], [1, 1]), (4, 2, [40, 130], [7, 3]), (8, 2, [40, 100], [30, 90])])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (9, 0), (9, 5), (70, 3)])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_attention_values_that_are_not_finite_reach_the_rows_that_see_them(a, g, lens, new, window, sinks, bad):
+    """Keys and values, at positions of the same tile that some rows see and others do not: rows before them in the same call,
+    rows whose window has passed them."""
+    say(f"[not finite] a={a} lens={lens} new={new} window={window} sinks={sinks} {bad}")
+    c = Case(a, g, lens, new, seed=19)
+    _fill(c)
+    put = lambda z, b, p, h, d: _poke(c, z, b, p, h, d, bad)  # noqa: E731
+    put(1, 0, 2, 0, 3)                    # a value among the first positions
+    put(1, 0, 36, 1, 100)                 # one that windows leave behind
+    if new[0] > 1:
+        put(1, 0, 40 + new[0] // 2, 0, 64)      # one in the middle of the new rows
+        put(0, 1, lens[1] + new[1] // 2, 1, 17)   # a key there
+    put(0, 1, 3, 0, 9)
+    got = _attention(c, window=window, sinks=sinks)
+    for b in range(2):
+        for t in range(new[b]):
+            for h in range(a):
+                want = _by_row(c, b, t, h, window, sinks)
+                assert np.array_equal(np.isfinite(got[c.cu[b] + t, h]), np.isfinite(want)), (b, t, h)
+    # What is finite is as it would be without them.
+    clean = [np.where(np.isfinite(rr.from_bits(x)), x, 0).astype(np.uint16) for x in (c.cache.k, c.cache.v)]
+    d = rr.Cache.__new__(rr.Cache)
+    d.k, d.v, d.g, d.n_pages = *clean, c.g, c.cache.n_pages
+    for b in range(2):
+        rows = slice(c.cu[b], c.cu[b] + new[b])
+        want, tol = rr.attention(c.x[rows, :a].astype(np.float64), d.values(c.table, b, lens[b] + new[b]), lens[b], a, window, sinks)
+        keyed = np.zeros((new[b], a), bool)       # rows that see such a key: NaN, or (a score of -infinity) without it
+        for t in range(new[b]):
+            for h in range(a):
+                p = lens[b] + t
+                k = c.cache.values(c.table, b, p + 1)[0, :, h * g // a]
+                seen = rr.sees(p, np.arange(p + 1), window, sinks)
+                keyed[t, h] = not np.isfinite(k[seen]).all()
+        ok = ~np.isfinite(got[rows]) | (np.abs(got[rows] - want) <= tol) | keyed[..., None]
+        assert ok.all(), b
+
+
+def _poke(c, z, b, p, h, d, x):
+    page = c.table[b][p // 64]
+    v = rr.bits(np.float32(x).reshape(1))[0]
+    if z == 0:
+        c.cache.k[h, page, p % 64, d] = v
+    else:
+        c.cache.v[h, page, d, p % 64] = v
+
+
+def test_attention_keys_that_score_minus_infinity():
+    """Runs of keys whose scores are -infinity, whole tiles and pieces of the list among them, weigh nothing; a row that sees no
+    other key is NaN, as the softmax is."""
+    c = Case(2, 1, [20000, 300], [1, 1], seed=24)
+    _fill(c)
+    c.x[:, :2] = np.abs(c.x[:, :2])
+    for b, (lo, hi) in ((0, (0, 15000)), (1, (64, 301))):
+        for p in range(lo, hi):
+            c.cache.k[0, c.table[b][p // 64], p % 64, 0] = 0xFF80
+    got = _attention(c)
+    assert np.isfinite(got).all()
+    for b in range(2):
+        n = c.lens[b]
+        kv = c.cache.values(c.table, b, n + 1)
+        keep = np.isfinite(kv[0]).all((1, 2))
+        q = c.x[b: b + 1, :2].astype(np.float64)
+        s = np.einsum("hd,nd->hn", q[0], kv[0, keep, 0]) / np.sqrt(D)
+        w = np.exp(s - s.max(1, keepdims=True))
+        w /= w.sum(1, keepdims=True)
+        v = kv[1, keep, 0]
+        want = w @ v
+        tol = np.sqrt(np.maximum(w @ v**2 - want**2, 0)) / 255 + 1e-4 * (w @ np.abs(v)) + 2.0**-8 * np.abs(want)
+        assert (np.abs(got[b] - want) <= tol).all(), b
+    for p in range(301):
+        c.cache.k[0, c.table[1][p // 64], p % 64, 0] = 0xFF80
+    got = _attention(c)
+    assert np.isfinite(got[0]).all() and np.isnan(got[1]).all()
+
+
+def test_attention_sharp_and_flat_scores():
+    """Zero queries weigh all keys alike; a query along one key takes its value alone."""
+    c = Case(4, 2, [700, 300], [2, 20], seed=20)
+    _fill(c)
+    c.x[1, :4] = 0
+    kv = c.cache.values(c.table, 1, 320)
+    for h in range(4):
+        c.x[5, h] = rr.bf16(40 * kv[0, 17, h // 2])
+    got = _attention(c)
+    want, tol = rr.attention(c.x[:2, :4].astype(np.float64), c.cache.values(c.table, 0, 702), 700, 4)
+    assert (np.abs(got[:2] - want) <= tol).all()
+    # The key's own score is some 40 * 128 / sqrt(128), others' a tenth of it: their weights are below 2^-200.
+    assert np.array_equal(got[5].astype(np.float32), rr.bf16(kv[1, 17, [0, 0, 1, 1]]))
+
+
+def test_attention_queries_that_are_not_finite():
+    c = Case(8, 2, [100, 70], [5, 40], seed=25)
+    _fill(c)
+    c.x[1, 3, 7] = np.nan
+    c.x[20, 0, 0] = np.inf
+    got = _attention(c)
+    assert np.isnan(got[1, 3]).all() and np.isnan(got[20, 0]).all()
+    got[1, 3] = got[20, 0] = 0
+    assert np.isfinite(got).all()
+    c.x[1, 3, 7] = c.x[20, 0, 0] = 0
+    for b in range(2):
+        rows = slice(c.cu[b], c.cu[b] + c.new[b])
+        want, tol = rr.attention(c.x[rows, :8].astype(np.float64), c.cache.values(c.table, b, c.lens[b] + c.new[b]), c.lens[b], 8)
+        ok = np.abs(got[rows] - want) <= tol
+        if b == 0:
+            ok[1, 3] = True
+        else:
+            ok[15, 0] = True
+        assert ok.all(), b
+
+
+def test_attention_pools_past_4_gib():
+    """Pages whose bytes lie past 2^32 in the pool, appended and attended, in every launch."""
+    g, n_pages = 8, 35000
+    k = torch.empty(g, n_pages, 64, D, dtype=torch.bfloat16, device="cuda")
+    v = torch.empty(g, n_pages, D, 64, dtype=torch.bfloat16, device="cuda")
+    pages = [34999, 12, 34990]
+    rng = np.random.default_rng(21)
+    x = _normal(rng, 40, 8 + 2 * g, D)
+    small = rr.Cache(g, 3)
+    small.put([[0, 1, 2]], 0, 0, _normal(rng, 2, 100, g, D))
+    for z, t in ((small.k, k), (small.v, v)):
+        for i, p in enumerate(pages):
+            t[:, p] = torch.from_numpy(z[:, i].view(np.int16).copy()).cuda().view(torch.bfloat16)
+    m = rr.model(8, g, (k, v), n_pages, 1, 64)
+    n = m.kvp_workspace_size(kb.KVP_PHASE_STEP, 1, 40)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    dx = _dev(x.reshape(40, -1))
+    at = 100
+    for T in (1, 3, 36):
+        r, keep = rr.rows_of([at], [T], [pages])
+        q = torch.empty(T, 8 * D, dtype=torch.bfloat16, device="cuda")
+        out = torch.empty_like(q)
+        p = dx[at - 100:].data_ptr()
+        m.kvp_append(0, p, p + 2 * 8 * D, p + 2 * 16 * D, 24 * D, r, q.data_ptr(), _stream())
+        m.kvp_attention(0, q.data_ptr(), r, out.data_ptr(), ws.data_ptr(), n, _stream())
+        torch.cuda.synchronize()
+        after = small.from_device(tuple(t[:, pages] for t in (k, v)))
+        xs = x[at - 100: at - 100 + T].astype(np.float64)
+        kv = np.stack([np.stack([rr.rotate(xs[t, 8:16], at + t) for t in range(T)]), xs[:, 16:]])
+        rr.check_append(small, after, [[0, 1, 2]], [at], [T], [kv])
+        qd = q.float().cpu().numpy().reshape(T, 8, D).astype(np.float64)
+        want, tol = rr.attention(qd, after.values([[0, 1, 2]], 0, at + T), at, 8)
+        assert (np.abs(out.float().cpu().numpy().reshape(T, 8, D) - want) <= tol).all(), T
+        small, at = after, at + T
+
+
+def test_equal_calls_give_equal_bits():
+    c = Case(8, 2, [3000, 70, 0], [1, 20, 300], seed=22)
+    _fill(c)
+    for w in ((0, 0), (600, 4)):
+        a, b = (_attention(c, window=w[0], sinks=w[1]) for _ in range(2))
+        assert np.array_equal(a, b)
+
+
+def test_noalloc_step_refuses_a_layer_with_a_window():
+    m = kb.Model(1, 512, 4, 2, D, kb.KVP_DTYPE_BF16, [0], max_batch=2, max_seq=64, kv_capacity=64)
+    t = torch.zeros(1 << 20, dtype=torch.bfloat16, device="cuda")
+    p = t.data_ptr()
+    m.kvp_set_layer(0, p, p, p, p)
+    m.kvp_set_kv_slot(0, p, p)
+    m.kvp_set_layer_window(0, 5, 1)
+    with pytest.raises(kb.KvpError) as e:
+        m.kvp_decode_step_noalloc(p, p, 3, p + 4096, 1, _stream())
+    assert e.value.code == kb.KVP_E_STATE
