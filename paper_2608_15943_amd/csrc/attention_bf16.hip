@@ -37,14 +37,39 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7F80
 // The halves of a word that are marked in bits 15 and 31, as a mask.
 __device__ __forceinline__ uint32_t halves(uint32_t bits) { return (bits >> 15 & 0x10001u) * 0xFFFFu; }
 
+// What rows t0 .. t0 + rows - 1 of a sequence see together.
+template <bool WIN>
+struct Span {
+    int all, last;           // positions up to `all` every row sees (but for its window), past `last` none does
+    int low, whole;          // WIN: the first position in the first row's window, and in the last row's
+    Span() = default;
+    __device__ __forceinline__ Span(const ListArgs& A, const SeqRows& s, int t0, int rows) {
+        const int n = min(s.act - t0, rows);
+        all = n > 0 ? s.len + t0 : -1;
+        last = n > 0 ? s.len + t0 + n - 1 : -1;
+        low = WIN ? all - A.window + 1 : 0;
+        whole = WIN ? last - A.window + 1 : 0;
+    }
+    // Whether some row does not see all of the tile that begins at p0.
+    __device__ __forceinline__ bool edge(const ListArgs& A, int p0) const {
+        return p0 + TILE - 1 > all || (WIN && p0 < whole && p0 + TILE > A.sinks);
+    }
+    // Whether some row sees some of it.
+    __device__ __forceinline__ bool sees(const ListArgs& A, int p0) const {
+        return p0 <= last && (!WIN || p0 + TILE > low || p0 < A.sinks);
+    }
+    // Whether no row sees position p.
+    __device__ __forceinline__ bool unseen(const ListArgs& A, int p) const {
+        return p > last || (WIN && p < low && p >= A.sinks);
+    }
+};
+
 // 16 NB columns of an item, from row t0 of the sequence on.
 template <int NB, bool WIN>
-struct Columns {
+struct Columns : Span<WIN> {
     int lim[NB];             // the last position that the column sees, -1 where there is none
     float m[NB], l[NB];      // running maximum (log2 domain) and sum of the weights
     f32x4 o[NB][8];          // O^T: dimensions 16 db + 4 grp + 0..3 of the column
-    int all, last;           // positions up to `all` every row sees (but for its window), past `last` none does
-    int low, whole;          // WIN: the first position in the first row's window, and in the last row's
 
     // Column of block cb: its row, from the item's or wave's first on (past every row where the column
     // is none of the `rows` rows'), and its head.
@@ -82,62 +107,61 @@ struct Columns {
 #pragma unroll
             for (int db = 0; db < 8; ++db) o[cb][db] = f32x4{};
         }
-        const int n = min(s.act - t0, rows);
-        all = n > 0 ? s.len + t0 : -1;
-        last = n > 0 ? s.len + t0 + n - 1 : -1;
-        if (WIN) {
-            low = all - A.window + 1;
-            whole = last - A.window + 1;
-        }
+        *(Span<WIN>*)this = Span<WIN>(A, s, t0, rows);
     }
-    // Whether some column does not see all of the tile that begins at p0.
-    __device__ __forceinline__ bool edge(const AttnArgs& A, int p0) const {
-        return p0 + TILE - 1 > all || (WIN && p0 < whole && p0 + TILE > A.sinks);
-    }
-    // Whether some column sees some of it.
-    __device__ __forceinline__ bool sees(const AttnArgs& A, int p0) const {
-        return p0 <= last && (!WIN || p0 + TILE > low || p0 < A.sinks);
-    }
-    __device__ __forceinline__ bool hidden(const AttnArgs& A, int cb, int p) const {
-        return p > lim[cb] || (WIN && p <= lim[cb] - A.window && p >= A.sinks);
-    }
-    // Whether no column sees position p.
-    __device__ __forceinline__ bool unseen(const AttnArgs& A, int p) const { return p > last || (WIN && p < low && p >= A.sinks); }
-
-    // Weights of the tile at p0 from its scores: lane (column, grp) holds positions p0 + 32 s + 8 grp + 4 e + i in block
-    // 2 s + e; out: the rows of P, pb.  is_edge: branches around the masks (two copies of this code cost registers).
-    __device__ __forceinline__ void softmax(const AttnArgs& A, f32x4 (&sc)[NB][4], bool is_edge, int p0, bf16x8 (&pb)[NB][2]) {
+    // Hides what a column does not see of the tile at p0 in its scores (lane (column, grp) holds positions p0 + 32 s + 8 grp +
+    // 4 e + i in block 2 s + e) and moves the running maxima.
+    __device__ __forceinline__ void maxima(const AttnArgs& A, f32x4 (&sc)[NB][4], bool is_edge, int p0) {
         const int grp = (threadIdx.x >> 4) & 3;
+        if (is_edge) {
+            const int at = p0 + 8 * grp;          // the lane's first position; the others are constants further
 #pragma unroll
-        for (int cb = 0; cb < NB; ++cb) {
-            if (is_edge) {
+            for (int cb = 0; cb < NB; ++cb) {
+                const int hi = lim[cb] - at, lo = hi - A.window, sk = A.sinks - at;
 #pragma unroll
                 for (int tb = 0; tb < 4; ++tb)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (hidden(A, cb, p0 + 32 * (tb >> 1) + 8 * grp + 4 * (tb & 1) + i)) sc[cb][tb][i] = -INFINITY;
+                    for (int i = 0; i < 4; ++i) {
+                        const int off = 32 * (tb >> 1) + 4 * (tb & 1) + i;
+                        if (off > hi || (WIN && off <= lo && off >= sk)) sc[cb][tb][i] = -INFINITY;
+                    }
             }
-            float mx = -INFINITY;
+        }
+        // The lanes of a column look at their own scores first: the maxima move rarely.
+        float mx[NB];
+        bool moves = false;
+#pragma unroll
+        for (int cb = 0; cb < NB; ++cb) {
+            mx[cb] = -INFINITY;
 #pragma unroll
             for (int tb = 0; tb < 4; ++tb)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[cb][tb][i]);
-            const float mt = pair32_max(pair16_max(mx)) * A.scale_log2;
-            if (__any(mt > m[cb] + kLazy)) {
-                const float m_new = fmaxf(m[cb], mt);
-                const float alpha = __builtin_amdgcn_exp2f(m[cb] - m_new);
-                m[cb] = m_new;
-                l[cb] *= alpha;
+                for (int i = 0; i < 4; ++i) mx[cb] = fmaxf(mx[cb], sc[cb][tb][i]);
+            moves |= mx[cb] * A.scale_log2 > m[cb] + kLazy;
+        }
+        if (__any(moves)) {
 #pragma unroll
-                for (int db = 0; db < 8; ++db) o[cb][db] *= alpha;
+            for (int cb = 0; cb < NB; ++cb) {
+                const float mt = pair32_max(pair16_max(mx[cb])) * A.scale_log2;
+                if (mt > m[cb] + kLazy) {
+                    const float alpha = __builtin_amdgcn_exp2f(m[cb] - mt);
+                    m[cb] = mt;
+                    l[cb] *= alpha;
+#pragma unroll
+                    for (int db = 0; db < 8; ++db) o[cb][db] *= alpha;
+                }
             }
+        }
+    }
+    // The tile's weights, the rows of P, and their sums.
+    __device__ __forceinline__ void weights(const AttnArgs& A, const f32x4 (&sc)[NB][4], bf16x8 (&pb)[NB][2]) {
+#pragma unroll
+        for (int cb = 0; cb < NB; ++cb) {
             uint32_t pw[8];
 #pragma unroll
-            for (int tb = 0; tb < 4; ++tb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sc[cb][tb][i] = __builtin_amdgcn_exp2f(fmaf(sc[cb][tb][i], A.scale_log2, -m[cb]));
-#pragma unroll
-            for (int i = 0; i < 8; ++i) pw[i] = pack2bf(sc[cb][i >> 1][2 * (i & 1)], sc[cb][i >> 1][2 * (i & 1) + 1]);
+            for (int i = 0; i < 8; ++i)
+                pw[i] = pack2bf(__builtin_amdgcn_exp2f(fmaf(sc[cb][i >> 1][2 * (i & 1)], A.scale_log2, -m[cb])),
+                                __builtin_amdgcn_exp2f(fmaf(sc[cb][i >> 1][2 * (i & 1) + 1], A.scale_log2, -m[cb])));
             float lt = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -204,7 +228,7 @@ struct Columns {
 // At most 16 NB columns.  NW 0: a share of the list, one wave.  Else one item, whose tiles NW waves take in turn and
 // join in LDS.
 template <int NW, int NB, bool WIN>
-__global__ __launch_bounds__(NW ? 64 * NW : 64, NW == 8 ? 2 : 1) void rows_few_kernel(AttnArgs A) {
+__global__ __launch_bounds__(NW ? 64 * NW : 64, 1) void rows_few_kernel(AttnArgs A) {
     constexpr bool LIST = NW == 0;
     constexpr int STEP = LIST ? 1 : NW, WAVES = LIST ? 1 : NW;
     __shared__ uint64_t nf[WAVES][D];      // values that are not finite
@@ -288,7 +312,8 @@ __global__ __launch_bounds__(NW ? 64 * NW : 64, NW == 8 ? 2 : 1) void rows_few_k
         }
         __builtin_amdgcn_sched_barrier(0);
         bf16x8 pb[NB][2];
-        C.softmax(A, sc, edge, p0, pb);
+        C.maxima(A, sc, edge, p0);
+        C.weights(A, sc, pb);
         if (edge) {
             uint32_t any = 0;
 #pragma unroll
@@ -366,42 +391,40 @@ __global__ __launch_bounds__(NW ? 64 * NW : 64, NW == 8 ? 2 : 1) void rows_few_k
     }
 }
 
-typedef __attribute__((address_space(3))) void lvoid_t;
-
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 // Buffer resource of one page and head of K or V at p, the same for the wave (word 3: a valid 32-bit data format).
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t page_buffer(const uint16_t* p) {
+__device__ __forceinline__ i32x4 page_buffer(const uint16_t* p) {
     const uint64_t a = (uint64_t)p;
-    const uint64_t u = (uint32_t)__builtin_amdgcn_readfirstlane((int)a) |
-                       (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(a >> 32)) << 32;
-    return __builtin_amdgcn_make_buffer_rsrc((void*)u, 0, kHalfPage * 2, 0x00020000);
+    return i32x4{__builtin_amdgcn_readfirstlane((int)a), __builtin_amdgcn_readfirstlane((int)(a >> 32) & 0xFFFF), kHalfPage * 2,
+                 0x00020000};
+}
+// Four KB of a page into LDS at `lds` (both the same for the wave), 16 bytes a lane and KB: the lane's bytes lie at v0 of
+// the first KB, at v1, v2 and v3 of the others.  In assembly, so that the compiler, which cannot tell the stages of a tile
+// apart, does not wait for these loads before every read of LDS; they write nothing but LDS, m0 is as it was, and the caller
+// waits.
+__device__ __forceinline__ void load_4kb(i32x4 page, uint32_t lds, uint32_t at, uint32_t v0, uint32_t v1, uint32_t v2, uint32_t v3) {
+    uint32_t m0;
+    asm volatile("s_mov_b32 %0, m0\n\t"
+                 "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %5, %9, %10 offen lds\n\t"
+                 "s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %6, %9, %11 offen lds\n\t"
+                 "s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %7, %9, %12 offen lds\n\t"
+                 "s_mov_b32 m0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %8, %9, %13 offen lds\n\t"
+                 "s_mov_b32 m0, %0"
+                 : "=&s"(m0)
+                 : "s"(lds), "s"(lds + 1024), "s"(lds + 2048), "s"(lds + 3072), "v"(v0), "v"(v1), "v"(v2), "v"(v3), "s"(page),
+                   "s"(at), "s"(at + 1024), "s"(at + 2048), "s"(at + 3072)
+                 : "memory");
 }
 
-// Eight 16-byte LDS reads and their wait: written by hand, since the compiler would first wait for the loads that go into
-// the other stage.  K: the four chunks of two rows' blocks, OFF and OFF + STEP from a0 .. a3; V: four rows' blocks of two
-// chunks.
-template <int OFF, int STEP>
-__device__ __forceinline__ void read_k(uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, u32x4 (&f)[8]) {
-    asm volatile("ds_read_b128 %0, %8 offset:%12\n\tds_read_b128 %1, %9 offset:%12\n\t"
-                 "ds_read_b128 %2, %10 offset:%12\n\tds_read_b128 %3, %11 offset:%12\n\t"
-                 "ds_read_b128 %4, %8 offset:%13\n\tds_read_b128 %5, %9 offset:%13\n\t"
-                 "ds_read_b128 %6, %10 offset:%13\n\tds_read_b128 %7, %11 offset:%13\n\t"
-                 "s_waitcnt lgkmcnt(0)"
-                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]), "=&v"(f[6]),
-                   "=&v"(f[7])
-                 : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "i"(OFF), "i"(OFF + STEP)
-                 : "memory");
-}
-template <int OFF, int STEP>
-__device__ __forceinline__ void read_v(uint32_t a0, uint32_t a1, u32x4 (&f)[8]) {
-    asm volatile("ds_read_b128 %0, %8 offset:%10\n\tds_read_b128 %1, %9 offset:%10\n\t"
-                 "ds_read_b128 %2, %8 offset:%11\n\tds_read_b128 %3, %9 offset:%11\n\t"
-                 "ds_read_b128 %4, %8 offset:%12\n\tds_read_b128 %5, %9 offset:%12\n\t"
-                 "ds_read_b128 %6, %8 offset:%13\n\tds_read_b128 %7, %9 offset:%13\n\t"
-                 "s_waitcnt lgkmcnt(0)"
-                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]), "=&v"(f[6]),
-                   "=&v"(f[7])
-                 : "v"(a0), "v"(a1), "i"(OFF), "i"(OFF + STEP), "i"(OFF + 2 * STEP), "i"(OFF + 3 * STEP)
-                 : "memory");
+// 16 fragments of NB products each, their LDS reads four fragments ahead of them.
+template <int SYNC, int NB>
+__device__ __forceinline__ void reads_ahead() {
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, SYNC);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, NB, SYNC);
+        if (i < 12) __builtin_amdgcn_sched_group_barrier(0x100, 1, SYNC);
+    }
 }
 
 // Workgroup: an item of 4 mw rows, wave v's 16 NB columns are its rows v mw .. (v + 1) mw - 1.  The tiles go from memory to
@@ -415,33 +438,23 @@ __global__ __launch_bounds__(256, 2) void rows_many_kernel(AttnArgs A) {
     // banks.
     __shared__ u32x4 kl[2][TILE * 16], vl[2][D * 8];
     __shared__ uint64_t nf[D];             // values that are not finite
-    auto key = [](int R) { return (R & 3) | ((R >> 3) & 3) << 2; };
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     Item it;
+    Split sp;
     uint32_t w = 0, left;
+    int parts = 0;                         // LIST: of every item, 0: shares are even
     if constexpr (LIST) {
-        Split sp;
-        if (!take_share<false, WIN>(A, &sp, &w, &left, &it)) {
+        const Parts<WIN> P(A, gridDim.x);
+        bool some;
+        if ((parts = P.k)) {
+            w = blockIdx.x < P.items * parts ? xcd_remap(blockIdx.x, P.items * parts) : blockIdx.x;
+            some = P.take(A, w, &left, &it);
+        } else {
+            some = take_share<false, WIN>(A, &sp, &w, &left, &it);
+        }
+        if (!some) {
             if (tid == 0) A.cut_many[blockIdx.x].np = 0;
             return;
-        }
-        // The item that the share begins and does not end: that of its last tile.
-        if (tid < 64) {
-            CutItem cut{};
-            if (w + 1 < sp.W) {
-                const uint32_t xe = sp.start(w + 1) - 1;
-                Lanes<false, WIN> L;
-                list_tiles<false, WIN>(A, L);
-                const Item e = find_tile<false, WIN>(A, L, xe);
-                if (e.t + 1 < e.n && xe - e.t >= sp.start(w)) {
-                    cut.np = sp.wave_of(xe - e.t + e.n - 1) - w + 1;
-                    cut.row = e.s.row0 + e.c * A.m;
-                    cut.n = e.s.n - e.c * A.m;
-                    cut.act = e.s.act - e.c * A.m;
-                    cut.head = e.kvh * (A.a / A.g);
-                }
-            }
-            if (tid == 0) A.cut_many[w] = cut;
         }
     } else {
         // The last block of every sequence first, as the longest, and so on; K/V heads change fastest: with
@@ -460,27 +473,70 @@ __global__ __launch_bounds__(256, 2) void rows_many_kernel(AttnArgs A) {
     Columns<NB, WIN> C;
     u32x4 q[NB][4];
     Table<WIN> tab;
-    auto issue = [&](const Item& i, int stg) {
-        const size_t at = tab.page(A, i);
-        const __amdgpu_buffer_rsrc_t kr = page_buffer(A.kc + at * kHalfPage), vr = page_buffer(A.vc + at * kHalfPage);
-        // The lane's 16 bytes of each of this wave's four KB of K (rows 16 wave + 4 i + lane / 16) and of V^T (rows
-        // 32 wave + 8 i + lane / 8).
+    // The lane's 16 bytes of each of this wave's four KB of K (rows 16 wave + 4 i + lane / 16) and of V^T (rows
+    // 32 wave + 8 i + lane / 8).
+    auto issue = [&](size_t at, int stg) __attribute__((always_inline)) {
         const int now = thread_now() & 63;
         const uint32_t ksrc = (now >> 4) * (2 * D) + 16 * ((now & 15) ^ ((now >> 4) | ((2 * wave) & 3) << 2));
         const uint32_t vsrc = (now >> 3) * (2 * TILE) + 16 * ((now & 7) ^ (now >> 4));
+        const uint32_t kd = (uint32_t)(uintptr_t)&kl[stg][256 * wave], vd = (uint32_t)(uintptr_t)&vl[stg][256 * wave];
+        load_4kb(page_buffer(A.kc + at * kHalfPage), __builtin_amdgcn_readfirstlane(kd), 4096 * wave, ksrc, ksrc, ksrc ^ 64u, ksrc ^ 64u);
+        load_4kb(page_buffer(A.vc + at * kHalfPage), __builtin_amdgcn_readfirstlane(vd), 4096 * wave, vsrc, vsrc ^ 64u, vsrc, vsrc ^ 64u);
+    };
+    // Scores of a K stage: the lane's rows of the four score blocks have one key; their chunks 4 ks + grp.
+    const int col = tid & 15, grp = (tid >> 4) & 3;
+    const int krow = 8 * (col >> 2) + (col & 3), kk = (krow & 3) | ((krow >> 3) & 3) << 2;
+    auto scores = [&](const u32x4* kl, f32x4 (&z)[NB][4]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lvoid_t*)&kl[stg][256 * wave + 64 * i], 16, i < 2 ? ksrc : ksrc ^ 64u,
-                                                     4096 * wave + 1024 * i, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lvoid_t*)&vl[stg][256 * wave + 64 * i], 16, i & 1 ? vsrc ^ 64u : vsrc,
-                                                     4096 * wave + 1024 * i, 0, 0);
-        }
+        for (int tb = 0; tb < 4; ++tb)
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                const bf16x8 f = as_bf16x8(kl[(krow + 32 * (tb >> 1) + 4 * (tb & 1)) * 16 + ((4 * ks + grp) ^ kk)]);
+#pragma unroll
+                for (int cb = 0; cb < NB; ++cb) z[cb][tb] = mfma16x16x32(f, as_bf16x8(q[cb][ks]), ks ? z[cb][tb] : f32x4{});
+            }
+        reads_ahead<0, NB>();
+    };
+    auto values = [&](const u32x4* vl, const bf16x8 (&pb)[NB][2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int db = 0; db < 8; ++db)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const bf16x8 f = as_bf16x8(vl[(16 * db + col) * 8 + ((4 * s + grp) ^ (col >> 1))]);
+#pragma unroll
+                for (int cb = 0; cb < NB; ++cb) C.o[cb][db] = mfma16x16x32(f, pb[cb][s], C.o[cb][db]);
+            }
+        reads_ahead<1, NB>();
     };
     bool whole = it.t == 0;
     int t0 = it.c * A.m + wave * A.mw;        // the wave's first row
-    issue(it, 0);
+    const size_t at0 = tab.page(A, it);
+    issue(at0, 0);
     C.load_q(A, it, t0, A.mw, q);
     C.begin(A, it.s, t0, A.mw);
+    if constexpr (LIST) {
+        // While the first loads are under way: the item that the share begins and does not end, that of its last tile.
+        if (tid < 64) {
+            CutItem cut{};
+            auto begins = [&](const Item& e, int np) {
+                cut.np = np;
+                cut.row = e.s.row0 + e.c * A.m;
+                cut.n = e.s.n - e.c * A.m;
+                cut.act = e.s.act - e.c * A.m;
+                cut.head = e.kvh * (A.a / A.g);
+            };
+            if (parts) {
+                if (it.t == 0) begins(it, parts);
+            } else if (w + 1 < sp.W) {
+                const uint32_t xe = sp.start(w + 1) - 1;
+                Lanes<false, WIN> L;
+                list_tiles<false, WIN>(A, L);
+                const Item e = find_tile<false, WIN>(A, L, xe);
+                if (e.t + 1 < e.n && xe - e.t >= sp.start(w)) begins(e, sp.wave_of(xe - e.t + e.n - 1) - w + 1);
+            }
+            if (tid == 0) A.cut_many[w] = cut;
+        }
+    }
     for (int stg = 0;; stg ^= 1) {
         const bool ends = it.t + 1 == it.n;
         bool more = left > 1;
@@ -491,97 +547,56 @@ __global__ __launch_bounds__(256, 2) void rows_many_kernel(AttnArgs A) {
             else
                 ++nx.t;
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // this wave's part of the tile is in LDS
+        const size_t at = more ? tab.page(A, nx) : 0;
+        // This wave's part of the tile is in LDS: vmcnt(0), by the builtin, so that the compiler knows that nothing else is
+        // under way either.
+        __builtin_amdgcn_s_waitcnt(0x0F70);
         __syncthreads();
         const int p0 = TILE * it.template at<WIN>(A);
         // Values that not all of the item's rows see.
         bool spoilt = false;
-        {
-            Columns<1, WIN> B;       // the item's rows
-            const int n = min(it.s.act - it.c * A.m, A.m);
-            B.all = n > 0 ? it.s.len + it.c * A.m : -1;
-            B.last = B.all + n - 1;
-            if (n <= 0) B.last = -1;
-            if (WIN) B.low = B.all - A.window + 1, B.whole = B.last - A.window + 1;
-            if (B.edge(A, p0)) {
-                bool bad = false;
+        const Span<WIN> B(A, it.s, it.c * A.m, A.m);
+        if (B.edge(A, p0)) {
+            bool bad = false;
+#pragma unroll 1
+            for (int i = tid; i < D * 8; i += 256) {
+                const int d = i >> 3, c = (i & 7) ^ ((d >> 1) & 7);
+                u32x4 x = vl[stg][i];
+                uint32_t bits = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int i = thread_now() + 256 * j, d = i >> 3, c = (i & 7) ^ ((d >> 1) & 7);
-                    u32x4 x = vl[stg][i];
-                    uint32_t bits = 0;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int p = p0 + 8 * c + 2 * e;
-                        x[e] &= (B.unseen(A, p) ? 0u : 0xFFFFu) | (B.unseen(A, p + 1) ? 0u : 0xFFFF0000u);
-                        const uint32_t b = not_finite(x[e]);
-                        bits |= (b >> 15 & 1) << (2 * e) | (b >> 31) << (2 * e + 1);
-                        x[e] &= ~halves(b);
-                    }
-                    vl[stg][i] = x;
-                    ((uint8_t*)&nf[d])[c] = (uint8_t)bits;
-                    bad |= bits != 0;
+                for (int e = 0; e < 4; ++e) {
+                    const int p = p0 + 8 * c + 2 * e;
+                    x[e] &= (B.unseen(A, p) ? 0u : 0xFFFFu) | (B.unseen(A, p + 1) ? 0u : 0xFFFF0000u);
+                    const uint32_t b = not_finite(x[e]);
+                    bits |= (b >> 15 & 1) << (2 * e) | (b >> 31) << (2 * e + 1);
+                    x[e] &= ~halves(b);
                 }
-                spoilt = __syncthreads_or(bad);
+                vl[stg][i] = x;
+                ((uint8_t*)&nf[d])[c] = (uint8_t)bits;
+                bad |= bits != 0;
             }
-        }
-        if (more) issue(nx, stg ^ 1);
-        if (C.sees(A, p0)) {
-            const bool edge = C.edge(A, p0);
+            spoilt = __syncthreads_or(bad);
             if (spoilt) C.spoil(A, nf, p0);
+        }
+        if (more) issue(at, stg ^ 1);
+        if (C.sees(A, p0)) {
             f32x4 sc[NB][4];
-            const int now = thread_now(), col = now & 15, grp = (now >> 4) & 3;
-            // The lane's rows of the four score blocks have one key; their chunks 4 ks + grp.
-            const int krow = 8 * (col >> 2) + (col & 3), kk = key(krow);
-            const uint32_t kb = (uint32_t)(uintptr_t)&kl[stg][krow * 16];
-            const uint32_t k0 = kb + 16 * (grp ^ kk), k1 = kb + 16 * ((4 + grp) ^ kk), k2 = kb + 16 * ((8 + grp) ^ kk),
-                           k3 = kb + 16 * ((12 + grp) ^ kk);
-            auto scores = [&](auto tb_t) __attribute__((always_inline)) {
-                constexpr int s = decltype(tb_t)::value;      // blocks 2 s and 2 s + 1: rows 32 s, 32 s + 4 further
-                u32x4 f[8];
-                read_k<s * 32 * 2 * D, 4 * 2 * D>(k0, k1, k2, k3, f);
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-#pragma unroll
-                        for (int cb = 0; cb < NB; ++cb)
-                            sc[cb][2 * s + e] = mfma16x16x32(as_bf16x8(f[4 * e + ks]), as_bf16x8(q[cb][ks]),
-                                                             ks ? sc[cb][2 * s + e] : f32x4{});
-            };
-            __builtin_amdgcn_s_setprio(1);
-            scores(std::integral_constant<int, 0>{});
-            scores(std::integral_constant<int, 1>{});
-            __builtin_amdgcn_s_setprio(0);
+            scores(kl[stg], sc);
+            C.maxima(A, sc, C.edge(A, p0), p0);
             bf16x8 pb[NB][2];
-            C.softmax(A, sc, edge, p0, pb);
-            const uint32_t vb = (uint32_t)(uintptr_t)&vl[stg][col * 8];
-            const uint32_t v0 = vb + 16 * (grp ^ ((col >> 1) & 7)), v1 = v0 ^ 64u;
-            auto vals = [&](auto d0_t) __attribute__((always_inline)) {
-                constexpr int d0 = decltype(d0_t)::value;
-                u32x4 f[8];
-                read_v<d0 * 16 * 2 * TILE, 16 * 2 * TILE>(v0, v1, f);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-#pragma unroll
-                        for (int cb = 0; cb < NB; ++cb)
-                            C.o[cb][d0 + i] = mfma16x16x32(as_bf16x8(f[2 * i + s]), pb[cb][s], C.o[cb][d0 + i]);
-            };
-            __builtin_amdgcn_s_setprio(1);
-            vals(std::integral_constant<int, 0>{});
-            vals(std::integral_constant<int, 4>{});
-            __builtin_amdgcn_s_setprio(0);
+            C.weights(A, sc, pb);
+            values(vl[stg], pb);
         }
         if (ends || !more) {
             float* piece = A.part + ((2 * (size_t)w + (whole ? 1 : 0)) * A.cols + wave * wcols) * PSTRIDE;
             C.finish(A, it, t0, A.mw, whole && ends, piece);
             if (!more) break;
             whole = true;
-            t0 = nx.c * A.m + wave * A.mw;
-            C.load_q(A, nx, t0, A.mw, q);
-            C.begin(A, nx.s, t0, A.mw);
+            if constexpr (LIST) {
+                t0 = nx.c * A.m + wave * A.mw;
+                C.load_q(A, nx, t0, A.mw, q);
+                C.begin(A, nx.s, t0, A.mw);
+            }
         }
         it = nx;
         --left;
@@ -595,24 +610,27 @@ int many_shares(int simds) { return std::max(1, 2 * simds / 4); }
 constexpr int kFewCols = 32;      // up to here a wave takes all columns of an item
 template <int NB, bool WIN>
 void launch_few(int nw, int grid, const AttnArgs& A, hipStream_t st) {
-    constexpr int MOST = NB == 1 ? 8 : 4;       // waves of a workgroup that have the registers for it
     if (nw == 0) hipLaunchKernelGGL((rows_few_kernel<0, NB, WIN>), dim3(grid), dim3(64), 0, st, A);
     else if (nw == 1) hipLaunchKernelGGL((rows_few_kernel<1, NB, WIN>), dim3(grid), dim3(64), 0, st, A);
     else if (nw == 2) hipLaunchKernelGGL((rows_few_kernel<2, NB, WIN>), dim3(grid), dim3(128), 0, st, A);
-    else hipLaunchKernelGGL((rows_few_kernel<MOST, NB, WIN>), dim3(grid), dim3(64 * MOST), 0, st, A);
+    else hipLaunchKernelGGL((rows_few_kernel<4, NB, WIN>), dim3(grid), dim3(256), 0, st, A);
 }
-template <int NB, bool WIN>
-void launch_many(bool list, int grid, const AttnArgs& A, hipStream_t st) {
-    if (list) hipLaunchKernelGGL((rows_many_kernel<true, NB, WIN>), dim3(grid), dim3(256), 0, st, A);
-    else hipLaunchKernelGGL((rows_many_kernel<false, NB, WIN>), dim3(grid), dim3(256), 0, st, A);
+template <bool LIST, int NB, bool WIN>
+void launch_many(int grid, const AttnArgs& A, hipStream_t st) {
+    hipLaunchKernelGGL((rows_many_kernel<LIST, NB, WIN>), dim3(grid), dim3(256), 0, st, A);
 }
 
-// Waves that take an item of few columns where a launch without a list and a join is the faster one, else 0.  tiles: of
-// the longest item.
-int few_waves(int64_t items, int64_t tiles, int simds) {
-    if (tiles <= 2) return 1;
-    if (tiles > std::min<int64_t>(32, 14 + items / 4)) return 0;
-    return items <= simds / 4 ? 8 : items <= simds / 2 ? 2 : 1;
+// Waves that take an item of few columns (16 nb) where a launch without a list and a join is the faster one, else 0.  tiles: of
+// the longest item.  One workgroup an item of 1, 2 and 4 waves against the list, 32 heads on 8, in us.  nb 1: 1 sequence of
+// 200 positions 8.4, 7.9, 7.7 and 10.3, of 500 13.5, 11.2, 11.0 and 10.1; 8 of 200 9.2, 8.2, 7.8 and 10.2, 500 16, 11.9,
+// 11.6 and 10.5; 16 of 500 16.7, 12.2, 11.8 and 13.1, 1000 31, 20, 19.5 and 18.8; 32 of 1000 39, 28, 27 and 31, 2000 74, 50, 49
+// and 53; 64 of 500 26.6, 27.3, 30 and 31.6, 2000 91, 94, 95 and 99; 100 of 500 44, 47, 53 and 51, 2000 165, 159, 169 and 156.  nb
+// 2 (8 rows a sequence): 1 of 500 17.9, 15.9, 14.7 and 11.5; 8 of 500 19.8, 16.9, 15.4 and 13.9; 16 of 1000 38, 26, 23.4 and
+// 27; 64 of 1000 52, 56, 60 and 68.  (Past 32 tiles one long sequence among short ones would cost more than there is to gain; 8
+// waves have too few registers: 18.9 for 1 of 500, nb 2.)
+int few_waves(int64_t items, int64_t tiles, int nb, int simds) {
+    if (tiles > std::min<int64_t>(32, nb == 1 ? 4 + items / 11 : items < 96 ? 4 : 32)) return 0;
+    return items <= simds / 4 ? 4 : items < simds / 2 ? 2 : 1;
 }
 
 template <bool WIN>
@@ -631,7 +649,7 @@ hipError_t launch(AttnArgs& A, int simds, hipStream_t st) {
     if (r.max_new * heads <= kFewCols) {
         A.m = r.max_new;
         A.cols = A.m * heads;
-        const int items = r.B * A.g, nw = listed(items, A.m) ? few_waves(items, most(A.m), simds) : 1;
+        const int items = r.B * A.g, nw = listed(items, A.m) ? few_waves(items, most(A.m), A.cols <= 16 ? 1 : 2, simds) : 1;
         if (nw) {
             if (A.cols <= 16) launch_few<1, WIN>(nw, items, A, st);
             else launch_few<2, WIN>(nw, items, A, st);
@@ -649,29 +667,52 @@ hipError_t launch(AttnArgs& A, int simds, hipStream_t st) {
             hipLaunchKernelGGL(join_few_kernel, dim3(items * A.cols), dim3(kJoinThreads), 0, st, A);
         return hipGetLastError();
     }
-    // Rows of a wave: what its 16 (where they hold a quarter of the longest sequence's rows) or 32 columns hold, and no
-    // more than that quarter.
-    const int nb = 4 * (16 / heads) >= r.max_new ? 1 : 2;
+    // Columns of a wave, 16 nb, and items one by one or as a list, by what each would take, in us.  t1: a tile of an item
+    // whose workgroup has its CU to itself; t2: one of two workgroups' (measured: 30000 positions, one block of rows; prompts of
+    // 8192 rows, 64 heads on 8).  One by one: the longest item's tiles one after the other, all tiles on all CUs, or K and V
+    // from memory once, whichever is most (and above it where they are alike).  The list: all tiles on all CUs, or what the L2s (4
+    // MB an XCD) do not hold of K and V for every share, a second launch, and the pieces' way to memory and back, the more the
+    // more items are cut; nb 3 has no list, its pieces cost more than its tiles gain.  Lengths are bounds: of several sequences
+    // 0.8 of them counts, and the list, which shares uneven ones evenly, has its items' cuts for nothing.
+    // Measured, nb 1, 2, 3 one by one, then 1 and 2 listed; 32 heads on 8: a prompt of 700 rows 18, 22, 29, 34, 35; 2000 49, 53,
+    // 69, 97, 85; 4000 164, 136, 141, 253, 204; 4 x 4096 (16 on 8) 338, 274, 264, 472, 401; 60 rows behind 3000 positions 49, 67,
+    // 94, 24, 30; 512 behind 8000 128, 173, 243, 102, 88; 100 behind 30000 446, 593, 841, 87, 80; three chunks of 333-1001
+    // behind 700-5000 146, 146, 185, 147, 129; 8 x 100 behind 3000 67, 72, 96, 125, 73.
+    static constexpr double t1[3] = {0.95, 1.26, 1.79}, t2[3] = {0.60, 0.95, 1.345};
+    const double cus = simds / 4., part = r.B > 1 ? 0.8 : 1., tile_us = 4. * kHalfPage / 6e6;
+    const int shares = many_shares(simds);
+    int nb = 0;
+    bool list = false;
+    double best = 0;
+    for (int i = 1; i <= 3; ++i) {
+        // Rows of a wave: no more than a quarter of the longest sequence's.
+        const int mw = std::min(16 * i / heads, (r.max_new + 3) / 4), m = 4 * mw;
+        if (mw < 1) continue;
+        const int64_t items = (int64_t)A.g * (r.rows / m + r.B), grid = (int64_t)A.g * r.B * ((r.max_new + m - 1) / m);
+        const double n = most(m), mean = part * std::max(WIN ? n - 1 : n - r.max_new / (2. * TILE), n / 2);
+        const double T = A.g * ((double)r.rows / m + 0.5 * r.B) * mean, kv = part * A.g * r.B * n;
+        const double longest = n * t1[i - 1], all = T * t2[i - 1] / cus, once = kv * tile_us;
+        const double again = 2 * items <= shares && r.B == 1 ? once : T * tile_us * std::max(0., 1 - 32e6 / (kv * 4 * kHalfPage));
+        const double one = 5 + std::cbrt(longest * longest * longest + all * all * all + once * once * once) + grid / 2000.,
+                     shared = 18 + 3.5 * i + std::max(all, again) + (r.B > 1 ? 0 : 6. * i * std::min(1., (double)items / shares));
+        if (grid < 1 << 24 && (!nb || one < best)) nb = i, list = false, best = one;          // 2^32 threads
+        if (i < 3 && listed(items, m) && (!nb || shared < best)) nb = i, list = true, best = shared;
+    }
+    if (!nb) return hipErrorInvalidValue;
     A.mw = std::min(16 * nb / heads, (r.max_new + 3) / 4);
     A.m = 4 * A.mw;
     A.cols = A.m * heads;
-    const int shares = many_shares(simds);
-    const int64_t items = (int64_t)A.g * (r.rows / A.m + r.B), grid = (int64_t)A.g * r.B * ((r.max_new + A.m - 1) / A.m);
-    // Items one by one or the list, in us.  One by one: the tiles of the longest one after the other, a part of all
-    // work, and blocks that are none (the grid has as many for every sequence as the longest may have).  The list: all
-    // work shared evenly, a second launch, and the pieces' way to memory and back.  Of the tiles some 0.6 of the most
-    // that there may be.
-    const double n = most(A.m), T = 0.6 * items * n;
-    const double one = 6 + 1.65 * n + T / 512 + grid / 2000.,
-                 list = 12 + T / 256 + (std::min<double>(T, shares) + items) * A.cols * (PSTRIDE * sizeof(float)) / 2.3e6;
-    const bool fits = grid < 1 << 24;       // 2^32 threads
-    if ((one < list && fits) || !listed(items, A.m)) {
-        if (!fits) return hipErrorInvalidValue;
-        nb == 1 ? launch_many<1, WIN>(false, grid, A, st) : launch_many<2, WIN>(false, grid, A, st);
+    const int64_t items = (int64_t)A.g * (r.rows / A.m + r.B);
+    if (!list) {
+        const int grid = A.g * r.B * ((r.max_new + A.m - 1) / A.m);
+        if (nb == 1) launch_many<false, 1, WIN>(grid, A, st);
+        else if (nb == 2) launch_many<false, 2, WIN>(grid, A, st);
+        else launch_many<false, 3, WIN>(grid, A, st);
         return hipGetLastError();
     }
     A.cut_many = (CutItem*)(A.part + (size_t)2 * shares * A.cols * PSTRIDE);
-    nb == 1 ? launch_many<1, WIN>(true, shares, A, st) : launch_many<2, WIN>(true, shares, A, st);
+    if (nb == 1) launch_many<true, 1, WIN>(shares, A, st);
+    else launch_many<true, 2, WIN>(shares, A, st);
     if ((e = hipGetLastError()) != hipSuccess || shares == 1) return e;
     const dim3 join(shares - 1, (A.cols + kJoinCols - 1) / kJoinCols);
     if (4 * items <= shares)
@@ -685,7 +726,7 @@ hipError_t launch(AttnArgs& A, int simds, hipStream_t st) {
 
 // Pieces, then what the join reads.
 size_t attention_rows_bytes(int B, int g, int simds) {
-    const size_t pieces = (size_t)2 * PSTRIDE * sizeof(float) * std::max(kFewCols * few_shares(simds), 128 * many_shares(simds));
+    const size_t pieces = (size_t)2 * PSTRIDE * sizeof(float) * std::max(kFewCols * few_shares(simds), 256 * many_shares(simds));
     return pieces + std::max((size_t)B * g * sizeof(int2), (size_t)many_shares(simds) * sizeof(CutItem));
 }
 

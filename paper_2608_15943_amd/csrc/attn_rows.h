@@ -239,6 +239,51 @@ __device__ __forceinline__ bool take_share(const ListArgs& A, Split* sp, uint32_
     *it = find_tile<FEW, WIN>(A, L, x);
     return true;
 }
+// Items cut into equal parts, one a share, in place of the even list.  The blocks of a sequence and K/V head then read the
+// same positions at about the same time and on one XCD (shares run in blocks), and share its L2; even shares begin anywhere,
+// and each reads K and V for itself.  Only where every item has k parts (the device's workgroups over the items, two at
+// least) of nearly as many tiles: no part is longer than 1.4 even shares.
+template <bool WIN>
+struct Parts {
+    uint32_t items;
+    int k;                   // parts of an item, 0: no such cut
+    __device__ __forceinline__ Parts(const ListArgs& A, uint32_t shares) {
+        const int lane = threadIdx.x & 63;
+        float n = 0.f, T = 0.f, hi = 0.f, lo = 1e9f;
+        for (int b = lane; b < A.r.B; b += 64) {
+            const SeqRows s = seq_rows(A.r, b);
+            if (!s.n) continue;
+            const int nb = blocks_of(s, A.m);
+            const float first = tiles_of<WIN>(A, s, 0), last = tiles_of<WIN>(A, s, nb - 1);
+            n += (float)nb * A.g;
+            T += (float)nb * A.g * 0.5f * (first + last);
+            hi = fmaxf(hi, fmaxf(first, last) + (WIN ? 1.f : 0.f));
+            lo = fminf(lo, fminf(first, last));
+        }
+        n = wave_sum(n);
+        T = wave_sum(T);
+        hi = wave_max(hi);
+        lo = -wave_max(-lo);
+        items = n < 1e6f ? (uint32_t)n : 1u << 20;      // exact below 2^24
+        k = items ? shares / items : 0;
+        if (k < 2 || lo < k || ceilf(hi / k) * shares > 1.4f * T) k = 0;
+    }
+    // Part w % k of item w / k: false past the last.
+    __device__ __forceinline__ bool take(const ListArgs& A, uint32_t w, uint32_t* left, Item* it) const {
+        int first;
+        if (w >= items * k) return false;
+        auto count = [&](const SeqRows& s) { return blocks_of(s, A.m) * A.g; };
+        if (!find_item(A.r, w / k, count, &it->b, &it->s, &first)) return false;
+        const int x = w / k - first, nb = blocks_of(it->s, A.m), j = w % k;
+        it->kvh = x / nb;
+        it->c = x % nb;
+        it->template begin<WIN>(A);
+        it->t = (int)((int64_t)it->n * j / k);
+        *left = (int)((int64_t)it->n * (j + 1) / k) - it->t;
+        return *left > 0;
+    }
+};
+
 // The item behind `it` in the list; false past the end.
 template <bool WIN>
 __device__ __forceinline__ bool next_item(const ListArgs& A, Item& it) {
