@@ -2,10 +2,14 @@
 // beside them.
 //
 // Pages hold 64 positions: K [64][128], V [128][64], the positions of one dimension side by side.  Many rows
-// (append_rows_kernel): a workgroup owns the rows that fall into one page of one sequence, for some of the head vectors (Q,
-// K, V): it evaluates the rotation of its at most 64 x 64 angles once, in double precision.  V is turned in registers: a lane
+// (append_rows_kernel): a workgroup owns the rows that fall into half a page of one sequence, for some of the head vectors
+// (Q, K, V): it evaluates the rotation of its at most 32 x 64 angles once, in double precision.  V is turned in registers: a lane
 // takes 8 dimensions of 8 positions, whose words it deals out again as 16-byte runs of positions.  One row a sequence
 // (append_row_kernel): a wave a head vector.  Only positions of the call's rows are written, each once.
+//
+// Bound by memory: 2568 rows in 7 chunks (64 query heads, 8 K/V heads; 105 MB) 30 us, 3.5 TB/s (41 with workgroups of 64
+// positions and 8 vectors, 31 with 32 and 8 or 16); prompts of 4 x 4096 rows (16, 8; 268 MB) 68 us, 4.0 TB/s (67, 75); one row
+// of each of 8 sequences 3.2 us, the latency of three loads that depend on each other (length, page, row).
 #include "rope_rows.h"
 
 namespace kvp {
@@ -23,21 +27,33 @@ struct Args {
     int first;         // 0: from the first Q vector, a: from the first K vector
 };
 
-// Many rows: workgroup = the new rows of one page, for kPer of the head vectors.
-constexpr int kPer = 2 * kWaves;
+// Many rows: workgroup = the new rows of kPart positions of one page, for kWaves of the head vectors, one a wave, whose rows
+// are requested ahead of the angles.
+constexpr int kPart = 32;
 template <class Src>
 __global__ __launch_bounds__(kThreads) void append_rows_kernel(Src src, Args A, RopeFreqs th) {
-    __shared__ float2 cs[kPage][kHead / 2];
+    __shared__ float2 cs[kPart][kHead / 2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int b, first;
     SeqRows s;
-    auto pages = [](const SeqRows& s) { return s.act > 0 ? (s.len + s.act - 1) / kPage - s.len / kPage + 1 : 0; };
-    if (!find_item(A.r, blockIdx.x, pages, &b, &s, &first)) return;
-    const int pos0 = (s.len / kPage + (int)blockIdx.x - first) * kPage;
-    const int lo = max(s.len - pos0, 0), hi = min(s.len + s.act - pos0, kPage);   // new: lo <= place < hi
+    auto parts = [](const SeqRows& s) { return s.act > 0 ? (s.len + s.act - 1) / kPart - s.len / kPart + 1 : 0; };
+    if (!find_item(A.r, blockIdx.x, parts, &b, &s, &first)) return;
+    const int pos0 = (s.len / kPart + (int)blockIdx.x - first) * kPart;
+    const int lo = max(s.len - pos0, 0), hi = min(s.len + s.act - pos0, kPart);   // new: lo <= place < hi
     const int row0 = s.row0 + pos0 - s.len;                                       // row of place 0 (if new)
-    const int page = page_of(A.r, b, pos0);
-    const int hv0 = A.first + blockIdx.y * kPer, hv1 = min(hv0 + kPer, A.first + A.vectors);
+    const int hv0 = A.first + blockIdx.y * kWaves, hv = hv0 + wave;
+    const int z = hv < A.a ? 0 : hv < A.a + A.g ? 1 : 2, h = z == 0 ? hv : z == 1 ? hv - A.a : hv - A.a - A.g;
+    // Q and K: lane (place, c) holds dimensions 8 c .. + 7 (even i) and the same of the second half, 8 (i / 2) places further.
+    // V: lane (grp, c) holds dimensions 8 c .. + 7 of places 8 grp + i.
+    typename Src::Raw x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int p = z == 2 ? 8 * (lane >> 4) + i : 8 * (i >> 1) + (lane >> 3);
+        const int d = z == 2 ? 8 * (lane & 15) : 8 * (lane & 7) + 64 * (i & 1);
+        x[i] = typename Src::Raw{};
+        if (hv < A.first + A.vectors && p >= lo && p < hi) x[i] = src.raw8(row0 + p, z, h * kHead + d);
+    }
+    const int page = page_of(A.r, b, pos0), at = pos0 % kPage;
     if (hv0 < A.a + A.g) {
         const Turns turns(th, tid % (kHead / 2));       // kThreads is a multiple of that
         for (int i = tid; i < (hi - lo) * (kHead / 2); i += kThreads) {
@@ -46,56 +62,48 @@ __global__ __launch_bounds__(kThreads) void append_rows_kernel(Src src, Args A, 
         }
     }
     __syncthreads();
-    for (int hv = hv0 + wave; hv < hv1; hv += kWaves) {
-        if (hv < A.a + A.g) {
-            // Q and K: lane (place of 8, c) holds dimensions 8 c .. + 7 and the same of the second half.
-            const int c = lane & 7;
-            const bool isq = hv < A.a;
-            const int h = isq ? hv : hv - A.a;
-            for (int p = (lo & ~7) + (lane >> 3); p < hi; p += 8) {
-                if (p < lo) continue;
-                float x[16];
-                src.template load<8>(row0 + p, isq ? 0 : 1, h * kHead + 8 * c, x);
-                src.template load<8>(row0 + p, isq ? 0 : 1, h * kHead + 64 + 8 * c, x + 8);
+    if (hv >= A.first + A.vectors) return;
+    if (z < 2) {
+        const int c = lane & 7;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) rotate(x[i], x[8 + i], cs[p][8 * c + i]);
-                uint16_t* o = isq ? A.q_out + ((size_t)(row0 + p) * A.a + h) * kHead + 8 * c
-                                  : A.kc + (((size_t)h * A.r.n_pages + page) * kPage + p) * kHead + 8 * c;
+        for (int i = 0; i < 4; ++i) {
+            const int p = 8 * i + (lane >> 3);
+            if (p < lo || p >= hi) continue;
+            float y[16];
+            Src::widen(x[2 * i], y);
+            Src::widen(x[2 * i + 1], y + 8);
 #pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    u32x4 w;
+            for (int e = 0; e < 8; ++e) rotate(y[e], y[8 + e], cs[p][8 * c + e]);
+            uint16_t* o = z == 0 ? A.q_out + ((size_t)(row0 + p) * A.a + h) * kHead + 8 * c
+                                 : A.kc + (((size_t)h * A.r.n_pages + page) * kPage + at + p) * kHead + 8 * c;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = pack2bf(x[8 * z + 2 * e], x[8 * z + 2 * e + 1]);
-                    *(u32x4*)(o + 64 * z) = w;
-                }
+            for (int j = 0; j < 2; ++j) {
+                u32x4 w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = pack2bf(y[8 * j + 2 * e], y[8 * j + 2 * e + 1]);
+                *(u32x4*)(o + 64 * j) = w;
             }
+        }
+        return;
+    }
+    const int c = lane & 15, p0 = 8 * (lane >> 4);
+    u32x4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = Src::bits(x[i]);
+    uint16_t* dst = A.vc + (((size_t)h * A.r.n_pages + page) * kHead + 8 * c) * kPage + at + p0;
+    const bool full = p0 >= lo && p0 + 8 <= hi;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        u32x4 run;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)      // dimension e of two positions
+            run[j] = __builtin_amdgcn_perm(v[2 * j + 1][e >> 1], v[2 * j][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+        if (full) {
+            *(u32x4*)(dst + e * kPage) = run;
         } else {
-            // V: lane (grp, c) holds dimensions 8 c .. 8 c + 7 of places 8 grp .. 8 grp + 7 of a half page.
-            const int h = hv - A.a - A.g, grp = lane >> 4, c = lane & 15;
-            for (int p0 = (lo & ~31) + 8 * grp; p0 < hi; p0 += 32) {
-                u32x4 x[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    x[j] = u32x4{0, 0, 0, 0};
-                    if (p0 + j >= lo && p0 + j < hi) x[j] = src.v8(row0 + p0 + j, h * kHead + 8 * c);
-                }
-                uint16_t* dst = A.vc + (((size_t)h * A.r.n_pages + page) * kHead + 8 * c) * kPage + p0;
-                const bool full = p0 >= lo && p0 + 8 <= hi;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    u32x4 run;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)      // dimension e of two positions
-                        run[j] = __builtin_amdgcn_perm(x[2 * j + 1][e >> 1], x[2 * j][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
-                    if (full) {
-                        *(u32x4*)(dst + e * kPage) = run;
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (p0 + j >= lo && p0 + j < hi) dst[e * kPage + j] = (uint16_t)(run[j >> 1] >> (16 * (j & 1)));
-                    }
-                }
-            }
+            for (int j = 0; j < 8; ++j)
+                if (p0 + j >= lo && p0 + j < hi) dst[e * kPage + j] = (uint16_t)(run[j >> 1] >> (16 * (j & 1)));
         }
     }
 }
@@ -144,8 +152,8 @@ hipError_t launch(const Src& src, const Args& A, const RopeFreqs& th, hipStream_
         hipLaunchKernelGGL(append_row_kernel<Src>, grid, dim3(kThreads), 0, st, src, A, th);
         return hipGetLastError();
     }
-    // n rows lie in at most n / 64 + 2 pages.
-    const dim3 grid(r.rows / kPage + 2 * r.B, (A.vectors + kPer - 1) / kPer);
+    // n rows lie in at most n / 32 + 2 parts of 32 positions.
+    const dim3 grid(r.rows / kPart + 2 * r.B, (A.vectors + kWaves - 1) / kWaves);
     hipLaunchKernelGGL(append_rows_kernel<Src>, grid, dim3(kThreads), 0, st, src, A, th);
     return hipGetLastError();
 }

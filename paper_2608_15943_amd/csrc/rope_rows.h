@@ -81,8 +81,19 @@ struct Bf16Src {
             }
         }
     }
-    // Eight values of V, or one, as bf16.
-    __device__ __forceinline__ u32x4 v8(int row, int col) const { return *(const u32x4*)(v + (size_t)row * ldkv + col); }
+    // Eight values as they are in memory; those in fp32, and as bf16.
+    typedef u32x4 Raw;
+    __device__ __forceinline__ Raw raw8(int row, int z, int col) const {
+        return *(const u32x4*)(z == 0 ? q + (size_t)row * ldq + col : (z == 1 ? k : v) + (size_t)row * ldkv + col);
+    }
+    static __device__ __forceinline__ void widen(const Raw& w, float* x) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[2 * e] = __uint_as_float(w[e] << 16);
+            x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+        }
+    }
+    static __device__ __forceinline__ u32x4 bits(const Raw& w) { return w; }
     __device__ __forceinline__ uint16_t v1(int row, int col) const { return v[(size_t)row * ldkv + col]; }
 };
 
@@ -102,10 +113,20 @@ struct PlaneSrc {
             for (int i = 0; i < N_; ++i) x[i] += p[i];
         }
     }
-    __device__ __forceinline__ u32x4 v8(int row, int col) const {
+    struct Raw {
         float x[8];
-        load<8>(row, 2, col, x);
-        return u32x4{pack2bf(x[0], x[1]), pack2bf(x[2], x[3]), pack2bf(x[4], x[5]), pack2bf(x[6], x[7])};
+    };
+    __device__ __forceinline__ Raw raw8(int row, int z, int col) const {
+        Raw w;
+        load<8>(row, z, col, w.x);
+        return w;
+    }
+    static __device__ __forceinline__ void widen(const Raw& w, float* x) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = w.x[e];
+    }
+    static __device__ __forceinline__ u32x4 bits(const Raw& w) {
+        return u32x4{pack2bf(w.x[0], w.x[1]), pack2bf(w.x[2], w.x[3]), pack2bf(w.x[4], w.x[5]), pack2bf(w.x[6], w.x[7])};
     }
     __device__ __forceinline__ uint16_t v1(int row, int col) const {
         float x;
