@@ -16,7 +16,6 @@
 #include <math.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "attn_rows.h"
 
@@ -30,6 +29,8 @@ struct AttnArgs : ListArgs {
     const uint16_t* kc;
     const uint16_t* vc;
     float scale_log2;
+    // Of many columns: tiles and parts of an item at most; or the parts of all items together.
+    int longest, parts, jobs;
 };
 
 // Bits 15 and 31: whether the bf16 numbers of a word are not finite.
@@ -427,11 +428,109 @@ __device__ __forceinline__ void reads_ahead() {
     }
 }
 
-// Workgroup: an item of 4 mw rows, wave v's 16 NB columns are its rows v mw .. (v + 1) mw - 1.  The tiles go from memory to
-// LDS directly, two stages of 32 KB, one barrier a tile: it ends the loads of the tile that comes and the reads of the one
-// before it, whose stage is then loaded again.  Two workgroups a CU run in each other's waits.
-// LIST: a share of the list; else one item, counted from a sequence's last.
-template <bool LIST, int NB, bool WIN>
+// A bound of the tiles of every block of a sequence (without a window that of its last row).
+template <bool WIN>
+__device__ __forceinline__ int most_tiles(const ListArgs& A, const SeqRows& s) {
+    const int n = s.act ? (s.len + s.act - 1) / TILE + 1 : 1;
+    return WIN ? min(n, (A.window + A.m + TILE - 2) / TILE + 1 + sink_tiles(A)) : n;
+}
+// An item, or a part of it, as a workgroup takes it.
+struct Part {
+    Item it;
+    int part, parts;
+    int slot, step;          // of its first piece, from one to the next
+};
+// The item, or part, of workgroup x; join: the item whose parts workgroup x joins.  False: there is none.
+//
+// By length (A.jobs 0): a grid of A.parts x the longest sequence's blocks x B x g, parts of A.longest tiles at most.  The last
+// block of every sequence first, as the longest, and so on; the blocks' last parts before all others.
+// By count: A.jobs parts at most, so long that they are no more; sequence by sequence, the first parts of its items first.
+// Either way parts that run together read the same positions at about the same time, and share them in L2.  K/V heads
+// change fastest: with 8 of them each XCD reads one of them only.
+template <bool WIN>
+__device__ __forceinline__ bool take_part(const AttnArgs& A, int x, bool join, Part* p) {
+    Item& it = p->it;
+    int longest = A.longest;
+    if (!A.jobs) {
+        const int blocks = (A.r.max_new + A.m - 1) / A.m;
+        it.kvh = x % A.g;
+        x /= A.g;
+        it.b = x % A.r.B;
+        x /= A.r.B;
+        it.c = blocks - 1 - x % blocks;
+        p->part = join ? 0 : A.parts - 1 - x / blocks;
+        it.s = seq_rows(A.r, it.b);
+        if (it.c >= blocks_of(it.s, A.m)) return false;
+        // The sequences before it have row0 / m + b blocks at most.
+        p->slot = ((it.s.row0 / A.m + it.b + it.c) * A.g + it.kvh) * A.parts;
+        p->step = 1;
+    } else {
+        const int lane = threadIdx.x & 63;
+        // Items, and tiles if all blocks had as many as their sequence's longest: parts of ceil(tiles / (jobs - items)) tiles are
+        // jobs at most.  Sums alone, so that every workgroup finds the same number.
+        SeqRows s{0, 0, 0, 0};
+        int items = 0;
+        float n_lane = 0.f;
+        uint64_t t_lane = 0;
+        for (int b0 = 0; b0 < A.r.B; b0 += 64) {
+            items = 0;
+            if (b0 + lane < A.r.B) {
+                s = seq_rows(A.r, b0 + lane);
+                items = blocks_of(s, A.m) * A.g;
+                n_lane += (float)items;
+                t_lane += (uint64_t)items * most_tiles<WIN>(A, s);
+            }
+        }
+        const float room = (float)A.jobs - wave_sum(n_lane), tiles = wave_sum((float)t_lane) * 1.00001f;
+        longest = room < 1.f ? 1 << 30 : (int)fminf(ceilf(tiles / room), 1e9f);
+        longest = __builtin_amdgcn_readfirstlane(longest);
+        int item0 = 0, job0 = 0, n = 0;
+        for (int b0 = 0;; b0 += 64) {
+            if (b0 >= A.r.B) return false;
+            if (A.r.B > 64) {
+                items = 0;
+                if (b0 + lane < A.r.B) {
+                    s = seq_rows(A.r, b0 + lane);
+                    items = blocks_of(s, A.m) * A.g;
+                }
+            }
+            const int jobs = items ? items * ((most_tiles<WIN>(A, s) + longest - 1) / longest) : 0;
+            int ip = items, jp = jobs;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const int u = __shfl_up(ip, off), v = __shfl_up(jp, off);
+                if (lane >= off) ip += u, jp += v;
+            }
+            const int w = __popcll(__ballot(join ? item0 + ip <= x : job0 + jp <= x));    // lanes before the one that holds x
+            if (w < 64) {
+                it.b = b0 + w;
+                it.s = {__builtin_amdgcn_readlane(s.row0, w), __builtin_amdgcn_readlane(s.n, w), __builtin_amdgcn_readlane(s.len, w),
+                        __builtin_amdgcn_readlane(s.act, w)};
+                n = __builtin_amdgcn_readlane(items, w);
+                item0 += __builtin_amdgcn_readlane(ip - items, w);
+                job0 += __builtin_amdgcn_readlane(jp - jobs, w);
+                break;
+            }
+            item0 += __builtin_amdgcn_readlane(ip, 63);
+            job0 += __builtin_amdgcn_readlane(jp, 63);
+        }
+        x -= join ? item0 : job0;
+        p->part = x / n;
+        x %= n;
+        it.kvh = x % A.g;
+        it.c = n / A.g - 1 - x / A.g;
+        p->slot = job0 + x;
+        p->step = n;
+    }
+    it.template begin<WIN>(A);
+    p->parts = (it.n + longest - 1) / longest;
+    return p->part < p->parts;
+}
+
+// Workgroup: a part of an item of 4 mw rows, wave v's 16 NB columns are its rows v mw .. (v + 1) mw - 1.  The tiles go from
+// memory to LDS directly, two stages of 32 KB, one barrier a tile: it ends the loads of the tile that comes and the reads of
+// the one before it, whose stage is then loaded again.  Two workgroups a CU run in each other's waits.
+template <int NB, bool WIN>
 __global__ __launch_bounds__(256, 2) void rows_many_kernel(AttnArgs A) {
     // K: chunk c (16 bytes, 8 dimensions) of row R at place c ^ key(R) of its 16, key of the bits that differ among the 16 rows
     // of a fragment; V^T: chunk c (8 positions) of row d at place c ^ (d / 2 % 8) of its 8: the 16 lanes of a group fall on all
@@ -439,36 +538,11 @@ __global__ __launch_bounds__(256, 2) void rows_many_kernel(AttnArgs A) {
     __shared__ u32x4 kl[2][TILE * 16], vl[2][D * 8];
     __shared__ uint64_t nf[D];             // values that are not finite
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    Item it;
-    Split sp;
-    uint32_t w = 0, left;
-    int parts = 0;                         // LIST: of every item, 0: shares are even
-    if constexpr (LIST) {
-        const Parts<WIN> P(A, gridDim.x);
-        bool some;
-        if ((parts = P.k)) {
-            w = blockIdx.x < P.items * parts ? xcd_remap(blockIdx.x, P.items * parts) : blockIdx.x;
-            some = P.take(A, w, &left, &it);
-        } else {
-            some = take_share<false, WIN>(A, &sp, &w, &left, &it);
-        }
-        if (!some) {
-            if (tid == 0) A.cut_many[blockIdx.x].np = 0;
-            return;
-        }
-    } else {
-        // The last block of every sequence first, as the longest, and so on; K/V heads change fastest: with
-        // 8 of them each XCD reads one of them only.
-        const int x = blockIdx.x / A.g;
-        it.kvh = blockIdx.x % A.g;
-        it.b = x % A.r.B;
-        it.c = gridDim.x / (A.r.B * A.g) - 1 - x / A.r.B;
-        it.s = seq_rows(A.r, it.b);
-        if (it.c >= blocks_of(it.s, A.m)) return;
-        it.t = 0;
-        it.template begin<WIN>(A);
-        left = it.n;
-    }
+    Part P;
+    if (!take_part<WIN>(A, blockIdx.x, false, &P)) return;
+    Item& it = P.it;
+    const int end = (int)((int64_t)it.n * (P.part + 1) / P.parts);
+    it.t = (int)((int64_t)it.n * P.part / P.parts);
     const int r = A.a / A.g, wcols = A.mw * r;
     Columns<NB, WIN> C;
     u32x4 q[NB][4];
@@ -508,56 +582,32 @@ __global__ __launch_bounds__(256, 2) void rows_many_kernel(AttnArgs A) {
             }
         reads_ahead<1, NB>();
     };
-    bool whole = it.t == 0;
-    int t0 = it.c * A.m + wave * A.mw;        // the wave's first row
-    const size_t at0 = tab.page(A, it);
-    issue(at0, 0);
+    const int t0 = it.c * A.m + wave * A.mw;        // the wave's first row
+    issue(tab.page(A, it), 0);
     C.load_q(A, it, t0, A.mw, q);
     C.begin(A, it.s, t0, A.mw);
-    if constexpr (LIST) {
-        // While the first loads are under way: the item that the share begins and does not end, that of its last tile.
-        if (tid < 64) {
-            CutItem cut{};
-            auto begins = [&](const Item& e, int np) {
-                cut.np = np;
-                cut.row = e.s.row0 + e.c * A.m;
-                cut.n = e.s.n - e.c * A.m;
-                cut.act = e.s.act - e.c * A.m;
-                cut.head = e.kvh * (A.a / A.g);
-            };
-            if (parts) {
-                if (it.t == 0) begins(it, parts);
-            } else if (w + 1 < sp.W) {
-                const uint32_t xe = sp.start(w + 1) - 1;
-                Lanes<false, WIN> L;
-                list_tiles<false, WIN>(A, L);
-                const Item e = find_tile<false, WIN>(A, L, xe);
-                if (e.t + 1 < e.n && xe - e.t >= sp.start(w)) begins(e, sp.wave_of(xe - e.t + e.n - 1) - w + 1);
-            }
-            if (tid == 0) A.cut_many[w] = cut;
-        }
-    }
+    const Span<WIN> B(A, it.s, it.c * A.m, A.m);    // of all its rows
     for (int stg = 0;; stg ^= 1) {
-        const bool ends = it.t + 1 == it.n;
-        bool more = left > 1;
-        Item nx = it;
-        if (more) {
-            if (LIST && ends)
-                more = next_item<WIN>(A, nx);
-            else
-                ++nx.t;
-        }
-        const size_t at = more ? tab.page(A, nx) : 0;
+        const int p0 = TILE * it.template at<WIN>(A);
+        const bool more = ++it.t < end;
+        const size_t at = more ? tab.page(A, it) : 0;
         // This wave's part of the tile is in LDS: vmcnt(0), by the builtin, so that the compiler knows that nothing else is
         // under way either.
         __builtin_amdgcn_s_waitcnt(0x0F70);
         __syncthreads();
-        const int p0 = TILE * it.template at<WIN>(A);
-        // Values that not all of the item's rows see.
+        // Values that not all of the item's rows see: where some are not finite they are taken out.
         bool spoilt = false;
-        const Span<WIN> B(A, it.s, it.c * A.m, A.m);
         if (B.edge(A, p0)) {
-            bool bad = false;
+            uint32_t any = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32x4 x = vl[stg][tid + 256 * i];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) any |= not_finite(x[e]);
+            }
+            spoilt = __syncthreads_or(any);
+        }
+        if (spoilt) {
 #pragma unroll 1
             for (int i = tid; i < D * 8; i += 256) {
                 const int d = i >> 3, c = (i & 7) ^ ((d >> 1) & 7);
@@ -565,18 +615,15 @@ __global__ __launch_bounds__(256, 2) void rows_many_kernel(AttnArgs A) {
                 uint32_t bits = 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int p = p0 + 8 * c + 2 * e;
-                    x[e] &= (B.unseen(A, p) ? 0u : 0xFFFFu) | (B.unseen(A, p + 1) ? 0u : 0xFFFF0000u);
                     const uint32_t b = not_finite(x[e]);
                     bits |= (b >> 15 & 1) << (2 * e) | (b >> 31) << (2 * e + 1);
                     x[e] &= ~halves(b);
                 }
                 vl[stg][i] = x;
                 ((uint8_t*)&nf[d])[c] = (uint8_t)bits;
-                bad |= bits != 0;
             }
-            spoilt = __syncthreads_or(bad);
-            if (spoilt) C.spoil(A, nf, p0);
+            __syncthreads();
+            C.spoil(A, nf, p0);
         }
         if (more) issue(at, stg ^ 1);
         if (C.sees(A, p0)) {
@@ -587,25 +634,63 @@ __global__ __launch_bounds__(256, 2) void rows_many_kernel(AttnArgs A) {
             C.weights(A, sc, pb);
             values(vl[stg], pb);
         }
-        if (ends || !more) {
-            float* piece = A.part + ((2 * (size_t)w + (whole ? 1 : 0)) * A.cols + wave * wcols) * PSTRIDE;
-            C.finish(A, it, t0, A.mw, whole && ends, piece);
-            if (!more) break;
-            whole = true;
-            if constexpr (LIST) {
-                t0 = nx.c * A.m + wave * A.mw;
-                C.load_q(A, nx, t0, A.mw, q);
-                C.begin(A, nx.s, t0, A.mw);
+        if (!more) break;
+    }
+    C.finish(A, it, t0, A.mw, P.parts == 1, A.part + ((size_t)(P.slot + P.part * P.step) * A.cols + wave * wcols) * PSTRIDE);
+}
+
+// Joins the parts of items that have several: workgroup (item, 16 of its columns); half a wave takes two columns, lane
+// i dimensions 4 i .. + 3 of them, two parts requested at a time.
+constexpr int kJoinPartCols = 16;
+template <bool WIN>
+__global__ __launch_bounds__(kJoinThreads) void join_parts_kernel(AttnArgs A) {
+    Part P;
+    if (!take_part<WIN>(A, blockIdx.x, true, &P)) return;
+    const Item& it = P.it;
+    const int np = P.parts, r = A.a / A.g, cols = min(A.cols, (it.s.n - it.c * A.m) * r);
+    const int lane = threadIdx.x & 31, c0 = kJoinPartCols * blockIdx.y + 2 * (threadIdx.x >> 5);
+    if (np == 1 || c0 >= cols) return;
+    const float* p = A.part + (size_t)P.slot * A.cols * PSTRIDE;
+    const size_t step = (size_t)P.step * A.cols * PSTRIDE;
+    float M[2] = {-INFINITY, -INFINITY}, den[2] = {0.f, 0.f};
+    f32x4 num[2] = {};
+    for (int i0 = 0; i0 < np; i0 += 2) {
+        f32x4 v[2][2];
+        f32x2 ml[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                // A part past the last and a column past the item's repeat the last one.
+                const float* s = p + min(i0 + i, np - 1) * step + (size_t)min(c0 + j, cols - 1) * PSTRIDE;
+                v[i][j] = *(const f32x4*)(s + 4 * lane);
+                ml[i][j] = *(const f32x2*)(s + D);
             }
-        }
-        it = nx;
-        --left;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (i0 + i >= np) continue;
+                const float Mn = fmaxf(M[j], ml[i][j][0]), f = __builtin_amdgcn_exp2f(M[j] - Mn), wt = __builtin_amdgcn_exp2f(ml[i][j][0] - Mn);
+                den[j] = den[j] * f + wt * ml[i][j][1];
+                num[j] = num[j] * f + wt * v[i][j];
+                M[j] = Mn;
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int c = c0 + j, t = it.c * A.m + c / r;
+        if (c >= cols) break;
+        const float inv = 1.f / den[j];
+        u32x2 o = {pack2bf(num[j][0] * inv, num[j][1] * inv), pack2bf(num[j][2] * inv, num[j][3] * inv)};
+        if (t >= it.s.act) o = u32x2{0, 0};
+        *(u32x2*)(A.out + ((size_t)(it.s.row0 + t) * A.a + it.kvh * r + c % r) * D + 4 * lane) = o;
     }
 }
 
-// Shares of the list: one wave a SIMD of few columns, as many workgroups as a CU holds of many.
+// Shares of the list: one wave a SIMD.
 int few_shares(int simds) { return std::min(simds, kMaxDecodeSplits); }
-int many_shares(int simds) { return std::max(1, 2 * simds / 4); }
+constexpr int64_t kPieceCols = 1 << 18;      // columns of the pieces: 138 MB
 
 constexpr int kFewCols = 32;      // up to here a wave takes all columns of an item
 template <int NB, bool WIN>
@@ -614,10 +699,6 @@ void launch_few(int nw, int grid, const AttnArgs& A, hipStream_t st) {
     else if (nw == 1) hipLaunchKernelGGL((rows_few_kernel<1, NB, WIN>), dim3(grid), dim3(64), 0, st, A);
     else if (nw == 2) hipLaunchKernelGGL((rows_few_kernel<2, NB, WIN>), dim3(grid), dim3(128), 0, st, A);
     else hipLaunchKernelGGL((rows_few_kernel<4, NB, WIN>), dim3(grid), dim3(256), 0, st, A);
-}
-template <bool LIST, int NB, bool WIN>
-void launch_many(int grid, const AttnArgs& A, hipStream_t st) {
-    hipLaunchKernelGGL((rows_many_kernel<LIST, NB, WIN>), dim3(grid), dim3(256), 0, st, A);
 }
 
 // Waves that take an item of few columns (16 nb) where a launch without a list and a join is the faster one, else 0.  tiles: of
@@ -633,6 +714,79 @@ int few_waves(int64_t items, int64_t tiles, int nb, int simds) {
     return items <= simds / 4 ? 4 : items < simds / 2 ? 2 : 1;
 }
 
+// How many columns are cut: columns of a wave, and the parts of items, by what the launch would take, in us.
+//
+// t1: a tile of a workgroup that has its CU to itself, t2: one of two workgroups'.  A launch takes, whichever is most (and above
+// it where they are alike), its longest part, all tiles on all CUs, or K and V from memory once; of parts that are alike, the
+// rounds of them that the device runs.  Every round begins some parts, and pieces go to memory and back.  What the host has
+// are bounds: of several sequences 0.79 of the longest's tiles counts, and the longest parts may come last.
+//
+// Parts by length (no more than a bound of each sequence's tiles says) cost nothing to find; parts by count, which the device
+// cuts from what the sequences really have, about 5 us more, and need no room for pieces that are not made.  Neither is better
+// throughout.  Measured, the best of 1, 2 and 3 blocks of 16 columns: whole, parts by length, by count; 32 heads on 8.  Alike: a
+// prompt of 2000 rows 49, 60, 58; 4 prompts of 1000 51, 92, 72; 600 rows behind 3000 positions 64, 50, 59; 100 behind 30000
+// 446, 74, 75; 400 behind 30000 448, 214, 198; 8 x 100 behind 3000 67, 62, 72.  Unlike: 4 x 100-800 behind 0-3000 96, 82, 68;
+// 3 x 333-1001 behind 700-5000 147, 118, 120; 3 x 50-500 behind 100-20000 321, 120, 101; 16 x 9-200 behind 10-6000 153, 121,
+// 109; 2 x 300-2000 behind 1000-40000 (64 heads) 1201, no room, 571.
+struct Cut {
+    int nb = 0, longest = 0, parts = 0, jobs = 0, grid = 0, m = 0, cols = 0, slots = 0;
+    int64_t items = 0, sparse = 0, most = 0;      // a bound of the items, and with every sequence as long as the longest
+    double us = 0;
+    Cut() = default;
+    Cut(int nb_, int heads, const AttnArgs& A_, int simds, bool window)
+        : nb(nb_), A(&A_), cus(std::max(simds / 4, 1)), win(window) {
+        const NewRows& r = A->r;
+        m = 4 * std::min(16 * nb / heads, (r.max_new + 3) / 4);
+        cols = m * heads;
+        slots = 2 * cus;
+        items = (int64_t)A->g * (r.rows / m + r.B);
+        sparse = (int64_t)A->g * r.B * ((r.max_new + m - 1) / m);
+    }
+    void by_length(int k, Cut* best) {
+        longest = (int)((most + k - 1) / k);
+        parts = (int)((most + longest - 1) / longest);
+        jobs = 0;
+        if (sparse * parts >= 1 << 24 || (parts > 1 && items * parts * cols > kPieceCols)) return;      // 2^32 threads
+        grid = (int)(sparse * parts);
+        take(best);
+    }
+    void by_count(int count, Cut* best) {
+        parts = 0;
+        jobs = count;
+        if (items >= jobs || sparse > INT32_MAX || (int64_t)jobs * cols > kPieceCols) return;
+        grid = jobs;
+        take(best);
+    }
+
+private:
+    const AttnArgs* A = nullptr;
+    int cus = 1;
+    bool win = false;
+    void take(Cut* best) {
+        static constexpr double t1s[3] = {0.75, 1.14, 1.38}, t2s[3] = {0.57, 0.85, 1.26};
+        const NewRows& r = A->r;
+        const double t1 = t1s[nb - 1], t2 = t2s[nb - 1], n = (double)most;
+        double mean = win ? std::max(n - 1, 1.) : std::max(n - r.max_new / (2. * TILE), n / 2);
+        const bool like = win || mean > 0.8 * n, several = r.B > 1;
+        const double part = several ? 0.79 : 1.;
+        if (!win) mean *= part;
+        const double N = several ? std::min(A->g * ((double)r.rows / m + 0.5 * r.B), (double)sparse) : sparse, T = N * mean;
+        const double L = jobs ? std::ceil(T / std::max(jobs - N, 1.)) : longest;
+        const double n_parts = N * std::max(1., mean / L) + (mean > L && several ? 0.34 * N : 0);
+        const double all = T * t2 / cus, once = part * A->g * r.B * n * (4. * kHalfPage / 6e6);
+        const double rounds = n_parts / slots, full = std::floor(rounds), rest = rounds - full;
+        const double last = rest == 0 ? 0 : rest <= 0.5 ? t1 : t1 + (2 * t2 - t1) * (2 * rest - 1);
+        const double even = T / n_parts * (2 * t2 * full + last), longest_us = std::min(L, n) * t1;
+        const double u = like && (!jobs || !several) ? 0.55 : 0.1;
+        us = 5 + (1 - u) * std::cbrt(longest_us * longest_us * longest_us + all * all * all + once * once * once) +
+             u * std::max(even, std::max(longest_us, once)) + 3.4 * std::ceil(rounds) + grid / 2000.;
+        if (parts != 1) us += 3 + n_parts * cols * (PSTRIDE * 4 * 0.4e-6);
+        if (jobs) us += 4.8;
+        if (several) us += (jobs ? 0.1 : 0.68) * std::min(L, n) * t2;
+        if (!best->nb || us < best->us) *best = *this;
+    }
+};
+
 template <bool WIN>
 hipError_t launch(AttnArgs& A, int simds, hipStream_t st) {
     const NewRows& r = A.r;
@@ -643,13 +797,12 @@ hipError_t launch(AttnArgs& A, int simds, hipStream_t st) {
         if (!WIN) return n;
         return std::min<int64_t>(n, ((int64_t)A.window + m + TILE - 2) / TILE + 1 + (A.sinks + TILE - 1) / TILE);
     };
-    // The list counts tiles in 31 bits; where it might not, items run one by one.
-    auto listed = [&](int64_t items, int m) { return items * most(m) <= INT32_MAX; };
     hipError_t e;
     if (r.max_new * heads <= kFewCols) {
         A.m = r.max_new;
         A.cols = A.m * heads;
-        const int items = r.B * A.g, nw = listed(items, A.m) ? few_waves(items, most(A.m), A.cols <= 16 ? 1 : 2, simds) : 1;
+        // The list counts tiles in 31 bits; where it might not, items run one by one.
+        const int items = r.B * A.g, nw = items * most(A.m) <= INT32_MAX ? few_waves(items, most(A.m), A.cols <= 16 ? 1 : 2, simds) : 1;
         if (nw) {
             if (A.cols <= 16) launch_few<1, WIN>(nw, items, A, st);
             else launch_few<2, WIN>(nw, items, A, st);
@@ -667,67 +820,44 @@ hipError_t launch(AttnArgs& A, int simds, hipStream_t st) {
             hipLaunchKernelGGL(join_few_kernel, dim3(items * A.cols), dim3(kJoinThreads), 0, st, A);
         return hipGetLastError();
     }
-    // Columns of a wave, 16 nb, and items one by one or as a list, by what each would take, in us.  t1: a tile of an item
-    // whose workgroup has its CU to itself; t2: one of two workgroups' (measured: 30000 positions, one block of rows; prompts of
-    // 8192 rows, 64 heads on 8).  One by one: the longest item's tiles one after the other, all tiles on all CUs, or K and V
-    // from memory once, whichever is most (and above it where they are alike).  The list: all tiles on all CUs, or what the L2s (4
-    // MB an XCD) do not hold of K and V for every share, a second launch, and the pieces' way to memory and back, the more the
-    // more items are cut; nb 3 has no list, its pieces cost more than its tiles gain.  Lengths are bounds: of several sequences
-    // 0.8 of them counts, and the list, which shares uneven ones evenly, has its items' cuts for nothing.
-    // Measured, nb 1, 2, 3 one by one, then 1 and 2 listed; 32 heads on 8: a prompt of 700 rows 18, 22, 29, 34, 35; 2000 49, 53,
-    // 69, 97, 85; 4000 164, 136, 141, 253, 204; 4 x 4096 (16 on 8) 338, 274, 264, 472, 401; 60 rows behind 3000 positions 49, 67,
-    // 94, 24, 30; 512 behind 8000 128, 173, 243, 102, 88; 100 behind 30000 446, 593, 841, 87, 80; three chunks of 333-1001
-    // behind 700-5000 146, 146, 185, 147, 129; 8 x 100 behind 3000 67, 72, 96, 125, 73.
-    static constexpr double t1[3] = {0.95, 1.26, 1.79}, t2[3] = {0.60, 0.95, 1.345};
-    const double cus = simds / 4., part = r.B > 1 ? 0.8 : 1., tile_us = 4. * kHalfPage / 6e6;
-    const int shares = many_shares(simds);
-    int nb = 0;
-    bool list = false;
-    double best = 0;
-    for (int i = 1; i <= 3; ++i) {
-        // Rows of a wave: no more than a quarter of the longest sequence's.
-        const int mw = std::min(16 * i / heads, (r.max_new + 3) / 4), m = 4 * mw;
-        if (mw < 1) continue;
-        const int64_t items = (int64_t)A.g * (r.rows / m + r.B), grid = (int64_t)A.g * r.B * ((r.max_new + m - 1) / m);
-        const double n = most(m), mean = part * std::max(WIN ? n - 1 : n - r.max_new / (2. * TILE), n / 2);
-        const double T = A.g * ((double)r.rows / m + 0.5 * r.B) * mean, kv = part * A.g * r.B * n;
-        const double longest = n * t1[i - 1], all = T * t2[i - 1] / cus, once = kv * tile_us;
-        const double again = 2 * items <= shares && r.B == 1 ? once : T * tile_us * std::max(0., 1 - 32e6 / (kv * 4 * kHalfPage));
-        const double one = 5 + std::cbrt(longest * longest * longest + all * all * all + once * once * once) + grid / 2000.,
-                     shared = 18 + 3.5 * i + std::max(all, again) + (r.B > 1 ? 0 : 6. * i * std::min(1., (double)items / shares));
-        if (grid < 1 << 24 && (!nb || one < best)) nb = i, list = false, best = one;          // 2^32 threads
-        if (i < 3 && listed(items, m) && (!nb || shared < best)) nb = i, list = true, best = shared;
+    Cut best;
+    for (int nb = 1; nb <= 3; ++nb) {
+        if (std::min(16 * nb / heads, (r.max_new + 3) / 4) < 1) continue;
+        Cut c(nb, heads, A, simds, WIN);
+        c.most = most(c.m);
+        for (int k = 1; k <= std::min<int64_t>(64, c.most); k += 1 + k / 6) c.by_length(k, &best);
+        if (c.most >= 8)
+            for (int k = 1; k <= 4; ++k) c.by_count(k * c.slots, &best);
     }
-    if (!nb) return hipErrorInvalidValue;
-    A.mw = std::min(16 * nb / heads, (r.max_new + 3) / 4);
-    A.m = 4 * A.mw;
-    A.cols = A.m * heads;
-    const int64_t items = (int64_t)A.g * (r.rows / A.m + r.B);
-    if (!list) {
-        const int grid = A.g * r.B * ((r.max_new + A.m - 1) / A.m);
-        if (nb == 1) launch_many<false, 1, WIN>(grid, A, st);
-        else if (nb == 2) launch_many<false, 2, WIN>(grid, A, st);
-        else launch_many<false, 3, WIN>(grid, A, st);
-        return hipGetLastError();
+    if (!best.nb) {
+        // The longest sequence's blocks times B are more than a grid can have: no item is cut.
+        for (int nb = 1; nb <= 3; ++nb)
+            if (std::min(16 * nb / heads, (r.max_new + 3) / 4) >= 1) best = Cut(nb, heads, A, simds, WIN);
+        best.jobs = 1;
+        best.grid = best.items;
+        if (best.items >= 1 << 24 || best.sparse > INT32_MAX) return hipErrorInvalidValue;
     }
-    A.cut_many = (CutItem*)(A.part + (size_t)2 * shares * A.cols * PSTRIDE);
-    if (nb == 1) launch_many<true, 1, WIN>(shares, A, st);
-    else launch_many<true, 2, WIN>(shares, A, st);
-    if ((e = hipGetLastError()) != hipSuccess || shares == 1) return e;
-    const dim3 join(shares - 1, (A.cols + kJoinCols - 1) / kJoinCols);
-    if (4 * items <= shares)
-        hipLaunchKernelGGL(join_long_kernel, join, dim3(kJoinThreads), 0, st, A);
-    else
-        hipLaunchKernelGGL(join_many_kernel, join, dim3(kJoinThreads), 0, st, A);
+    A.mw = best.m / 4;
+    A.m = best.m;
+    A.cols = best.cols;
+    A.longest = best.longest;
+    A.parts = best.parts;
+    A.jobs = best.jobs;
+    if (best.nb == 1) hipLaunchKernelGGL((rows_many_kernel<1, WIN>), dim3(best.grid), dim3(256), 0, st, A);
+    else if (best.nb == 2) hipLaunchKernelGGL((rows_many_kernel<2, WIN>), dim3(best.grid), dim3(256), 0, st, A);
+    else hipLaunchKernelGGL((rows_many_kernel<3, WIN>), dim3(best.grid), dim3(256), 0, st, A);
+    if ((e = hipGetLastError()) != hipSuccess || best.parts == 1 || best.jobs == 1) return e;
+    const dim3 join(best.jobs ? best.items : best.sparse, (A.cols + kJoinPartCols - 1) / kJoinPartCols);
+    hipLaunchKernelGGL((join_parts_kernel<WIN>), join, dim3(kJoinThreads), 0, st, A);
     return hipGetLastError();
 }
 
 }  // namespace
 
-// Pieces, then what the join reads.
+// Pieces, then what the few columns' join reads.
 size_t attention_rows_bytes(int B, int g, int simds) {
-    const size_t pieces = (size_t)2 * PSTRIDE * sizeof(float) * std::max(kFewCols * few_shares(simds), 256 * many_shares(simds));
-    return pieces + std::max((size_t)B * g * sizeof(int2), (size_t)many_shares(simds) * sizeof(CutItem));
+    const size_t cols = std::max<size_t>(kPieceCols, (size_t)2 * kFewCols * few_shares(simds));
+    return cols * PSTRIDE * sizeof(float) + (size_t)B * g * sizeof(int2);
 }
 
 hipError_t attention_rows(const NewRows& r, int a, int g, int window, int sinks, const uint16_t* q, const uint16_t* kc,

@@ -597,6 +597,75 @@ __global__ __launch_bounds__(256, NB == 1 ? 4 : 3) void attention_many_kernel(At
     }
 }
 
+// Many rows: workgroups for each share, which join the item that it begins and does not end; a wave a pair
+// of columns, with the pieces of both requested together.
+constexpr int kJoinCols = 2 * kJoinWaves;
+__global__ __launch_bounds__(kJoinThreads) void join_many_kernel(ListArgs A) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = A.a / A.g, w0 = blockIdx.x;
+    const CutItem it = A.cut_many[w0];
+    if (it.np == 0) return;
+    const size_t step = (size_t)A.cols * PSTRIDE;
+    const int c0 = kJoinCols * blockIdx.y + 2 * wave;
+    const int cols = min(A.cols, it.n * r);
+    if (c0 >= cols) return;
+    float M[2] = {-INFINITY, -INFINITY}, den[2] = {0.f, 0.f};
+    f32x2 num[2] = {{0.f, 0.f}, {0.f, 0.f}};
+    for (int i0 = 0; i0 < it.np; i0 += 2) {
+        f32x2 v[2][2], ml[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                // A piece past the last and a column past the item's repeat the last one.
+                const float* p = A.part + slot_of(w0, min(i0 + i, it.np - 1)) * step + (size_t)min(c0 + j, cols - 1) * PSTRIDE;
+                v[i][j] = *(const f32x2*)(p + 2 * lane);
+                ml[i][j] = *(const f32x2*)(p + D);
+            }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (i0 + i >= it.np) continue;
+                const float Mn = fmaxf(M[j], ml[i][j][0]), f = exp2f(M[j] - Mn), wt = exp2f(ml[i][j][0] - Mn);
+                den[j] = den[j] * f + wt * ml[i][j][1];
+                num[j][0] = num[j][0] * f + wt * v[i][j][0];
+                num[j][1] = num[j][1] * f + wt * v[i][j][1];
+                M[j] = Mn;
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int c = c0 + j, t = c / r;
+        if (c >= cols) break;
+        const uint32_t o = t < it.act ? pack2bf(num[j][0] / den[j], num[j][1] / den[j]) : 0u;
+        *(uint32_t*)(A.out + ((size_t)(it.row + t) * A.a + it.head + c % r) * D + 2 * lane) = o;
+    }
+}
+
+// The same where items have many pieces.
+__global__ __launch_bounds__(kJoinThreads) void join_long_kernel(ListArgs A) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = A.a / A.g, w0 = blockIdx.x;
+    const CutItem it = A.cut_many[w0];
+    if (it.np == 0) return;
+    const int c0 = kJoinCols * blockIdx.y + 2 * wave;
+    const int cols = min(A.cols, it.n * r);
+    if (c0 >= cols) return;
+    const size_t step = (size_t)A.cols * PSTRIDE;
+    f32x4 num[2];
+    float den[2];
+    // A column past the item's repeats the last one.
+    join_halves<2>(it.np, [&](int i, int j) { return A.part + slot_of(w0, i) * step + (size_t)min(c0 + j, cols - 1) * PSTRIDE; }, num,
+                   den);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int c = c0 + j, t = c / r;
+        if (c >= cols) break;
+        u32x2 o = {pack2bf(num[j][0] / den[j], num[j][1] / den[j]), pack2bf(num[j][2] / den[j], num[j][3] / den[j])};
+        if (t >= it.act) o = u32x2{0, 0};
+        if (lane < 32) *(u32x2*)(A.out + ((size_t)(it.row + t) * A.a + it.head + c % r) * D + 4 * lane) = o;
+    }
+}
+
 // Shares of the list.  Few: one wave a SIMD (of 1, 1.5, 2 and 3 a SIMD, us: 64 x 32768 positions 738, 743,
 // 746, 761; 8 x 64K-128K 287, 290, 292, 299; 16 x 4 rows over 1500-8000 positions 44, 46, 47, 52; 3/4 of a wave
 // 739, 289, 45; half a wave 930, 359, 50; requesting two tiles ahead changes none of them).  Many: as many

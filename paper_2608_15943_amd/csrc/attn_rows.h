@@ -64,7 +64,7 @@ __device__ __forceinline__ int sink_tiles(const ListArgs& A) { return (A.sinks +
 __device__ __forceinline__ int gap_at(const ListArgs& A, int p) {
     return max(p - A.window + 1 - TILE * sink_tiles(A), 0) / TILE;
 }
-// Tiles of block c of a sequence, and of its first c blocks; a block without a row that sees anything
+// Tiles of block c of a sequence, and of its first c blocks (without a window); a block without a row that sees anything
 // counts one (it writes zeros).
 template <bool WIN>
 __device__ __forceinline__ int tiles_of(const ListArgs& A, const SeqRows& s, int c) {
@@ -72,25 +72,19 @@ __device__ __forceinline__ int tiles_of(const ListArgs& A, const SeqRows& s, int
     if (last < c * A.m) return 1;
     return (s.len + last) / TILE + 1 - (WIN ? gap_at(A, s.len + c * A.m) : 0);
 }
-template <bool WIN>
 __device__ __forceinline__ uint32_t tiles_before(const ListArgs& A, const SeqRows& s, int c) {
     const int m = A.m, full = min(c, s.act / m);            // blocks whose m rows all see something
     uint32_t n = full + floor_sum(full, TILE, m, s.len + m - 1);
-    if (WIN) {
-        // The gaps: floor((base + i m) / 64) where that is positive.
-        const int base = s.len - A.window + 1 - TILE * sink_tiles(A);
-        const int c0 = base >= 0 ? 0 : min((m - 1 - base) / m, full);
-        if (c0 < full) n -= floor_sum(full - c0, TILE, m, base + c0 * m);
-    }
-    if (c > full) n += tiles_of<WIN>(A, s, full) + (c - full - 1);
+    if (c > full) n += tiles_of<false>(A, s, full) + (c - full - 1);
     return n;
 }
 __device__ __forceinline__ int blocks_of(const SeqRows& s, int m) { return (s.n + m - 1) / m; }
-// FEW: every sequence has one block at most.
+// FEW: every sequence has one block at most.  (With a window there is no other list.)
 template <bool FEW, bool WIN>
 __device__ __forceinline__ uint32_t seq_tiles(const ListArgs& A, const SeqRows& s) {
+    static_assert(FEW || !WIN);
     if (FEW) return s.n ? tiles_of<WIN>(A, s, 0) : 0;
-    return tiles_before<WIN>(A, s, blocks_of(s, A.m));
+    return tiles_before(A, s, blocks_of(s, A.m));
 }
 
 // The list shared by W waves: wave w starts at tile floor(w T / W).  T < 2^31, W <= 4096.
@@ -186,24 +180,14 @@ __device__ __forceinline__ Item find_tile(const ListArgs& A, Lanes<FEW, WIN>& L,
     rem %= n;
     it.c = 0;
     it.t = rem;
-    if (!FEW && WIN) {
-        // The last block with tiles_before <= rem.
-        int lo = 0, hi = blocks_of(it.s, A.m);
-        while (hi - lo > 1) {
-            const int c = (lo + hi) / 2;
-            if (tiles_before<WIN>(A, it.s, c) <= rem) lo = c;
-            else hi = c;
-        }
-        it.c = lo;
-        it.t = rem - tiles_before<WIN>(A, it.s, lo);
-    } else if (!FEW) {
+    if (!FEW) {
         // The last block with tiles_before <= rem.  About c (1 + (len + m / 2) / 64) + c^2 m / 128 tiles lie
         // before block c: its root, then exactly.
         const float al = A.m / 128.f, be = 1.f + (max(it.s.len, 0) + 0.5f * A.m) / 64.f;
         const int cmax = blocks_of(it.s, A.m) - 1;
         int c = (int)((sqrtf(be * be + 4.f * al * rem) - be) / (2.f * al));
         c = __builtin_amdgcn_readfirstlane(min(max(c, 0), cmax));
-        uint32_t n0 = tiles_before<WIN>(A, it.s, c);
+        uint32_t n0 = tiles_before(A, it.s, c);
         while (c > 0 && n0 > rem) n0 -= tiles_of<WIN>(A, it.s, --c);
         for (; c < cmax; ++c) {
             const uint32_t k = tiles_of<WIN>(A, it.s, c);
@@ -239,51 +223,6 @@ __device__ __forceinline__ bool take_share(const ListArgs& A, Split* sp, uint32_
     *it = find_tile<FEW, WIN>(A, L, x);
     return true;
 }
-// Items cut into equal parts, one a share, in place of the even list.  The blocks of a sequence and K/V head then read the
-// same positions at about the same time and on one XCD (shares run in blocks), and share its L2; even shares begin anywhere,
-// and each reads K and V for itself.  Only where every item has k parts (the device's workgroups over the items, two at
-// least) of nearly as many tiles: no part is longer than 1.4 even shares.
-template <bool WIN>
-struct Parts {
-    uint32_t items;
-    int k;                   // parts of an item, 0: no such cut
-    __device__ __forceinline__ Parts(const ListArgs& A, uint32_t shares) {
-        const int lane = threadIdx.x & 63;
-        float n = 0.f, T = 0.f, hi = 0.f, lo = 1e9f;
-        for (int b = lane; b < A.r.B; b += 64) {
-            const SeqRows s = seq_rows(A.r, b);
-            if (!s.n) continue;
-            const int nb = blocks_of(s, A.m);
-            const float first = tiles_of<WIN>(A, s, 0), last = tiles_of<WIN>(A, s, nb - 1);
-            n += (float)nb * A.g;
-            T += (float)nb * A.g * 0.5f * (first + last);
-            hi = fmaxf(hi, fmaxf(first, last) + (WIN ? 1.f : 0.f));
-            lo = fminf(lo, fminf(first, last));
-        }
-        n = wave_sum(n);
-        T = wave_sum(T);
-        hi = wave_max(hi);
-        lo = -wave_max(-lo);
-        items = n < 1e6f ? (uint32_t)n : 1u << 20;      // exact below 2^24
-        k = items ? shares / items : 0;
-        if (k < 2 || lo < k || ceilf(hi / k) * shares > 1.4f * T) k = 0;
-    }
-    // Part w % k of item w / k: false past the last.
-    __device__ __forceinline__ bool take(const ListArgs& A, uint32_t w, uint32_t* left, Item* it) const {
-        int first;
-        if (w >= items * k) return false;
-        auto count = [&](const SeqRows& s) { return blocks_of(s, A.m) * A.g; };
-        if (!find_item(A.r, w / k, count, &it->b, &it->s, &first)) return false;
-        const int x = w / k - first, nb = blocks_of(it->s, A.m), j = w % k;
-        it->kvh = x / nb;
-        it->c = x % nb;
-        it->template begin<WIN>(A);
-        it->t = (int)((int64_t)it->n * j / k);
-        *left = (int)((int64_t)it->n * (j + 1) / k) - it->t;
-        return *left > 0;
-    }
-};
-
 // The item behind `it` in the list; false past the end.
 template <bool WIN>
 __device__ __forceinline__ bool next_item(const ListArgs& A, Item& it) {
@@ -467,75 +406,6 @@ __global__ __launch_bounds__(kJoinThreads) void join_short_kernel(ListArgs A) {
     u32x2 o = {pack2bf(num[0][0] / den[0], num[0][1] / den[0]), pack2bf(num[0][2] / den[0], num[0][3] / den[0])};
     if (t >= s.act) o = u32x2{0, 0};
     if (lane < 32) *(u32x2*)(A.out + ((size_t)(s.row0 + t) * A.a + kvh * r + c % r) * D + 4 * lane) = o;
-}
-
-// Many rows: workgroups for each share, which join the item that it begins and does not end; a wave a pair
-// of columns, with the pieces of both requested together.
-constexpr int kJoinCols = 2 * kJoinWaves;
-__global__ __launch_bounds__(kJoinThreads) void join_many_kernel(ListArgs A) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = A.a / A.g, w0 = blockIdx.x;
-    const CutItem it = A.cut_many[w0];
-    if (it.np == 0) return;
-    const size_t step = (size_t)A.cols * PSTRIDE;
-    const int c0 = kJoinCols * blockIdx.y + 2 * wave;
-    const int cols = min(A.cols, it.n * r);
-    if (c0 >= cols) return;
-    float M[2] = {-INFINITY, -INFINITY}, den[2] = {0.f, 0.f};
-    f32x2 num[2] = {{0.f, 0.f}, {0.f, 0.f}};
-    for (int i0 = 0; i0 < it.np; i0 += 2) {
-        f32x2 v[2][2], ml[2][2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                // A piece past the last and a column past the item's repeat the last one.
-                const float* p = A.part + slot_of(w0, min(i0 + i, it.np - 1)) * step + (size_t)min(c0 + j, cols - 1) * PSTRIDE;
-                v[i][j] = *(const f32x2*)(p + 2 * lane);
-                ml[i][j] = *(const f32x2*)(p + D);
-            }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (i0 + i >= it.np) continue;
-                const float Mn = fmaxf(M[j], ml[i][j][0]), f = exp2f(M[j] - Mn), wt = exp2f(ml[i][j][0] - Mn);
-                den[j] = den[j] * f + wt * ml[i][j][1];
-                num[j][0] = num[j][0] * f + wt * v[i][j][0];
-                num[j][1] = num[j][1] * f + wt * v[i][j][1];
-                M[j] = Mn;
-            }
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int c = c0 + j, t = c / r;
-        if (c >= cols) break;
-        const uint32_t o = t < it.act ? pack2bf(num[j][0] / den[j], num[j][1] / den[j]) : 0u;
-        *(uint32_t*)(A.out + ((size_t)(it.row + t) * A.a + it.head + c % r) * D + 2 * lane) = o;
-    }
-}
-
-// The same where items have many pieces.
-__global__ __launch_bounds__(kJoinThreads) void join_long_kernel(ListArgs A) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = A.a / A.g, w0 = blockIdx.x;
-    const CutItem it = A.cut_many[w0];
-    if (it.np == 0) return;
-    const int c0 = kJoinCols * blockIdx.y + 2 * wave;
-    const int cols = min(A.cols, it.n * r);
-    if (c0 >= cols) return;
-    const size_t step = (size_t)A.cols * PSTRIDE;
-    f32x4 num[2];
-    float den[2];
-    // A column past the item's repeats the last one.
-    join_halves<2>(it.np, [&](int i, int j) { return A.part + slot_of(w0, i) * step + (size_t)min(c0 + j, cols - 1) * PSTRIDE; }, num,
-                   den);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int c = c0 + j, t = c / r;
-        if (c >= cols) break;
-        u32x2 o = {pack2bf(num[j][0] / den[j], num[j][1] / den[j]), pack2bf(num[j][2] / den[j], num[j][3] / den[j])};
-        if (t >= it.act) o = u32x2{0, 0};
-        if (lane < 32) *(u32x2*)(A.out + ((size_t)(it.row + t) * A.a + it.head + c % r) * D + 4 * lane) = o;
-    }
 }
 
 }  // namespace

@@ -348,6 +348,107 @@ def test_attention_many_blocks_and_many_pieces(a, g, lens, new, window, sinks):
     _check_attention(c, _attention(c, window=window, sinks=sinks), window, sinks)
 
 
+def _spread(B, most_new, most_len, seed):
+    """Lengths and new rows that are unlike each other; the longest last."""
+    rng = np.random.default_rng(seed)
+    lens, new = rng.integers(0, most_len, B), rng.integers(1, most_new, B)
+    lens[-1], new[0] = most_len, most_new
+    return lens.tolist(), new.tolist()
+
+
+PARTS = [
+    # a, g, cached, new, window, sinks.  Items in parts of a bounded length, by 16, 32 and 48 columns a wave
+    (4, 1, [5000], [40], 0, 0), (16, 1, [9000], [33], 0, 0), (4, 2, [100, 9000, 0, -1, 3000], [30, 200, 0, 5, 90], 0, 0),
+    (2, 1, [30000, 5], [17, 100], 0, 0), (16, 8, [2000], [100], 0, 0), (32, 8, [3000], [20], 0, 0),
+    (4, 1, [5000], [40], 3000, 4), (16, 8, [20, 7000, 900], [90, 20, 120], 1000, 100), (16, 16, [100], [400], 333, 0),
+    (5, 1, *_spread(70, 20, 1500, 1), 0, 0), (5, 1, *_spread(70, 20, 3000, 2), 1500, 4),
+    # in parts of a bounded number; of more sequences than a wave has lanes, too
+    (64, 16, *_spread(6, 20, 6000, 3), 0, 0), (16, 16, *_spread(6, 250, 3000, 4), 0, 0), (32, 8, *_spread(6, 400, 6000, 5), 0, 0),
+    (12, 4, *_spread(70, 20, 3000, 6), 0, 0), (5, 1, *_spread(70, 60, 6000, 7), 0, 0), (16, 1, *_spread(70, 60, 3000, 8), 0, 0),
+    (16, 16, *_spread(12, 9, 12000, 9), 3000, 4),
+    # whole, 48 columns a wave
+    (64, 16, *_spread(4, 400, 1500, 10), 0, 0), (64, 16, *_spread(4, 400, 1500, 11), 700, 4),
+]
+
+
+@pytest.mark.parametrize("a,g,lens,new,window,sinks", PARTS)
+def test_attention_items_in_parts(a, g, lens, new, window, sinks):
+    say(f"[parts] a={a} g={g} lens={lens[:6]} new={new[:6]} window={window} sinks={sinks}")
+    c = Case(a, g, lens, new, seed=35)
+    _fill(c)
+    if window:
+        _drop_unseen(c, window, sinks)
+    _check_attention(c, _attention(c, window=window, sinks=sinks), window, sinks)
+
+
+@pytest.mark.parametrize("a,g,B,max_new,rows,max_pos,window", [
+    (16, 16, 12, 60, 88, 12000, 3000), (32, 8, 3, 250, 319, 12000, 3000), (4, 2, 3, 20, 20, 6000, 300), (32, 8, 2, 20, 40, 1500, 300),
+    (16, 16, 12, 60, 88, 12000, 0), (16, 8, 6, 90, 200, 12000, 0), (16, 1, 3, 64, 100, 40000, 0), (16, 16, 12, 60, 88, 12000, 10**6),
+])
+def test_attention_parts_of_loose_bounds(a, g, B, max_new, rows, max_pos, window):
+    """Parts that are laid out for bounds far above what the device finds: few rows, short contexts, none, inactive."""
+    lens = [[300, 0, -1, 64, 1100, 63, 1, 65, 127, 128, 2, 500][i] for i in range(B)]
+    new = [[17, 1, 2, 0, 9, 3, 1, 1, 5, 2, 7, 4][i] for i in range(B)]
+    say(f"[parts] a={a} g={g} B={B} max_new={max_new} rows={rows} max_pos={max_pos} window={window}")
+    c = Case(a, g, lens, new, seed=36, rows=rows, stride=max_pos // 64 + 1)
+    _fill(c)
+    got = _attention(c, max_pos=max_pos, max_new=max_new, max_seq=max_new, window=window, sinks=70 if window else 0)
+    _check_attention(c, got, window, 70 if window else 0)
+
+
+@pytest.mark.parametrize("a,lens,new", [(4, [3000], [40]), (16, *_spread(6, 250, 3000, 12))])
+@pytest.mark.parametrize("window", [0, 500])
+def test_attention_values_that_are_not_finite_in_parts(a, lens, new, window):
+    """A NaN or an infinity in one part of an item reaches the rows that see it, through the join, and no others."""
+    c = Case(a, a, lens, new, seed=37)
+    _fill(c)
+    n, T = lens[0], new[0]
+    _poke(c, 1, 0, 5, 0, 3, np.nan)
+    _poke(c, 1, 0, max(n - 490, 6), 1, 100, np.inf)         # leaves some rows' windows
+    _poke(c, 1, 0, n + T // 2, 2, 64, -np.inf)
+    _poke(c, 0, 0, n + T - 3, 3, 17, np.nan)
+    got = _attention(c, window=window)
+    for b in range(len(lens)):
+        for t in (0, T // 2 - 1, T // 2, T - 4, T - 3, T - 1) if b == 0 else (0, new[b] - 1):
+            for h in range(4):
+                want = _by_row(c, b, t, h, window, 0)
+                assert np.array_equal(np.isfinite(got[c.cu[b] + t, h]), np.isfinite(want)), (b, t, h)
+
+
+def test_attention_parts_that_score_minus_infinity():
+    """Whole parts of -infinity weigh nothing; rows that see nothing else are NaN."""
+    c = Case(4, 1, [4000], [40], seed=38)
+    _fill(c)
+    c.x[:, :4] = np.abs(c.x[:, :4])
+    q = c.x[:, :4].astype(np.float64)
+    want, tol = rr.attention(q, c.cache.values(c.table, 0, 4040)[:, 3900:], 100, 4)
+    for hi in (3900, 4040):
+        for p in range(hi):
+            c.cache.k[0, c.table[0][p // 64], p % 64, 0] = 0xFF80
+        got = _attention(c)
+        assert (np.abs(got - want) <= tol).all() if hi == 3900 else np.isnan(got).all()
+
+
+@pytest.mark.parametrize("a,g,lens,new", [(4, 2, [3000, 100, 2000], [40, 40, 40]), (16, 16, *_spread(6, 250, 3000, 4))])
+def test_attention_of_offsets_that_go_back_stays_in_bounds(a, g, lens, new):
+    """Sequences that overlap are no valid call; nothing outside its rows and its workspace is written."""
+    c = Case(a, g, lens, new, seed=39)
+    _fill(c)
+    dev = c.cache.to_device()
+    m = rr.model(a, g, dev, c.cache.n_pages, len(lens), c.rows)
+    r, keep = rr.rows_of(lens, new, c.table)
+    keep["cu"][1::2] = c.rows
+    keep["cu"][2::2] = 0
+    q = _dev(c.x[:, :a].reshape(c.rows, -1))
+    out = torch.full((c.rows + 8, a * D), 55.0, dtype=torch.bfloat16, device="cuda")
+    n = m.kvp_workspace_size(kb.KVP_PHASE_STEP, len(lens), c.rows)
+    ws = torch.full((n + 4096,), 0xAB, dtype=torch.uint8, device="cuda")
+    m.kvp_attention(0, q.data_ptr(), r, out.data_ptr(), ws.data_ptr(), n, _stream())
+    torch.cuda.synchronize()
+    assert (out[c.rows:] == 55.0).all() and (ws[n:] == 0xAB).all()
+    assert c.cache.from_device(dev).same(c.cache)
+
+
 def test_attention_one_row_each_without_cu():
     c = Case(8, 2, [5, -1, 31, 1500, 64, 0], [1] * 6, seed=12)
     _fill(c)
