@@ -228,6 +228,12 @@ struct Columns : Span<WIN> {
 
 // At most 16 NB columns.  NW 0: a share of the list, one wave.  Else one item, whose tiles NW waves take in turn and
 // join in LDS.
+//
+// Bound by memory: K and V are read once, straight into registers, 32 KB a tile and one wave a SIMD, which has 16 to 32 KB
+// requested at any time; a tile takes 5.5 us of the device's rate and some 1 us of vector and matrix work beside it.  64
+// sequences behind 16384 positions (32 heads on 8; 4.3 GB) 704 us, 6.1 TB/s, what a bare read reaches; 64 behind 3000-40000 in
+// windows of 4096 (1.07 GB) 195 us, 5.5 TB/s; 16 x 4 rows behind 1500-8000 (312 MB) 63 us, 4.9 TB/s: 9 or 10 tiles a wave, the
+// first behind the list, a length, a page number and a page, one after the other.  The join takes 4 to 5 us more.
 template <int NW, int NB, bool WIN>
 __global__ __launch_bounds__(NW ? 64 * NW : 64, 1) void rows_few_kernel(AttnArgs A) {
     constexpr bool LIST = NW == 0;
@@ -530,6 +536,14 @@ __device__ __forceinline__ bool take_part(const AttnArgs& A, int x, bool join, P
 // Workgroup: a part of an item of 4 mw rows, wave v's 16 NB columns are its rows v mw .. (v + 1) mw - 1.  The tiles go from
 // memory to LDS directly, two stages of 32 KB, one barrier a tile: it ends the loads of the tile that comes and the reads of
 // the one before it, whose stage is then loaded again.  Two workgroups a CU run in each other's waits.
+//
+// Bound by LDS and the matrix and vector units together.  A fragment of K or V that is read from LDS serves NB products: of 16
+// columns a wave the reads take longer than the products (8192 rows, 64 heads on 8: 1220 us), of 32 about as long (980), of 48
+// less (912 us, 1207 TFLOP/s; a large product of the library 1310-1400), with 242 of 256 registers; of 64 the accumulators
+// leave the first half of the registers (slower).  The reads of fragments run four ahead of the products.  The exponentials of
+// a tile take about half the products' time and run beside the other workgroup's.
+// Other ways: K a tile ahead of the softmax, 5 % slower at 32 columns; loads by the compiler's builtin, which waits for them
+// before every read of LDS, 4 %.
 template <int NB, bool WIN>
 __global__ __launch_bounds__(256, 2) void rows_many_kernel(AttnArgs A) {
     // K: chunk c (16 bytes, 8 dimensions) of row R at place c ^ key(R) of its 16, key of the bits that differ among the 16 rows
@@ -719,7 +733,8 @@ int few_waves(int64_t items, int64_t tiles, int nb, int simds) {
 // t1: a tile of a workgroup that has its CU to itself, t2: one of two workgroups'.  A launch takes, whichever is most (and above
 // it where they are alike), its longest part, all tiles on all CUs, or K and V from memory once; of parts that are alike, the
 // rounds of them that the device runs.  Every round begins some parts, and pieces go to memory and back.  What the host has
-// are bounds: of several sequences 0.79 of the longest's tiles counts, and the longest parts may come last.
+// are bounds: of several sequences 0.79 of the longest's tiles counts, and the longest parts may come last (not of prompts
+// without a context, of which the longest begin).
 //
 // Parts by length (no more than a bound of each sequence's tiles says) cost nothing to find; parts by count, which the device
 // cuts from what the sequences really have, about 5 us more, and need no room for pieces that are not made.  Neither is better
@@ -782,7 +797,7 @@ private:
              u * std::max(even, std::max(longest_us, once)) + 3.4 * std::ceil(rounds) + grid / 2000.;
         if (parts != 1) us += 3 + n_parts * cols * (PSTRIDE * 4 * 0.4e-6);
         if (jobs) us += 4.8;
-        if (several) us += (jobs ? 0.1 : 0.68) * std::min(L, n) * t2;
+        if (several && n * TILE >= r.max_new + TILE) us += (jobs ? 0.1 : 0.68) * std::min(L, n) * t2;     // cached contexts
         if (!best->nb || us < best->us) *best = *this;
     }
 };
