@@ -654,6 +654,65 @@ def test_equal_calls_give_equal_bits():
         assert np.array_equal(a, b)
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (500, 3)])
+def test_attention_captured_in_parts_follows_the_lengths(window, sinks):
+    """Two captured calls on one workspace, bounds far above most lengths, replayed in turn with other lengths and rows, eager
+    calls between them: each as the reference and as the same eager call, bit for bit."""
+    most = [300, 0, 64, 1100, 63, 1, 65, 127, 128, 2, 500, 2000]
+    B, a = len(most), 16
+    c = Case(a, a, most, [60] * B, seed=40, stride=12000 // 64 + 1)
+    _fill(c)
+    dev = c.cache.to_device()
+    m = rr.model(a, a, dev, c.cache.n_pages, B, 720)
+    if window:
+        m.kvp_set_layer_window(0, window, sinks)
+    calls, n = [], 0
+    for rows, max_new, max_pos in ((88, 60, 11999), (720, 60, 2059)):
+        r, keep = rr.rows_of(most, [0] * B, c.table, rows=rows, max_new=max_new, max_pos=max_pos)
+        q = _dev(c.x[:rows, :a].reshape(rows, -1))
+        calls.append((r, keep, q, torch.empty_like(q)))
+        n = max(n, m.kvp_workspace_size(kb.KVP_PHASE_STEP, B, rows))
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+
+    def run(i):
+        r, _, q, out = calls[i]
+        m.kvp_attention(0, q.data_ptr(), r, out.data_ptr(), ws.data_ptr(), n, torch.cuda.current_stream().cuda_stream)
+
+    with torch.cuda.stream(torch.cuda.Stream()):
+        run(0), run(1)
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in calls]
+    for i, g in enumerate(graphs):
+        with torch.cuda.graph(g):
+            run(i)
+    rng = np.random.default_rng(41)
+    for rep in range(4):
+        for i, g in enumerate(graphs):
+            r, keep, q, out = calls[i]
+            new = rng.multinomial(int(rng.integers(1, 88)), np.ones(B) / B) if i == 0 else rng.integers(0, 61, B)
+            lens = [int(x) if rep == 0 else int(rng.integers(-1, x + 1)) for x in most]
+            cu = np.concatenate([[0], np.cumsum(new)])
+            keep["len"].copy_(torch.tensor(lens, dtype=torch.int32))
+            keep["cu"].copy_(torch.tensor(cu, dtype=torch.int32))
+            out.fill_(55.0)
+            run(i)
+            eager = out.clone()
+            out.fill_(55.0)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, eager), (rep, i)
+            got = out.float().cpu().numpy().reshape(-1, a, D)
+            assert (got[cu[-1]:] == 55.0).all()
+            for b in range(B):
+                rows = slice(cu[b], cu[b + 1])
+                if lens[b] < 0:
+                    assert (got[rows] == 0).all()
+                elif new[b]:
+                    kv = c.cache.values(c.table, b, lens[b] + new[b])
+                    want, tol = rr.attention(c.x[rows, :a].astype(np.float64), kv, lens[b], a, window, sinks)
+                    assert (np.abs(got[rows] - want) <= tol).all(), (rep, i, b)
+
+
 def test_noalloc_step_refuses_a_layer_with_a_window():
     m = kb.Model(1, 512, 4, 2, D, kb.KVP_DTYPE_BF16, [0], max_batch=2, max_seq=64, kv_capacity=64)
     t = torch.zeros(1 << 20, dtype=torch.bfloat16, device="cuda")
