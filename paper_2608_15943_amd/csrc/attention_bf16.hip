@@ -435,8 +435,8 @@ __device__ __forceinline__ void load_4kb(i32x4 page, uint32_t lds, uint32_t at, 
                  "s_mov_b32 m0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %8, %9, %13 offen lds\n\t"
                  "s_mov_b32 m0, %0"
                  : "=&s"(m0)
-                 : "s"(lds), "s"(lds + 1024), "s"(lds + 2048), "s"(lds + 3072), "v"(v0), "v"(v1), "v"(v2), "v"(v3), "s"(page),
-                   "s"(at), "s"(at + 1024), "s"(at + 2048), "s"(at + 3072)
+                 : "s"(lds), "s"(lds + 1 * 1024), "s"(lds + 2 * 1024), "s"(lds + 3 * 1024), "v"(v0), "v"(v1), "v"(v2), "v"(v3), "s"(page),
+                   "s"(at), "s"(at + 1 * 1024), "s"(at + 2 * 1024), "s"(at + 3 * 1024)
                  : "memory");
 }
 
