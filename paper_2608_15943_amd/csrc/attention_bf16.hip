@@ -517,25 +517,41 @@ __device__ __forceinline__ bool take_part(const AttnArgs& A, int x, bool join, P
                     items = blocks_of(s, A.m) * A.g;
                 }
             }
-            const int jobs = items ? items * ((most_tiles<WIN>(A, s) + longest - 1) / longest) : 0;
-            int ip = items, jp = jobs;
+            const int tiles = items ? most_tiles<WIN>(A, s) : 0, k = (tiles + longest - 1) / longest, jobs = items * k;
+            int ie = 0, je = 0;            // before this lane's sequence
+            if (A.r.B <= 8) {
+                // The sequence of the longest parts first: a few sequences end with short ones (3 chunks 118 us, in their order
+                // 127; 6 of 13-900 rows 104, 113).  Many mix the long contexts of few rows, bound by memory, with the rest in
+                // any order, and are slower sorted (8: 132 and 134 us; 16: 123 and 109; 32: 127 and 114).
+                const int each = k ? (tiles + k - 1) / k : 0;
+                for (int i = 0; i < A.r.B; ++i) {
+                    const int e = __builtin_amdgcn_readlane(each, i), u = __builtin_amdgcn_readlane(items, i),
+                              v = __builtin_amdgcn_readlane(jobs, i);
+                    if (e > each || (e == each && i < lane)) ie += u, je += v;
+                }
+            } else {
+                ie = items, je = jobs;
 #pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const int u = __shfl_up(ip, off), v = __shfl_up(jp, off);
-                if (lane >= off) ip += u, jp += v;
+                for (int off = 1; off < 64; off <<= 1) {
+                    const int u = __shfl_up(ie, off), v = __shfl_up(je, off);
+                    if (lane >= off) ie += u, je += v;
+                }
+                ie -= items, je -= jobs;
             }
-            const int w = __popcll(__ballot(join ? item0 + ip <= x : job0 + jp <= x));    // lanes before the one that holds x
-            if (w < 64) {
+            const int at = x - (join ? item0 + ie : job0 + je);
+            const uint64_t here = __ballot(at >= 0 && at < (join ? items : jobs));
+            if (here) {
+                const int w = __builtin_ctzll(here);
                 it.b = b0 + w;
                 it.s = {__builtin_amdgcn_readlane(s.row0, w), __builtin_amdgcn_readlane(s.n, w), __builtin_amdgcn_readlane(s.len, w),
                         __builtin_amdgcn_readlane(s.act, w)};
                 n = __builtin_amdgcn_readlane(items, w);
-                item0 += __builtin_amdgcn_readlane(ip - items, w);
-                job0 += __builtin_amdgcn_readlane(jp - jobs, w);
+                item0 += __builtin_amdgcn_readlane(ie, w);
+                job0 += __builtin_amdgcn_readlane(je, w);
                 break;
             }
-            item0 += __builtin_amdgcn_readlane(ip, 63);
-            job0 += __builtin_amdgcn_readlane(jp, 63);
+            item0 += __builtin_amdgcn_readlane(ie + items, 63);
+            job0 += __builtin_amdgcn_readlane(je + jobs, 63);
         }
         x -= join ? item0 : job0;
         p->part = x / n;
