@@ -2,7 +2,8 @@
 // sequence b sits at position len_b + i and sees positions [0, len_b + i], or those of them that lie in its window or below
 // `sinks` (WIN).
 //
-// Columns, items, the list of tiles and the join are attn_rows.h's.  Scores and values on v_mfma_f32_16x16x32_bf16:
+// Columns, items, the list of tiles of few columns and its join are attn_rows.h's; items of more columns run whole or in
+// parts (take_part).  Scores and values on v_mfma_f32_16x16x32_bf16:
 //
 //   S^T = K Q^T  Row rho of score block tb = 2 s + e is position 32 s + 8 (rho / 4) + 4 e + rho % 4 of the tile, so that lane
 //                group grp ends with positions 32 s + 8 grp .. + 7 of its column: the run that a lane of the second product
