@@ -12,8 +12,8 @@
 //                weights is taken from the rounded ones, so that their rounding cancels where it is common.
 //
 // A weight is 0 where its position is hidden, but 0 times a value that is not finite is not.  In tiles that some row of an
-// item does not see whole, values that no row sees count as 0, and those that are not finite are taken out of the product
-// and put into the rows that see them (as NaN): what a hidden position holds reaches no row.
+// item does not see whole, values that are not finite are taken out of the product and put, as NaN, into the rows that see
+// them: what a hidden position holds reaches no row.
 #include <math.h>
 
 #include <algorithm>
