@@ -576,8 +576,8 @@ __device__ __forceinline__ bool take_part(const AttnArgs& A, int x, bool join, P
 // less (912 us, 1207 TFLOP/s; a large product of the library 1310-1400), with 242 of 256 registers; of 64 the accumulators
 // leave the first half of the registers (slower).  The reads of fragments run four ahead of the products.  The exponentials of
 // a tile take about half the products' time and run beside the other workgroup's.
-// Other ways: K a tile ahead of the softmax, 5 % slower at 32 columns; loads by the compiler's builtin, which waits for them
-// before every read of LDS, 4 %.
+// Other ways, both slower: K a tile ahead of the softmax, and loads by the compiler's builtin, which waits for them before
+// reads of LDS (prompts of 4 x 4096 and 8192 rows 1 %, chunks and windows 3 %).
 template <int NB, bool WIN>
 __global__ __launch_bounds__(256, 2) void rows_many_kernel(AttnArgs A) {
     // K: chunk c (16 bytes, 8 dimensions) of row R at place c ^ key(R) of its 16, key of the bits that differ among the 16 rows
