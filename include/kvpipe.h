@@ -439,9 +439,14 @@ int kvp_decode_step_paged(kvp_ctx* ctx, const void* x, const int32_t* len_dev, i
  *                         there that another sequence holds too is replaced, in seq's row, by a
  *                         free one.  src[i], dst[i], i < *n: the page it was and the page it
  *                         is now; the caller copies them (kvp_copy_pages, kvp_copy_pages_fp8) before
- *                         the append.  Positions without a page are left out (reserve them first).
- *                         All or nothing: KVP_E_CAPACITY when the pool has too few free pages or
- *                         more than max_pairs would have to be copied (*n = 0, nothing changes).
+ *                         the append.  Pages there that kvp_pager_trim let go of are replaced by
+ *                         free ones too (nothing to copy), but for those of a row's beginning that
+ *                         has pages behind them: a window's, which stay away.  KVP_E_CAPACITY when
+ *                         `from` lies on a page that is gone and the position in front of it on
+ *                         one too (a rollback, or a fork, to behind a window).  Positions behind the
+ *                         row's end are left out (reserve them).  All or nothing: KVP_E_CAPACITY
+ *                         when the pool has too few free pages or more than max_pairs would have to
+ *                         be copied (*n = 0, nothing changes).
  *   kvp_pager_trim     -- lets go of the pages of seq that lie wholly in positions [from, to):
  *                         their entries become -1, the row's end stays where it is; to <= from
  *                         does nothing.  With an attention window, rows from position p on

@@ -5,7 +5,8 @@
 // amount of HBM holds: that is the capacity side of KV sharing.
 //
 // A page may be held by several sequences (a shared prefix, after a fork): refs counts them, and a page
-// is free when nobody holds it.  A row may have holes (-1) where a window has left pages behind.
+// is free when nobody holds it.  A row may have holes (-1) where a window has left pages behind, or where
+// tokens were not accepted; who writes there gets pages again (kvp_pager_own).
 //
 // Pure host code: no device memory is touched; the caller copies table rows to the device, and pages
 // (kvp_copy_pages) where a call here says so.
@@ -135,13 +136,24 @@ extern "C" int kvp_pager_own(kvp_pager* p, int seq, int from, int to, int32_t* s
     int32_t* row = p->row(seq);
     const int j0 = from / kPageTokens;
     const int j1 = from == to ? j0 : std::min<int64_t>(((int64_t)to + kPageTokens - 1) / kPageTokens, p->held[seq]);
-    int need = 0;
-    for (int j = j0; j < j1; ++j) need += row[j] >= 0 && p->refs[row[j]] > 1;
-    if ((size_t)need > p->free.size())
-        return fail(KVP_E_CAPACITY, "kvp_pager_own: %d pages needed, %zu free", need, p->free.size());
-    if (need > max_pairs) return fail(KVP_E_CAPACITY, "kvp_pager_own: %d pages to copy, room for %d", need, max_pairs);
+    // Rows at `from` follow the position in front of it: a page for theirs alone would be no use.
+    if (j0 < j1 && row[j0] < 0 && from > 0 && row[(from - 1) / kPageTokens] < 0)
+        return fail(KVP_E_CAPACITY, "kvp_pager_own: sequence %d has no page for position %d", seq, from - 1);
+    // Holes from the row's beginning up to its first page are a window's and stay.
+    int first = 0, pairs = 0, gone = 0;
+    while (first < p->held[seq] && row[first] < 0) ++first;
+    if (first == p->held[seq]) first = 0;
+    for (int j = j0; j < j1; ++j) {
+        pairs += row[j] >= 0 && p->refs[row[j]] > 1;
+        gone += row[j] < 0 && j >= first;
+    }
+    if ((size_t)pairs + gone > p->free.size())
+        return fail(KVP_E_CAPACITY, "kvp_pager_own: %d pages needed, %zu free", pairs + gone, p->free.size());
+    if (pairs > max_pairs) return fail(KVP_E_CAPACITY, "kvp_pager_own: %d pages to copy, room for %d", pairs, max_pairs);
     for (int j = j0; j < j1; ++j)
-        if (row[j] >= 0 && p->refs[row[j]] > 1) {
+        if (row[j] < 0) {
+            if (j >= first) row[j] = p->take();
+        } else if (p->refs[row[j]] > 1) {
             src[*n] = row[j];
             --p->refs[row[j]];
             row[j] = dst[*n] = p->take();
