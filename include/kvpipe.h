@@ -425,16 +425,18 @@ int kvp_decode_step_paged(kvp_ctx* ctx, const void* x, const int32_t* len_dev, i
  * from a fresh pager, and a released sequence's pages are reused first.
  *   kvp_pager_reserve  -- grow sequence seq to hold positions [0, n_tokens);
  *                         all or nothing: KVP_E_CAPACITY when the pool or the
- *                         row is too small (nothing changes); never shrinks.
+ *                         row is too small (nothing changes); never shrinks.  Pages inside
+ *                         the row that kvp_pager_trim let go of stay away; KVP_E_CAPACITY too
+ *                         when the last page of the row that [0, n_tokens) reaches is one.
  *   kvp_pager_release  -- return all of seq's pages.
  *   kvp_pager_rows     -- copy the rows of seqs[0..B) to out [B][max_pages_per_seq]
  *                         (host memory; the caller copies it to the device).
  *
  * Several sequences may hold one page; it is free when the last of them lets go of it.
  *   kvp_pager_fork     -- sequence `to`, which holds none, gets the pages of `from` that hold
- *                         positions [0, n_tokens): the same pages, nothing is copied.
- *                         KVP_E_STATE where `to` holds pages, KVP_E_CAPACITY where `from` has
- *                         no pages for so many tokens.
+ *                         positions [0, n_tokens): the same pages, nothing is copied; what was
+ *                         trimmed there is missing in both.  KVP_E_STATE where `to` holds pages,
+ *                         KVP_E_CAPACITY where the row of `from` ends before so many tokens.
  *   kvp_pager_own      -- before rows are appended at positions [from, to) of seq: every page
  *                         there that another sequence holds too is replaced, in seq's row, by a
  *                         free one.  src[i], dst[i], i < *n: the page it was and the page it
@@ -450,7 +452,10 @@ int kvp_decode_step_paged(kvp_ctx* ctx, const void* x, const int32_t* len_dev, i
  *   kvp_pager_trim     -- lets go of the pages of seq that lie wholly in positions [from, to):
  *                         their entries become -1, the row's end stays where it is; to <= from
  *                         does nothing.  With an attention window, rows from position p on
- *                         see nothing in [sinks, p - window + 1).
+ *                         see nothing in [sinks, p - window + 1).  Of tokens that were not
+ *                         accepted, too; a row that then ends in trimmed pages grows after
+ *                         kvp_pager_own has given it pages for what is written there.  (A window
+ *                         of 1 can leave the row's last page behind: reserve first, then trim.)
  *   kvp_pager_compact  -- moves pages that are held so that they come to lie in front of all
  *                         free ones, at most max_pairs in this call: rows then hold the new
  *                         pages, and the caller copies src[i] to dst[i], i < *n, before it

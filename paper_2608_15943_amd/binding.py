@@ -472,7 +472,8 @@ class Pager:
         _check(lib().kvp_pager_reserve(self.p, seq, n_tokens), "kvp_pager_reserve")
 
     def try_reserve(self, seq, n_tokens) -> bool:
-        """reserve(); False (and nothing reserved) when the pool or the row is too small."""
+        """reserve(); False (and nothing reserved) when the pool or the row is too small, or the row ends in pages that
+        were trimmed (own() first)."""
         rc = lib().kvp_pager_reserve(self.p, seq, n_tokens)
         if rc == KVP_E_CAPACITY:
             return False
@@ -486,7 +487,8 @@ class Pager:
         _check(lib().kvp_pager_fork(self.p, src, dst, n_tokens), "kvp_pager_fork")
 
     def own(self, seq, start, end, max_pairs=None):
-        """Pages (src, dst), numpy int32, that the caller copies before it appends at [start, end)."""
+        """Pages (src, dst), numpy int32, that the caller copies before it appends at [start, end); pages there that were
+        trimmed are replaced."""
         if max_pairs is None:
             max_pairs = max((end + 63) // 64 - start // 64, 0)
         return self._pairs("kvp_pager_own", max_pairs, lambda *a: lib().kvp_pager_own(self.p, seq, start, end, *a))

@@ -87,16 +87,19 @@ extern "C" void kvp_pager_destroy(kvp_pager* p) { delete p; }
 extern "C" int kvp_pager_reserve(kvp_pager* p, int seq, int n_tokens) {
     if (const int rc = check_seq(p, seq, "kvp_pager_reserve")) return rc;
     if (n_tokens < 0) return fail(KVP_E_INVALID_ARG, "kvp_pager_reserve: n_tokens < 0");
-    const int64_t need = ((int64_t)n_tokens + 63) / 64;
+    const int64_t need = ((int64_t)n_tokens + kPageTokens - 1) / kPageTokens;
     if (need > p->max_pages)
         return fail(KVP_E_CAPACITY, "kvp_pager_reserve: %d tokens need %lld pages, a row holds %d", n_tokens,
                     (long long)need, p->max_pages);
-    const int have = p->held[seq];
+    const int have = p->held[seq], last = std::min((int)need, have) - 1;
+    int32_t* row = p->row(seq);
+    if (last >= 0 && row[last] < 0)
+        return fail(KVP_E_CAPACITY, "kvp_pager_reserve: positions from %d on of sequence %d were trimmed (kvp_pager_own maps them)",
+                    last * kPageTokens, seq);
     if (need <= have) return ok();
     const int add = (int)need - have;
     if ((size_t)add > p->free.size())
         return fail(KVP_E_CAPACITY, "kvp_pager_reserve: %d more pages needed, %zu free", add, p->free.size());
-    int32_t* row = p->row(seq);
     for (int j = have; j < (int)need; ++j) row[j] = p->take();
     p->held[seq] = (int)need;
     return ok();

@@ -99,3 +99,115 @@ def test_own_refuses_positions_behind_ones_that_are_gone():
     assert p.own(0, 960, 1024)[0].size == 0             # the window's own pages
     p.trim(0, 0, 1024)
     assert p.own(0, 0, 1)[0].size == 0 and p.rows([0])[0, 0] >= 0   # from the beginning again
+
+
+# ---- reserve ----------------------------------------------------------------------------------------
+
+def test_reserve_refuses_a_row_whose_end_was_trimmed():
+    p = kb.Pager(12, 2, 10)
+    p.reserve(0, 64)
+    p.reserve(1, 300)
+    p.trim(1, 192, 320)
+    before = _state(p, 2)
+    for n in (193, 256, 300, 320, 321, 500):            # positions from 192 on, with growth and without
+        assert not p.try_reserve(1, n)
+        assert _code(p.reserve, 1, n) == kb.KVP_E_CAPACITY
+    for n in (0, 64, 100, 192):                         # all there
+        p.reserve(1, n)
+    assert _state(p, 2) == before
+    p.own(1, 192, 300)
+    p.reserve(1, 300)
+    p.reserve(1, 321)
+    assert (p.rows([1])[0, :6] >= 0).all()
+
+
+def test_reserve_refuses_a_fork_to_behind_a_window():
+    p = kb.Pager(24, 2, 20)
+    p.reserve(0, 1280)
+    p.trim(0, 64, 1024)
+    p.fork(0, 1, 1000)
+    for n in (1000, 1024, 1100):
+        assert not p.try_reserve(1, n)
+    p.release(1)
+    p.fork(0, 1, 1030)                                  # the window's pages: goes on
+    p.reserve(1, 1100)
+    assert p.own(1, 1030, 1100)[0].size == 1 and (p.rows([1])[0, 16:18] >= 0).all()
+
+
+def test_reserve_grows_rows_with_a_window():
+    for window, sinks in ((1, 0), (64, 3), (130, 0), (200, 70)):
+        p = kb.Pager(12, 1, 40)
+        n = 0
+        for new in [70, 58, 64, 1, 63] + [37] * 40:
+            p.reserve(0, n + new)
+            p.trim(0, sinks, n - window + 1)            # what the next rows do not see
+            row = p.rows([0])[0]
+            for t in range(n, n + new):
+                j = np.arange(t + 1)
+                assert (row[j[(j > t - window) | (j < sinks)] // 64] >= 0).all()
+            n += new
+        assert n > 12 * 64
+
+
+# ---- as a server calls them ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("seed", range(6))
+def test_serving_with_rejected_tokens_windows_and_forks(seed):
+    """Random steps of sequences with a window: own, reserve, copies, rows written; some are not accepted and their pages
+    trimmed, at times a sequence is forked.  Every row written reads, through its sequence's pages, what the sequence wrote at each
+    position that it sees; and the calls refuse for want of pages alone."""
+    rng = np.random.RandomState(seed)
+    pages, seqs, width = [20, 9, 9, 16, 9, 24][seed], 5, 24
+    window, sinks = [(10**6, 0), (150, 5), (64, 70), (300, 0), (33, 1), (500, 128)][seed]
+    p = kb.Pager(pages, seqs, width)
+    pool = np.full((pages, 64), -1)
+    said = [[] for _ in range(seqs)]                    # what each sequence wrote
+    name = steps = refused = 0
+    for _ in range(1000):
+        s, op = int(rng.randint(seqs)), rng.rand()
+        n = len(said[s])
+        if op < 0.75:
+            new = int(rng.choice([1, 3, 30, 100]))
+            if n + new > 64 * width:
+                p.release(s)
+                said[s] = []
+                continue
+            try:
+                src, dst = p.own(s, n, n + new)
+                pool[dst] = pool[src]
+                p.reserve(s, n + new)
+            except kb.KvpError as e:
+                assert e.code == kb.KVP_E_CAPACITY
+                refused += 1
+                assert p.free_pages() < new // 64 + 2
+                p.release(s)
+                said[s] = []
+                continue
+            row = p.rows([s])[0]
+            t = np.arange(n, n + new)
+            pool[row[t // 64], t % 64] = name + t - n
+            said[s] = said[s] + list(range(name, name + new))
+            name += new
+            steps += 1
+            for at in t:
+                j = np.arange(at + 1)
+                j = j[(j > at - window) | (j < sinks)]
+                assert (row[j // 64] >= 0).all() and (pool[row[j // 64], j % 64] == np.array(said[s])[j]).all()
+            if rng.rand() < 0.4:                        # not all of them accepted
+                keep = n + int(rng.randint(0, new + 1))
+                said[s] = said[s][:keep]
+                p.trim(s, keep, 2**31 - 1 if rng.rand() < 0.5 else 64 * (-(-(n + new) // 64)))
+            p.trim(s, sinks, len(said[s]) - window + 1)
+        elif op < 0.85:
+            t = int(rng.randint(seqs))
+            if t != s and n:
+                p.release(t)
+                p.fork(s, t, n)
+                said[t] = list(said[s])
+        elif op < 0.95:
+            src, dst = p.compact(int(rng.randint(1, 8)))
+            pool[dst] = pool[src]
+        else:
+            p.release(s)
+            said[s] = []
+    assert steps > 300 and refused > 0
