@@ -383,7 +383,9 @@ int kvp_decode_step_noalloc(kvp_ctx* ctx, const void* x, const int32_t* len_dev,
  * maps position p of sequence b to page pages[b][p / 64], row p % 64, in every
  * producer's pool.  Entries are clamped to [0, n_pages) on the device, so a bad
  * entry reads or writes a wrong page of the pool but never leaves it; entries
- * covering positions a call touches must be mapped (kvp_pager_*).
+ * covering positions a call touches must be mapped (kvp_pager_*).  -1 marks an
+ * entry without a page: the calls on rows (kvp_append, kvp_step and their 8-bit
+ * forms) store nothing there, the others take it to page 0.
  */
 
 /* kvp_set_kv_pool -- producer l's page pools (device, caller-owned, 16-byte
@@ -521,7 +523,8 @@ typedef struct kvp_rows {
  * queries in bf16 (q_out == q with ld == a * d_h rotates in place).  Angles are evaluated in double, the rotation in
  * fp32, rounded once.  q with q_out, or k with v, may be NULL together; a consumer's k and v must
  * be (it rotates queries only).  Rows of no sequence and of inactive ones are left as they are in
- * q_out, positions that are not appended as they are in the pools.
+ * q_out, positions that are not appended as they are in the pools.  A row whose position has no page
+ * (-1 in the table) is rotated in q_out, and appended nowhere.
  * Errors: KVP_E_INVALID_ARG, KVP_E_CAPACITY, KVP_E_SHAPE, KVP_E_STATE (pools never set), KVP_E_HIP.
  */
 int kvp_append(kvp_ctx* ctx, int l, const void* q, const void* k, const void* v, int ld,
@@ -613,7 +616,8 @@ int kvp_page_bytes_fp8(const kvp_ctx* ctx, size_t* bytes);
  * fp32; keys and values go to 8 bits without a rounding between.  q with q_out, or k with v, may
  * be NULL together; a consumer's k and v must be (it rotates queries only).  Rows of no
  * sequence and of inactive ones are left as they are in q_out, positions that are not appended as they
- * are in the pools (but see the block's scale above).
+ * are in the pools (but see the block's scale above).  A row whose position has no page (-1 in the
+ * table) is rotated in q_out, and appended nowhere.
  * Errors: KVP_E_INVALID_ARG, KVP_E_CAPACITY, KVP_E_SHAPE, KVP_E_STATE (pools never set), KVP_E_HIP.
  */
 int kvp_append_fp8(kvp_ctx* ctx, int l, const void* q, const void* k, const void* v, int ld,

@@ -5,7 +5,7 @@
 // (append_rows_kernel): a workgroup owns the rows that fall into half a page of one sequence, for some of the head vectors
 // (Q, K, V): it evaluates the rotation of its at most 32 x 64 angles once, in double precision.  V is turned in registers: a lane
 // takes 8 dimensions of 8 positions, whose words it deals out again as 16-byte runs of positions.  One row a sequence
-// (append_row_kernel): a wave a head vector.  Only positions of the call's rows are written, each once.
+// (append_row_kernel): a wave a head vector.  Only positions of the call's rows that have a page are written, each once.
 //
 // Bound by memory: 2568 rows in 7 chunks (64 query heads, 8 K/V heads; 105 MB) 30 us, 3.5 TB/s (41 with workgroups of 64
 // positions and 8 vectors, 31 with 32 and 8 or 16); prompts of 4 x 4096 rows (16, 8; 268 MB) 68 us, 4.0 TB/s (67, 75); one row
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads) void append_rows_kernel(Src src, Args A, 
         }
     }
     __syncthreads();
-    if (hv >= A.first + A.vectors) return;
+    if (hv >= A.first + A.vectors || (z && page < 0)) return;
     if (z < 2) {
         const int c = lane & 7;
 #pragma unroll
@@ -130,12 +130,14 @@ __global__ __launch_bounds__(kThreads) void append_row_kernel(Src src, Args A, R
     }
     const Turns turns(th, lane);
     const int pos = s.len, p = pos % kPage;
-    const size_t at = (size_t)h * A.r.n_pages + page_of(A.r, b, pos);
+    const int page = page_of(A.r, b, pos);
+    const size_t at = (size_t)h * A.r.n_pages + max(page, 0);
     if (z < 2) {
         rotate(x1, x2, rotation(pos, turns));
         y1 = f2bf(x1);
         y2 = f2bf(x2);
     }
+    if (z && page < 0) return;
     uint16_t* o = z == 0   ? A.q_out + ((size_t)s.row0 * A.a + h) * kHead + lane
                   : z == 1 ? A.kc + (at * kPage + p) * kHead + lane
                            : A.vc + (at * kHead + lane) * kPage + p;

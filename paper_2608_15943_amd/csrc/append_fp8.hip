@@ -108,6 +108,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Src src, Args A, RopeF
                 }
                 continue;
             }
+            if (page < 0) continue;
             float* scp = A.sc + ((size_t)h * A.r.n_pages + page) * 2 * kPageBlks + pblk;
             const float old = lo > 0 ? *scp : 0.f;
             uint32_t m = 0;
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Src src, Args A, RopeF
                 }
             }
             if (lane == 0) *scp = n.s;
-        } else {
+        } else if (page >= 0) {
             // V: lane (grp, c) holds dimensions 8 c .. 8 c + 7 of places 4 grp .. 4 grp + 3, whose codes are word
             // grp of the dimensions' 16-byte runs; lanes of the four groups exchange words until each has two
             // whole runs, of dimensions 8 c + grp and 8 c + 4 + grp.
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(kThreads) void append_one_kernel(Src src, Args A, R
     src.template load<1>(s.row0, z, h * kHead + 64 + lane, &x2);
     const Turns turns(th, lane);
     const int pos = s.len, page = page_of(A.r, b, pos), pblk = pos / kBlk % kPageBlks, p = pos % kBlk;
-    const size_t at = (size_t)h * A.r.n_pages + page;
+    const size_t at = (size_t)h * A.r.n_pages + max(page, 0);
     float* scp = A.sc + at * 2 * kPageBlks + (z == 2 ? kPageBlks : 0) + pblk;
     const float old = z && p ? *scp : 0.f;
     if (z < 2) rotate(x1, x2, rotation(pos, turns));
@@ -216,6 +217,7 @@ __global__ __launch_bounds__(kThreads) void append_one_kernel(Src src, Args A, R
         o[64] = f2bf(x2);
         return;
     }
+    if (page < 0) return;
     const NewScale n(wave_maxu(max(__float_as_uint(x1) & 0x7FFFFFFFu, __float_as_uint(x2) & 0x7FFFFFFFu)), p > 0, old);
     const uint32_t c = n.bad ? 0u : e4m3_pack(x1 * n.inv, x2 * n.inv, 0.f, 0.f);
     if (z == 1) {

@@ -103,8 +103,11 @@ __device__ __forceinline__ bool find_item(const NewRows& r, int x, Count count, 
     return false;
 }
 
+// The page of a position that is appended, -1 where the table has none (nothing may be stored then); other entries are taken
+// to the pool's first or last page.
 __device__ __forceinline__ int page_of(const NewRows& r, int b, int pos) {
-    return min(max(r.pt[(size_t)b * r.stride + pos / kPage], 0), r.n_pages - 1);
+    const int page = r.pt[(size_t)b * r.stride + pos / kPage];
+    return page == -1 ? -1 : min(max(page, 0), r.n_pages - 1);
 }
 
 }  // namespace kvp
