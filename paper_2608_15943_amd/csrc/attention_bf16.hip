@@ -19,6 +19,7 @@
 #include <algorithm>
 
 #include "attn_rows.h"
+#include "part_length.h"
 
 namespace kvp {
 namespace {
@@ -490,8 +491,8 @@ __device__ __forceinline__ bool take_part(const AttnArgs& A, int x, bool join, P
         p->step = 1;
     } else {
         const int lane = threadIdx.x & 63;
-        // Items, and tiles if all blocks had as many as their sequence's longest: parts of ceil(tiles / (jobs - items)) tiles are
-        // jobs at most.  Sums alone, so that every workgroup finds the same number.
+        // Items, and tiles if all blocks had as many as their sequence's longest.  Sums alone, so that every workgroup finds the
+        // same length.
         SeqRows s{0, 0, 0, 0};
         int items = 0;
         float n_lane = 0.f;
@@ -505,9 +506,7 @@ __device__ __forceinline__ bool take_part(const AttnArgs& A, int x, bool join, P
                 t_lane += (uint64_t)items * most_tiles<WIN>(A, s);
             }
         }
-        const float room = (float)A.jobs - wave_sum(n_lane), tiles = wave_sum((float)t_lane) * 1.00001f;
-        longest = room < 1.f ? 1 << 30 : (int)fminf(ceilf(tiles / room), 1e9f);
-        longest = __builtin_amdgcn_readfirstlane(longest);
+        longest = __builtin_amdgcn_readfirstlane(part_length(A.jobs, wave_sum(n_lane), wave_sum((float)t_lane)));
         int item0 = 0, job0 = 0, n = 0;
         for (int b0 = 0;; b0 += 64) {
             if (b0 >= A.r.B) return false;
@@ -518,7 +517,7 @@ __device__ __forceinline__ bool take_part(const AttnArgs& A, int x, bool join, P
                     items = blocks_of(s, A.m) * A.g;
                 }
             }
-            const int tiles = items ? most_tiles<WIN>(A, s) : 0, k = (tiles + longest - 1) / longest, jobs = items * k;
+            const int tiles = items ? most_tiles<WIN>(A, s) : 0, k = parts_of(tiles, longest), jobs = items * k;
             int ie = 0, je = 0;            // before this lane's sequence
             if (A.r.B <= 8) {
                 // The sequence of the longest parts first: a few sequences end with short ones (3 chunks 118 us, in their order
@@ -563,7 +562,7 @@ __device__ __forceinline__ bool take_part(const AttnArgs& A, int x, bool join, P
         p->step = n;
     }
     it.template begin<WIN>(A);
-    p->parts = (it.n + longest - 1) / longest;
+    p->parts = parts_of(it.n, longest);
     return p->part < p->parts;
 }
 
