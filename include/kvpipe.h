@@ -551,7 +551,9 @@ int kvp_set_layer_window(kvp_ctx* ctx, int l, int window, int sinks);
  * statistics and sums in fp32, the weights rounded to bf16 (their sum is that of the rounded
  * ones).  What a position holds that a row does not see, infinities and NaN too, does not reach the
  * row; a value that is not finite makes that dimension NaN or infinite in the rows that see it, a key
- * that is not finite their whole row NaN where its score is +infinity or NaN.  max_new and max_pos choose between
+ * that is not finite their whole row NaN where its score is +infinity or NaN.  Range: largest magnitudes
+ * of a query and a key that multiply to at most 2^21 (scores of some 2^24, of which fp32 keeps units),
+ * values up to 2^80; a row past that may be infinite or NaN.  max_new and max_pos choose between
  * kernels: close bounds are faster.  Workspace: KVP_PHASE_STEP with B and rows.
  * Errors: as kvp_append, KVP_E_WORKSPACE.
  */
