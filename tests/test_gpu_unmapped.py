@@ -92,3 +92,40 @@ def test_step_where_there_is_no_page(new, fp8):
     for p, q, u in zip(got[1], want[1], start):
         q[:, table[2].tolist()] = u[:, table[2].tolist()]
         assert torch.equal(p.view(torch.uint8), q.view(torch.uint8))
+
+
+def test_rejected_tokens_give_their_pages_back():
+    """Two sequences that propose tokens, accept some and let go of the others' pages, which the other one may get, beside a fork
+    of the first; every step as the host's."""
+    say("[rejected tokens]")
+    pool, stride = 12, 8
+    s = Stack(4, 2, (0, 0, 2), pool, 3, seed=85)
+    p = kb.Pager(pool, 3, stride)
+    rng = np.random.default_rng(86)
+    lens, ids = [0, 0], [0, 1]
+    news = [[60, 30]] + [[int(rng.integers(1, 70)), int(rng.integers(1, 70))] for _ in range(14)]
+    gone = 0
+    for i, new in enumerate(news):
+        if i == 5:
+            p.fork(0, 2, lens[0])
+            for l in s.dev:
+                s.kv[l, 2] = s.kv[l, 0][:, : lens[0]].copy()
+            ids, lens = [0, 1, 2], lens + [lens[0]]
+        new = (new + [5])[: len(ids)]
+        for b, n, t in zip(ids, lens, new):
+            src, dst = p.own(b, n, n + t)
+            if src.size:
+                a, d = (torch.tensor(np.asarray(z, np.int32)).cuda() for z in (src, dst))
+                s.m.kvp_copy_pages(a.data_ptr(), d.data_ptr(), src.size, torch.cuda.current_stream().cuda_stream)
+            p.reserve(b, n + t)
+        x = _normal(rng, sum(new), s.h)
+        want = s.host(x, lens, new, seqs=ids)
+        got = s.step(x, lens, new, p.rows(ids))
+        assert np.abs(got - want).max() <= 2e-2 * np.abs(want).max(), (i, lens, new)
+        keep = [int(rng.integers(0, min(t, 12) + 1)) for t in new]
+        free = p.free_pages()
+        for j, (b, n, t, k) in enumerate(zip(ids, lens, new, keep)):
+            p.trim(b, n + k, 64 * stride)
+            lens[j] = n + k
+        gone += p.free_pages() - free
+    assert gone > 5
