@@ -7,9 +7,10 @@
 // takes 8 dimensions of 8 positions, whose words it deals out again as 16-byte runs of positions.  One row a sequence
 // (append_row_kernel): a wave a head vector.  Only positions of the call's rows that have a page are written, each once.
 //
-// Bound by memory: 2568 rows in 7 chunks (64 query heads, 8 K/V heads; 105 MB) 30 us, 3.5 TB/s (41 with workgroups of 64
-// positions and 8 vectors, 31 with 32 and 8 or 16); prompts of 4 x 4096 rows (16, 8; 268 MB) 68 us, 4.0 TB/s (67, 75); one row
-// of each of 8 sequences 3.2 us, the latency of three loads that depend on each other (length, page, row).
+// Bound by memory: 2568 rows in 7 chunks (64 query heads, 8 K/V heads; 105 MB) 26.7 us, 3.9 TB/s (a call from the host 30; 41
+// with workgroups of 64 positions and 8 vectors, 31 with 32 and 8 or 16); prompts of 4 x 4096 rows (16, 8; 268 MB) 68 us by such
+// calls, 4.0 TB/s (67, 75); one row of each of 8 sequences 3.2 us, the latency of three loads that depend on each other (length,
+// page, row).
 #include "rope_rows.h"
 
 namespace kvp {

@@ -748,14 +748,15 @@ void launch_few(int nw, int grid, const AttnArgs& A, hipStream_t st) {
     else hipLaunchKernelGGL((rows_few_kernel<4, NB, WIN>), dim3(grid), dim3(256), 0, st, A);
 }
 
-// Waves that take an item of few columns (16 nb) where a launch without a list and a join is the faster one, else 0.  tiles: of
-// the longest item.  One workgroup an item of 1, 2 and 4 waves against the list, 32 heads on 8, in us.  nb 1: 1 sequence of
-// 200 positions 8.4, 7.9, 7.7 and 10.3, of 500 13.5, 11.2, 11.0 and 10.1; 8 of 200 9.2, 8.2, 7.8 and 10.2, 500 16, 11.9,
-// 11.6 and 10.5; 16 of 500 16.7, 12.2, 11.8 and 13.1, 1000 31, 20, 19.5 and 18.8; 32 of 1000 39, 28, 27 and 31, 2000 74, 50, 49
-// and 53; 64 of 500 26.6, 27.3, 30 and 31.6, 2000 91, 94, 95 and 99; 100 of 500 44, 47, 53 and 51, 2000 165, 159, 169 and 156.  nb
-// 2 (8 rows a sequence): 1 of 500 17.9, 15.9, 14.7 and 11.5; 8 of 500 19.8, 16.9, 15.4 and 13.9; 16 of 1000 38, 26, 23.4 and
-// 27; 64 of 1000 52, 56, 60 and 68.  (Past 32 tiles one long sequence among short ones would cost more than there is to gain; 8
-// waves have too few registers: 18.9 for 1 of 500, nb 2.)
+// Waves that take an item of few columns (16 nb) where one launch without a join is the faster one, else 0.  tiles: of the
+// longest item.  One workgroup an item of 1, 2 and 4 waves against two launches (the list, or equal parts), 32 heads on 8, in us.
+// nb 1: 1 sequence of 200 positions 8.4, 7.9, 7.7 and 9.4, of 500 13.5, 11.2, 11.0 and 9.5; 8 of 200 9.2, 8.2, 7.8 and 9.2, 500
+// 16, 11.9, 11.6 and 9.7; 16 of 500 16.7, 12.2, 11.8 and 12.3, 1000 31, 20, 19.5 and 17.8; 32 of 1000 39, 28, 27 and 31, 2000 74,
+// 50, 49 and 53; 64 of 500 26.6, 27.3, 30 and 31.6, 2000 91, 94, 95 and 99; 100 of 500 44, 47, 53 and 51, 2000 165, 159, 169 and
+// 156.  nb 2 (8 rows a sequence): 1 of 500 17.9, 15.9, 14.7 and 10.5; 8 of 500 19.8, 16.9, 15.4 and 13.1; 16 of 1000 38, 26, 22.4
+// and 23.3; 64 of 1000 52, 56, 60 and 67.  The rule takes the slower one at three of these: 8 of 500 (4 waves, 20 %), 32 of 2000
+// (the list, 8 %) and 100 of 2000 (1 wave, 5 %).  (Past 32 tiles one long sequence among short ones would cost more than there is
+// to gain; 8 waves have too few registers: 18.9 for 1 of 500, nb 2.)
 int few_waves(int64_t items, int64_t tiles, int nb, int simds) {
     if (tiles > std::min<int64_t>(32, nb == 1 ? 4 + items / 11 : items < 96 ? 4 : 32)) return 0;
     return items <= simds / 4 ? 4 : items < simds / 2 ? 2 : 1;
@@ -771,7 +772,8 @@ int few_waves(int64_t items, int64_t tiles, int nb, int simds) {
 //
 // Parts by length (no more than a bound of each sequence's tiles says) cost nothing to find; parts by count, which the device
 // cuts from what the sequences really have, about 5 us more, and need no room for pieces that are not made.  Neither is better
-// throughout.  Measured, the best of 1, 2 and 3 blocks of 16 columns: whole, parts by length, by count; 32 heads on 8.  Alike: a
+// throughout.  The constants are fitted to sweeps over such launches on one card, most of them of 32 heads on 8; equal contexts of
+// several sequences and one long among short ones come out 10 to 20 % from the best.  Measured, the best of 1, 2 and 3 blocks of 16 columns: whole, parts by length, by count; 32 heads on 8.  Alike: a
 // prompt of 2000 rows 49, 60, 58; 4 prompts of 1000 51, 92, 72; 600 rows behind 3000 positions 64, 50, 59; 100 behind 30000
 // 446, 74, 75; 400 behind 30000 448, 214, 198; 8 x 100 behind 3000 67, 62, 72.  Unlike: 4 x 100-800 behind 0-3000 96, 82, 68;
 // 3 x 333-1001 behind 700-5000 147, 118, 120; 3 x 50-500 behind 100-20000 321, 120, 101; 16 x 9-200 behind 10-6000 153, 121,
