@@ -771,13 +771,14 @@ int few_waves(int64_t items, int64_t tiles, int nb, int simds) {
 // without a context, of which the longest begin).
 //
 // Parts by length (no more than a bound of each sequence's tiles says) cost nothing to find; parts by count, which the device
-// cuts from what the sequences really have, about 5 us more, and need no room for pieces that are not made.  Neither is better
-// throughout.  The constants are fitted to sweeps over such launches on one card, most of them of 32 heads on 8; equal contexts of
-// several sequences and one long among short ones come out 10 to 20 % from the best.  Measured, the best of 1, 2 and 3 blocks of 16 columns: whole, parts by length, by count; 32 heads on 8.  Alike: a
-// prompt of 2000 rows 49, 60, 58; 4 prompts of 1000 51, 92, 72; 600 rows behind 3000 positions 64, 50, 59; 100 behind 30000
-// 446, 74, 75; 400 behind 30000 448, 214, 198; 8 x 100 behind 3000 67, 62, 72.  Unlike: 4 x 100-800 behind 0-3000 96, 82, 68;
-// 3 x 333-1001 behind 700-5000 147, 118, 120; 3 x 50-500 behind 100-20000 321, 120, 101; 16 x 9-200 behind 10-6000 153, 121,
-// 109; 2 x 300-2000 behind 1000-40000 (64 heads) 1201, no room, 571.
+// cuts from what the sequences really have, about 5 us more, and need no room for pieces that are not made.  Neither is
+// better throughout.  The constants are fitted to sweeps over such launches on one card, most of them of 32 heads on 8; equal
+// contexts of several sequences and one long among short ones come out 10 to 20 % from the best.  Measured, the best of 1, 2
+// and 3 blocks of 16 columns: whole, parts by length, by count; 32 heads on 8.  Alike: a prompt of 2000 rows 49, 60, 58; 4
+// prompts of 1000 51, 92, 72; 600 rows behind 3000 positions 64, 50, 59; 100 behind 30000 446, 74, 75; 400 behind 30000 448,
+// 214, 198; 8 x 100 behind 3000 67, 62, 72.  Unlike: 4 x 100-800 behind 0-3000 96, 82, 68; 3 x 333-1001 behind 700-5000 147,
+// 118, 120; 3 x 50-500 behind 100-20000 321, 120, 101; 16 x 9-200 behind 10-6000 153, 121, 109; 2 x 300-2000 behind
+// 1000-40000 (64 heads) 1201, no room, 571.
 struct Cut {
     int nb = 0, longest = 0, parts = 0, jobs = 0, grid = 0, m = 0, cols = 0, slots = 0;
     int64_t items = 0, sparse = 0, most = 0;      // a bound of the items, and with every sequence as long as the longest
