@@ -384,8 +384,9 @@ int kvp_decode_step_noalloc(kvp_ctx* ctx, const void* x, const int32_t* len_dev,
  * producer's pool.  Entries are clamped to [0, n_pages) on the device, so a bad
  * entry reads or writes a wrong page of the pool but never leaves it; entries
  * covering positions a call touches must be mapped (kvp_pager_*).  -1 marks an
- * entry without a page: the calls on rows (kvp_append, kvp_step and their 8-bit
- * forms) store nothing there, the others take it to page 0.
+ * entry without a page: the decode step and the calls on rows (kvp_append,
+ * kvp_step and their 8-bit forms) store nothing there; reads, and
+ * kvp_prefill_paged, take it to page 0.
  */
 
 /* kvp_set_kv_pool -- producer l's page pools (device, caller-owned, 16-byte
@@ -413,8 +414,8 @@ int kvp_prefill_paged(kvp_ctx* ctx, const void* x, void* y, int B, int S, const 
 /*
  * kvp_decode_step_paged -- kvp_decode_step over the pools: every producer
  * appends at position len_b of row b of `pages`, and every layer attends over
- * positions [0, len_b] through it.  Same kernels and arithmetic as
- * kvp_decode_step (bit-identical y).  Errors: as kvp_decode_step, with
+ * positions [0, len_b] through it.  A token whose position has no page (-1) is
+ * appended nowhere.  Same kernels and arithmetic as kvp_decode_step (bit-identical y).  Errors: as kvp_decode_step, with
  * KVP_E_CAPACITY when max_len >= 64 * pages_stride; KVP_E_STATE, KVP_E_SHAPE.
  */
 int kvp_decode_step_paged(kvp_ctx* ctx, const void* x, const int32_t* len_dev, int max_len,

@@ -179,7 +179,9 @@ __global__ __launch_bounds__(256) void decode_qkv_epi_kernel(const float* __rest
     // heads' blocks: the slot of sequence b, or page pos / 64 of the head-major pools.
     size_t kv0, hstride;
     int vld, row;
+    bool stored = true;        // false: the position has no page
     if (pages.pt) {
+        stored = has_page(pages, b, pos / kPage);
         kv0 = (size_t)page_at(pages, b, pos / kPage) * kPage;
         hstride = (size_t)pages.n * kPage;
         vld = kPage;
@@ -231,12 +233,12 @@ __global__ __launch_bounds__(256) void decode_qkv_epi_kernel(const float* __rest
         if (h < a) {
             q[(size_t)b * a * D + h * D + i] = f2bf(o1);
             q[(size_t)b * a * D + h * D + i + HALF] = f2bf(o2);
-        } else {
+        } else if (stored) {
             const size_t kb = (kv0 + (size_t)(h - a) * hstride + row) * D;
             kc[kb + i] = f2bf(o1);
             kc[kb + i + HALF] = f2bf(o2);
         }
-    } else {
+    } else if (stored) {
         const int e = j - npairs, h = e / D, c = e - h * D;
         vc[(kv0 + (size_t)h * hstride) * D + (size_t)c * vld + row] = f2bf(val(0, c0));
     }
@@ -359,8 +361,10 @@ __global__ __launch_bounds__(1024) void gemm_decode_fused_kernel(const uint16_t*
     } else {
         // Rows (in units of D elements) of head 0's block holding pos and the stride between
         // heads' blocks: the slot of sequence b, or page pos / 64 of the head-major pools.
+        // False: the position has no page.
         auto place = [&](int b, int pos, size_t& kv0, size_t& hstride, int& vld, int& prow) {
             if (fq.pages.pt) {
+                if (!has_page(fq.pages, b, pos / kPage)) return false;
                 kv0 = (size_t)page_at(fq.pages, b, pos / kPage) * kPage;
                 hstride = (size_t)fq.pages.n * kPage;
                 vld = kPage;
@@ -371,6 +375,7 @@ __global__ __launch_bounds__(1024) void gemm_decode_fused_kernel(const uint16_t*
                 vld = fq.cap;
                 prow = pos;
             }
+            return true;
         };
         if (rot) {
             for (int t = threadIdx.x; t < 8 * M; t += blockDim.x) {
@@ -396,7 +401,7 @@ __global__ __launch_bounds__(1024) void gemm_decode_fused_kernel(const uint16_t*
                 } else {
                     size_t kv0, hstride;
                     int vld, prow;
-                    place(row, pos, kv0, hstride, vld, prow);
+                    if (!place(row, pos, kv0, hstride, vld, prow)) continue;
                     const size_t kb = (kv0 + (size_t)(h - fq.a) * hstride + prow) * D;
                     fq.kc[kb + i] = f2bf(o1);
                     fq.kc[kb + i + HALF] = f2bf(o2);
@@ -409,7 +414,7 @@ __global__ __launch_bounds__(1024) void gemm_decode_fused_kernel(const uint16_t*
                 const int e = 16 * j - nrot + c, h = e / D, d = e - h * D;
                 size_t kv0, hstride;
                 int vld, prow;
-                place(row, pos, kv0, hstride, vld, prow);
+                if (!place(row, pos, kv0, hstride, vld, prow)) continue;
                 fq.vc[(kv0 + (size_t)h * hstride) * D + (size_t)d * vld + prow] = f2bf(sum(row, c));
             }
         }

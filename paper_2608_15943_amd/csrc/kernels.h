@@ -26,6 +26,8 @@ struct Pages {
 __device__ __forceinline__ int page_at(const Pages& pg, int b, int j) {
     return min(max(pg.pt[(size_t)b * pg.stride + j], 0), pg.n - 1);
 }
+// Whether entry j has a page (-1: none); the appends of single tokens store nothing where it has none.
+__device__ __forceinline__ bool has_page(const Pages& pg, int b, int j) { return pg.pt[(size_t)b * pg.stride + j] != -1; }
 
 // ---- bf16 prefill ---------------------------------------------------------
 

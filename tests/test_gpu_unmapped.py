@@ -129,3 +129,44 @@ def test_rejected_tokens_give_their_pages_back():
             lens[j] = n + k
         gone += p.free_pages() - free
     assert gone > 5
+
+
+@pytest.mark.parametrize("B,a,w4", [(3, 4, None), (20, 4, None), (3, 3, None), (5, 4, 64)])
+def test_decode_step_where_there_is_no_page(B, a, w4):
+    """The same of kvp_decode_step_paged, whose single tokens go through other kernels: of small batches, of larger ones, of a
+    width that no small-batch kernel takes, with 4-bit weights."""
+    say(f"[unmapped decode] B={B} a={a} w4={w4}")
+    table, n_pages = _scattered(B, 2, 82)
+    s = Stack(a, 1, (0, 0, 2), n_pages, B, seed=82, w4=w4)
+    rng = np.random.default_rng(83)
+    for d in s.dev.values():
+        for t in d:
+            t.copy_(torch.randn(t.shape, device="cuda"))
+    start = [t.clone() for d in s.dev.values() for t in d]
+    lens = [(37 * b + 60) % 127 for b in range(B)]
+    gone = [0, B - 1]
+    n = s.m.kvp_workspace_size(kb.KVP_PHASE_DECODE, B, 1)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    x = _dev(_normal(rng, B, s.h))
+    dl = torch.tensor(lens, dtype=torch.int32, device="cuda")
+
+    def step(table):
+        for t, u in zip((t for d in s.dev.values() for t in d), start):
+            t.copy_(u)
+        pt = torch.from_numpy(table).cuda()
+        y = torch.empty_like(x)
+        s.m.kvp_decode_step_paged(x.data_ptr(), dl.data_ptr(), 127, pt.data_ptr(), 2, y.data_ptr(), B, ws.data_ptr(), n,
+                                  torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        return y, [t.clone() for d in s.dev.values() for t in d]
+
+    want = step(table)
+    bad = table.copy()
+    for b in gone:
+        bad[b, lens[b] // 64] = -1
+    got = step(bad)
+    rest = [b for b in range(B) if b not in gone]
+    assert torch.equal(got[0][rest], want[0][rest])
+    for p, q, u in zip(got[1], want[1], start):
+        q[:, table[gone].ravel().tolist()] = u[:, table[gone].ravel().tolist()]
+        assert torch.equal(p, q)
